@@ -66,7 +66,11 @@ typedef enum {
                                /* buffer holds (pdec_attn_step_noalloc only)             */
 } pdec_status;
 
-typedef enum { PDEC_DTYPE_F32 = 0, PDEC_DTYPE_BF16 = 1 } pdec_dtype;
+typedef enum {
+    PDEC_DTYPE_F32 = 0,
+    PDEC_DTYPE_BF16 = 1,
+    PDEC_DTYPE_E4M3 = 2 /* 8-bit cache rows (paged caches only): OCP e4m3 with one scale per token and kv head */
+} pdec_dtype;
 
 /* Sizes of one call.  All fields are host values. */
 typedef struct pdec_dims {
@@ -513,6 +517,153 @@ int pdec_attn_prefill_backward(const pdec_dims* dims, const void* q, const void*
                                const int32_t* prefix_lens, const void* out, const float* lse, const void* dout,
                                float* dq, float* dk_prefix, float* dv_prefix, float* dk_event, float* dv_event,
                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Paged caches ----
+ *
+ * A pool of pages holds the keys and values of many sequences (videos whose
+ * prefix is prefilled in chunks, or streams with caches of their own):
+ *   k_pages, v_pages [num_pages, page_size, H_kv, D]   token-major within a page
+ * and key t of sequence s is row t % page_size of page
+ * block_table[s][t / page_size].  Consecutive pages are a dense prefix: a
+ * sequence whose table counts up can be given to the dense entry points as it
+ * lies.  A table entry outside [0, num_pages) holds no keys: rows written to
+ * it are dropped, and its keys are hidden from every query.
+ *
+ * The rows are of the element type of q (float32 or bfloat16), or in 8 bits
+ * (PDEC_DTYPE_E4M3) with one power of two per token and kv head:
+ *   k_scales, v_scales [num_pages, H_kv, page_size] uint8, value = e4m3 * 2^(byte - 127).
+ * The append writes bytes 1..246; a byte of 0 counts as a scale of 0.
+ *
+ * A call serves a ragged batch of num_seqs sequences.  The new tokens of
+ * sequence s are rows [cu_tokens[s], cu_tokens[s+1]) of q, out, lse, k_new and
+ * v_new; a sequence may have none.  Rows of these behind the last sequence's
+ * (a padded batch) are neither read nor written.
+ *   cu_tokens   [num_seqs + 1] int32, device, from 0, non-decreasing, at most num_tokens
+ *   block_table [num_seqs, max_pages] int32, device
+ *   seq_lens    [num_seqs] int32, device: keys of the sequence, its new tokens included
+ * Lengths and offsets in device memory are a caller contract, as for the step
+ * calls; a value outside it gives wrong results, never a stray access.  With
+ * PDEC_DEBUG=1 the calls check them (pdec_check_paged_lengths), synchronising.
+ */
+typedef struct pdec_paged_dims {
+    int32_t num_seqs;     /* S >= 1                                                              */
+    int32_t num_tokens;   /* rows of q/out/lse (of k_new/v_new), >= 1                            */
+    int32_t num_q_heads;  /* H_q, a multiple of num_kv_heads                                     */
+    int32_t num_kv_heads; /* H_kv                                                                */
+    int32_t head_dim;     /* D: 64 or 128                                                        */
+    int32_t page_size;    /* tokens per page: a power of two, 16..1024                           */
+    int32_t num_pages;    /* pages of the pool, >= 1                                             */
+    int32_t max_pages;    /* columns of block_table, >= 1; max_pages * page_size <= 2^30         */
+    int32_t max_chunk;    /* upper bound on one sequence's new tokens; 0 means num_tokens        */
+    int32_t max_len;      /* upper bound on any sequence's keys; 0 means max_pages * page_size   */
+    int32_t dtype;        /* PDEC_DTYPE_F32 or PDEC_DTYPE_BF16: q, out, k_new, v_new, dense rows */
+    int32_t cache_dtype;  /* dtype, or PDEC_DTYPE_E4M3                                           */
+    int32_t causal;       /* attention: 1: new token i of n sees keys t <= len - n + i; 0: all   */
+                          /* new tokens see all len keys (the event streams' queries against a   */
+                          /* shared prefix; queries against another sequence's states)           */
+    float softmax_scale;  /* attention: <= 0 selects 1/sqrt(head_dim)                            */
+} pdec_paged_dims;
+
+/*
+ * Appends the new tokens' keys and values to their sequences' pages: with
+ * n = lens_in[s] the keys of s before, token i of s becomes key n + i, and
+ * lens_out[s] is n plus the new tokens.  A sequence whose tokens do not all
+ * fit (n + new > max_len), or whose lens_in is negative, is left as it was
+ * with lens_out[s] = lens_in[s].
+ *   k_new, v_new [num_tokens, H_kv, D] device, 16-byte aligned;
+ *   lens_in, lens_out [S] int32, device, different arrays;
+ *   k_scales, v_scales: e4m3 cache only, else NULL.
+ * A row x of D elements goes to an e4m3 cache as e4m3(x / 2^k), to nearest
+ * even, k the least integer in [-126, 119] with max |x| / 2^k <= 448 over the
+ * finite elements (0 if they are all 0), and the byte k + 127.  Dividing by a
+ * power of two is exact, so each element is rounded once: by at most 2^-4 of
+ * its value, or 2^(k-10).  Infinities and NaNs become NaN, magnitudes above
+ * 448 * 2^119 become that.
+ * Pages that receive rows must not be shared by two sequences of the call.
+ * num_q_heads, max_chunk, causal and softmax_scale are ignored.
+ * Asynchronous on `stream`.  Returns a pdec_status.
+ */
+int pdec_paged_kv_append(const pdec_paged_dims* dims, const void* k_new, const void* v_new, const int32_t* cu_tokens,
+                         const int32_t* block_table, const int32_t* lens_in, int32_t* lens_out, void* k_pages,
+                         void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream);
+
+/*
+ * The first cu_rows[s+1] - cu_rows[s] keys and values of every sequence as
+ * dense rows, in dims->dtype (exact: an e4m3 value times a power of two):
+ * row cu_rows[s] + t of k_out / v_out receives key t of s.  Rows t at or
+ * beyond seq_lens[s], and rows of absent pages, receive 0.
+ *   cu_rows [S + 1] int32, device, as cu_tokens, at most num_tokens;
+ *   k_out, v_out [num_tokens, H_kv, D] device, 16-byte aligned.  Rows behind
+ *   the last sequence's are left as they were.
+ * num_q_heads, max_chunk, causal and softmax_scale are ignored.
+ * Asynchronous on `stream`.  Returns a pdec_status.
+ */
+int pdec_paged_kv_read(const pdec_paged_dims* dims, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                       const uint8_t* v_scales, const int32_t* block_table, const int32_t* seq_lens,
+                       const int32_t* cu_rows, void* k_out, void* v_out, void* stream);
+
+/* Bytes of workspace pdec_paged_attn needs (0 for invalid dims).  Host only. */
+size_t pdec_paged_workspace_size(const pdec_paged_dims* dims);
+
+/* The kernels a pdec_paged_attn call uses, for tests and measurement. */
+typedef struct pdec_paged_plan {
+    int32_t rows_few;   /* rows (new tokens x H_q / H_kv) per work item of the kernel for      */
+                        /* sequences of few rows; 0: not launched                              */
+    int32_t rows_many;  /* the same of the kernel for many rows; 0: not launched               */
+    int32_t workers;    /* work-groups that share the keys of each of the two                  */
+    int32_t merge_pass; /* 1 if partial states are merged by a pass of their own               */
+} pdec_paged_plan;
+
+/* Host only.  Returns a pdec_status. */
+int pdec_query_paged_plan(const pdec_paged_dims* dims, pdec_paged_plan* plan);
+
+/*
+ * Attention of the new tokens over their sequences' pages, the tokens' own
+ * keys among them (append first, then attend): one new token per sequence (a
+ * decode step), chunks of a prefill, drafted tokens, or any mixture.
+ * Query i of sequence s, head h sees the keys t < min(len, len - n + i + 1)
+ * (causal) or t < len (not causal) on pages that are present;
+ *   out = sum_t p_t v_t, p_t = exp(scale <q, k_t> - lse), lse the log-sum-exp;
+ * a query that sees nothing gets 0 and -inf.  Hidden keys and values, whatever
+ * they hold (infinities and NaNs too), do not reach a query's result.
+ *   q, out [num_tokens, H_q, D], lse [num_tokens, H_q] float32 or NULL;
+ *   workspace >= pdec_paged_workspace_size(dims) bytes, device, 16-byte
+ *   aligned, contents ignored.
+ * Softmax statistics and sums are float32; for bfloat16 the probabilities meet
+ * the values in bfloat16, as in the step calls, while lse and the normaliser
+ * are sums of the unrounded ones.  Repeated calls agree bit for bit.
+ * Asynchronous on `stream`.  Returns a pdec_status.
+ */
+int pdec_paged_attn(const pdec_paged_dims* dims, const void* q, const void* k_pages, const void* v_pages,
+                    const uint8_t* k_scales, const uint8_t* v_scales, const int32_t* block_table,
+                    const int32_t* cu_tokens, const int32_t* seq_lens, void* out, float* lse, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/*
+ * The paged calls' contract for lengths, checked on HOST copies: cu starts at
+ * 0, never decreases and ends at most at num_tokens; 0 <= seq_lens[s] <=
+ * max_len; with attn != 0 also cu[s+1] - cu[s] <= max_chunk.  Returns
+ * PDEC_OK, PDEC_ERR_BAD_LENGTHS, or PDEC_ERR_INVALID_ARG.  Host only.
+ */
+int pdec_check_paged_lengths(const pdec_paged_dims* dims, const int32_t* cu, const int32_t* seq_lens, int32_t attn);
+
+/*
+ * Attention over two disjoint sets of keys joined into attention over both:
+ * of each of num_rows rows, with m = max(lse_a, lse_b), w = exp(lse - m),
+ *   out = (w_a out_a + w_b out_b) / (w_a + w_b),  lse = m + log(w_a + w_b).
+ * A side whose lse is -inf (it saw no key) is left out, whatever its out row
+ * holds; two such sides give 0 and -inf.  For instance pdec_paged_attn over a
+ * video's shared prefix (causal 0) and pdec_attn_step over the streams' own
+ * rows (max_prefix_len 0) join to the event-parallel step over both.
+ *   out_a, out_b, out [num_rows, head_dim] of dtype (float32 or bfloat16),
+ *   head_dim 64 or 128, 16-byte aligned, device; lse_a, lse_b, lse
+ *   [num_rows] float32, device.  out may be out_a or out_b, and lse lse_a or
+ *   lse_b (in place); lse may be NULL.  Products and sums are float32.
+ * Asynchronous on `stream`.  Returns a pdec_status.
+ */
+int pdec_merge_states(int64_t num_rows, int32_t head_dim, int32_t dtype, const void* out_a, const float* lse_a,
+                      const void* out_b, const float* lse_b, void* out, float* lse, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,250 @@
+// Writing rows to a paged cache and reading them back, and the join of two
+// attention results.
+//
+// All three move memory: a row in, a row out, a few operations per element.
+// 16-byte accesses; the sequence of a row is found once per wave by counting
+// the offsets at or below it (64 at a time, one memory round trip for up to 64
+// sequences, where a binary search would take one per halving).
+#pragma once
+
+#include "kernel_mfma.h"
+#include "paged_common.h"
+
+namespace pdec {
+
+struct PagedIoArgs {
+    const void* k_rows;  // append: k_new, v_new; read: k_out, v_out
+    const void* v_rows;
+    void* k_pages;
+    void* v_pages;
+    uint8_t* k_scales;
+    uint8_t* v_scales;
+    const int32_t* block_table;
+    const int32_t* cu;
+    const int32_t* lens;  // append: before; read: keys
+    int32_t* lens_out;    // append
+    int num_seqs, num_tokens, H_kv;
+    int page_shift, num_pages, max_pages, max_len;
+};
+
+// Sequence of row t (uniform over the wave): the last s with cu[s] <= t among
+// those with rows, or -1 for a row behind the last sequence's.
+__device__ inline int paged_owner(const PagedIoArgs& a, int t)
+{
+    const int lane = paged_lane();
+    int below = 0;  // ends cu[s + 1] at or below t: as many whole sequences lie before it
+    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
+        const int s = s0 + lane;
+        const uint64_t b = __ballot(s < a.num_seqs && a.cu[s + 1] <= t);
+        below += __builtin_popcountll(b);
+        if (~b) break;
+    }
+    return below < a.num_seqs ? below : -1;
+}
+
+__device__ inline int paged_io_page(const PagedIoArgs& a, int s, int t)
+{
+    const int p = a.block_table[(long)s * a.max_pages + (t >> a.page_shift)];
+    return (uint32_t)p < (uint32_t)a.num_pages ? p : -1;
+}
+
+// Eight consecutive elements of a row.
+template <typename T>
+struct Row8 {
+    u32x4_t x[sizeof(T) / 2];
+    __device__ inline void load(const void* p)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = static_cast<const u32x4_t*>(p)[i];
+    }
+    __device__ inline void store(void* p) const
+    {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) static_cast<u32x4_t*>(p)[i] = x[i];
+    }
+    __device__ inline float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(x[i >> 2][i & 3]);
+        else return __uint_as_float((i & 1) ? x[0][i >> 1] & 0xffff0000u : x[0][i >> 1] << 16);
+    }
+    __device__ inline void set(const float (&v)[8])
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i >> 2][i & 3] = __float_as_uint(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[0][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        }
+    }
+};
+
+// Eight elements of a row of D, D / 8 lanes to a row, as e4m3 with the row's
+// power of two: its byte in `byte`, the same in all of the row's lanes.
+// Infinities and NaNs are stored as NaN.  |x| 2^-k is at most 448, but for
+// magnitudes beyond 448 * 2^119, which become that (a larger power of two would
+// let a rounded-up value pass float32's range when read back).
+template <int D, typename T>
+__device__ inline uint2 quantise8(const Row8<T>& r, int& byte)
+{
+    uint32_t top = 0;  // |x| as its bits, which order as the values do
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t u = __float_as_uint(r.get(i)) & 0x7fffffffu;
+        top = u < 0x7f800000u ? max(top, u) : top;
+    }
+#pragma unroll
+    for (int off = 1; off < D / 8; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
+    // top = m 2^e, 1 <= m < 2, and 448 = 1.75 * 2^8: k = e - 8, one more where m > 1.75
+    // (a top below 2^-126 has e <= -127 and gets the least k)
+    int k = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+    k = top ? min(max(k, -126), 119) : 0;
+    byte = k + 127;
+    const float inv = __uint_as_float((uint32_t)(127 - k) << 23);  // 2^-k, 2^-119 .. 2^126
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const float x0 = r.get(i), x1 = r.get(i + 1);
+        int v = 0;
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(fminf(fmaxf(x0 * inv, -448.f), 448.f), fminf(fmaxf(x1 * inv, -448.f), 448.f), v, false);
+        if ((__float_as_uint(x0) & 0x7f800000u) == 0x7f800000u) v |= 0x7f;
+        if ((__float_as_uint(x1) & 0x7f800000u) == 0x7f800000u) v |= 0x7f00;
+        w[i / 4] |= ((uint32_t)v & 0xffffu) << (8 * (i & 2));
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+// One wave per token and tensor, its H_kv D elements in steps of 512.
+// grid (max(tokens, sequences / 64), 2).
+template <int D, typename T, bool QUANT>
+__global__ __launch_bounds__(64) void paged_append_kernel(PagedIoArgs a)
+{
+    const int t = blockIdx.x, lane = threadIdx.x;
+    const bool is_v = blockIdx.y != 0;
+    const int elems = a.H_kv * D;
+    const T* src = static_cast<const T*>(is_v ? a.v_rows : a.k_rows) + (long)t * elems;
+    Row8<T> row;
+    const bool token = t < a.num_tokens;  // work-groups beyond serve the counts of many sequences
+    if (token && 8 * lane < elems) row.load(src + 8 * lane);  // under the look-ups
+    // the counts after the append, by the first work-groups
+    if (!is_v && t < (a.num_seqs + 63) / 64) {
+        for (int s = 64 * t + lane; s < min(a.num_seqs, 64 * t + 64); s += 64) {
+            const int n = a.lens[s], m = min(max(a.cu[s + 1], 0), a.num_tokens) - min(max(a.cu[s], 0), a.num_tokens);
+            a.lens_out[s] = n >= 0 && m > 0 && n <= a.max_len - m ? n + m : n;
+        }
+    }
+    if (!token) return;
+    const int s = paged_owner(a, t);
+    if (s < 0) return;
+    const int n = a.lens[s], t0 = a.cu[s], m = min(a.cu[s + 1], a.num_tokens) - t0;
+    if (t0 < 0 || t < t0 || n < 0 || n > a.max_len - m) return;
+    const int key = n + t - t0;
+    const int page = paged_io_page(a, s, key);
+    if (page < 0) return;
+    const int slot = key & ((1 << a.page_shift) - 1);
+    const long at = (((long)page << a.page_shift) + slot) * elems;
+    unsigned char* dst = static_cast<unsigned char*>(is_v ? a.v_pages : a.k_pages) + at * (QUANT ? 1 : (int)sizeof(T));
+    for (int e = 8 * lane; e < elems; e += 512) {
+        if (e >= 512) row.load(src + e);
+        if constexpr (QUANT) {
+            int byte;
+            *reinterpret_cast<uint2*>(dst + e) = quantise8<D>(row, byte);
+            if (e % D == 0) {
+                uint8_t* sc = is_v ? a.v_scales : a.k_scales;
+                sc[(((long)page * a.H_kv + e / D) << a.page_shift) + slot] = (uint8_t)byte;
+            }
+        } else {
+            row.store(dst + e * (int)sizeof(T));
+        }
+    }
+}
+
+// A wave takes kReadRows consecutive rows of one tensor.  grid (rows / (4 kReadRows), 2).
+constexpr int kReadRows = 8;
+
+template <int D, typename T, bool QUANT>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const bool is_v = blockIdx.y != 0;
+    const int elems = a.H_kv * D;
+    const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kReadRows;
+    const int r1 = min(r0 + kReadRows, a.num_tokens);
+    if (r0 >= r1) return;
+    const unsigned char* pages = static_cast<const unsigned char*>(is_v ? a.v_pages : a.k_pages);
+    const uint8_t* scales = is_v ? a.v_scales : a.k_scales;
+    T* out = static_cast<T*>(const_cast<void*>(is_v ? a.v_rows : a.k_rows));
+    int s = paged_owner(a, r0);
+    if (s < 0) return;
+    int end = __builtin_amdgcn_readfirstlane(a.cu[s + 1]), first = __builtin_amdgcn_readfirstlane(a.cu[s]);
+    int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[s], 0), a.max_len));
+    for (int r = r0; r < r1; ++r) {
+        while (r >= end) {
+            if (++s >= a.num_seqs) return;
+            first = end;
+            end = __builtin_amdgcn_readfirstlane(a.cu[s + 1]);
+            len = __builtin_amdgcn_readfirstlane(min(max(a.lens[s], 0), a.max_len));
+        }
+        const int key = r - first;
+        const int page = key >= 0 && key < len ? __builtin_amdgcn_readfirstlane(paged_io_page(a, s, key)) : -1;
+        const int slot = key & ((1 << a.page_shift) - 1);
+        const long at = (((long)max(page, 0) << a.page_shift) + slot) * elems;
+        for (int e = 8 * lane; e < elems; e += 512) {
+            Row8<T> row;
+            if (page < 0) {
+                const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                row.set(z);
+            } else if constexpr (QUANT) {
+                const uint2 x = *reinterpret_cast<const uint2*>(pages + at + e);
+                const float sc = __uint_as_float((uint32_t)scales[(((long)page * a.H_kv + e / D) << a.page_shift) + slot] << 23);
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const int word = (int)(i ? x.y : x.x);
+                    const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
+                    v[i] = lo.x * sc, v[i + 1] = lo.y * sc, v[i + 2] = hi.x * sc, v[i + 3] = hi.y * sc;
+                }
+                row.set(v);
+            } else {
+                row.load(pages + (at + e) * (int)sizeof(T));
+            }
+            row.store(out + (long)r * elems + e);
+        }
+    }
+}
+
+// Eight elements per lane; a row's lanes are in one work-group.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void merge_states_kernel(long rows, const void* oa, const float* la, const void* ob,
+                                                           const float* lb, void* out, float* lse)
+{
+    constexpr int PER = D / 8;
+    const long i = (long)blockIdx.x * 256 + threadIdx.x, r = i / PER;
+    float x = 0.f, y = 0.f;
+    Row8<T> p, q;
+    const bool in = r < rows;
+    if (in) {
+        p.load(static_cast<const T*>(oa) + 8 * i);
+        q.load(static_cast<const T*>(ob) + 8 * i);
+        x = la[r];
+        y = lb[r];
+    }
+    __syncthreads();  // in place: one lane writes the lse that the row's other lanes read
+    if (!in) return;
+    const float m = fmaxf(x, y);
+    const bool use_a = x != kNegInf, use_b = y != kNegInf;
+    const float wa = use_a ? expf(x - m) : 0.f, wb = use_b ? expf(y - m) : 0.f;
+    const float total = wa + wb;
+    const float inv = (use_a | use_b) ? 1.f / total : 0.f;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float u = use_a ? wa * p.get(k) : 0.f;
+        v[k] = (use_b ? fmaf(wb, q.get(k), u) : u) * inv;
+    }
+    p.set(v);
+    p.store(static_cast<T*>(out) + 8 * i);
+    if (lse && i == r * PER) lse[r] = (use_a | use_b) ? m + logf(total) : kNegInf;
+}
+
+}  // namespace pdec

@@ -1,0 +1,382 @@
+// C ABI of the paged caches (include/pdec.h): argument checks, the plan of an
+// attention call, and the launches of kernel_paged_*.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <vector>
+
+#include "pdec.h"
+
+#include "kernel_paged_f32.h"
+#include "kernel_paged_finish.h"
+#include "kernel_paged_io.h"
+
+namespace pdec {
+
+namespace {
+
+template <int D, typename TQ, typename TC>
+void launch_f32_rows(const PagedArgs& a, dim3 grid, hipStream_t s)
+{
+    if (a.rows == 16) hipLaunchKernelGGL((paged_f32_kernel<D, 1, TQ, TC>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_f32_kernel<D, 2, TQ, TC>), grid, dim3(256), 0, s, a);
+}
+
+template <int D>
+void launch_f32_types(const PagedArgs& a, int dtype, int cache_dtype, dim3 grid, hipStream_t s)
+{
+    if (dtype == PDEC_DTYPE_F32) {
+        if (cache_dtype == PDEC_DTYPE_F32) launch_f32_rows<D, float, float>(a, grid, s);
+        else launch_f32_rows<D, float, fp8_t>(a, grid, s);
+    } else {
+        if (cache_dtype == PDEC_DTYPE_BF16) launch_f32_rows<D, uint16_t, uint16_t>(a, grid, s);
+        else launch_f32_rows<D, uint16_t, fp8_t>(a, grid, s);
+    }
+}
+
+int paged_grid(const PagedArgs& a)
+{
+    const long pairs = (long)a.H_kv * a.num_seqs * a.groups;
+    return a.whole ? (int)((pairs + 7) / 8 * 8) : a.workers;
+}
+
+}  // namespace
+
+void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t s)
+{
+    const dim3 grid((unsigned)paged_grid(a));
+    if (head_dim == 128) launch_f32_types<128>(a, dtype, cache_dtype, grid, s);
+    else launch_f32_types<64>(a, dtype, cache_dtype, grid, s);
+}
+
+void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t s)
+{
+    const int rows = (int)std::min<long>(a.rows, (long)a.max_chunk * a.G);
+    const dim3 grid((unsigned)(a.by_pair ? a.H_kv * a.num_seqs * a.groups : a.workers),
+                    (unsigned)((rows + kPagedFinishRows - 1) / kPagedFinishRows)),
+        block(64 * kPagedFinishRows);
+    if (head_dim == 128) {
+        if (dtype == PDEC_DTYPE_F32) hipLaunchKernelGGL((paged_finish_kernel<128, float>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((paged_finish_kernel<128, uint16_t>), grid, block, 0, s, a);
+    } else {
+        if (dtype == PDEC_DTYPE_F32) hipLaunchKernelGGL((paged_finish_kernel<64, float>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((paged_finish_kernel<64, uint16_t>), grid, block, 0, s, a);
+    }
+}
+
+}  // namespace pdec
+
+namespace {
+
+using namespace pdec;
+
+bool aligned(const void* p, uintptr_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int check_dims(const pdec_paged_dims* d)
+{
+    if (!d) return PDEC_ERR_INVALID_ARG;
+    if (d->num_seqs < 1 || d->num_tokens < 1 || d->num_q_heads < 1 || d->num_kv_heads < 1 ||
+        d->num_q_heads % d->num_kv_heads != 0 || d->num_pages < 1 || d->max_pages < 1 || d->max_chunk < 0 ||
+        d->max_len < 0 || d->causal < 0 || d->causal > 1 || d->page_size < 1)
+        return PDEC_ERR_INVALID_ARG;
+    if (std::isnan(d->softmax_scale) || std::isinf(d->softmax_scale)) return PDEC_ERR_INVALID_ARG;
+    if (d->dtype != PDEC_DTYPE_F32 && d->dtype != PDEC_DTYPE_BF16) return PDEC_ERR_UNSUPPORTED;
+    if (d->cache_dtype != d->dtype && d->cache_dtype != PDEC_DTYPE_E4M3) return PDEC_ERR_UNSUPPORTED;
+    if (d->head_dim != 64 && d->head_dim != 128) return PDEC_ERR_UNSUPPORTED;
+    if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
+        return PDEC_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)d->max_pages * d->page_size;
+    if (most > ((int64_t)1 << 30)) return PDEC_ERR_UNSUPPORTED;
+    if (d->max_len > most) return PDEC_ERR_INVALID_ARG;
+    // a token's keys, and a page, within 32-bit offsets (a pool may be larger)
+    if ((int64_t)d->num_kv_heads * d->head_dim * d->page_size * 4 > INT32_MAX) return PDEC_ERR_UNSUPPORTED;
+    return PDEC_OK;
+}
+
+int chunk_bound(const pdec_paged_dims* d) { return d->max_chunk > 0 ? std::min(d->max_chunk, d->num_tokens) : d->num_tokens; }
+int len_bound(const pdec_paged_dims* d) { return d->max_len > 0 ? d->max_len : d->max_pages * d->page_size; }
+int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
+
+struct AttnPlan {
+    PagedArgs few{}, many{};
+    bool use_few = false, use_many = false;
+    size_t few_bytes = 0, many_bytes = 0;
+};
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// The division of one launch's work over `workers` work-groups (paged_common.h),
+// and its workspace bytes; false if its unit count passes 32 bits.
+bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, size_t* bytes)
+{
+    const int64_t R = (int64_t)a.max_chunk * a.G;
+    if (R > INT32_MAX / 2) return false;
+    a.groups = (int)((R + a.rows - 1) / a.rows);
+    const int64_t units = (a.max_len + kUnit - 1) / kUnit;
+    const int64_t real_groups = (int64_t)d->num_tokens * a.G / a.rows + d->num_seqs;  // at most, over the batch
+    const int64_t pairs = (int64_t)d->num_seqs * a.groups * a.H_kv;
+    if (pairs > INT32_MAX / 2 || real_groups * a.H_kv * std::max<int64_t>(units, 1) > INT32_MAX / 2) return false;
+    a.workers = workers;
+    a.least = least;
+    // where no pair has more than a work-group's least there is nothing to cut
+    a.whole = units <= least ? 1 : 0;
+    a.by_pair = pairs <= workers ? 1 : 0;
+    *bytes = 0;
+    if (!a.whole)
+        *bytes = align256((size_t)workers * sizeof(int4)) + align256((size_t)2 * workers * a.rows * 2 * sizeof(float)) +
+                 (size_t)2 * workers * a.rows * d->head_dim * sizeof(float);
+    return true;
+}
+
+void place(PagedArgs& a, char* ws)
+{
+    if (a.whole) return;
+    a.cut = reinterpret_cast<int4*>(ws);
+    ws += align256((size_t)a.workers * sizeof(int4));
+    a.part_ml = reinterpret_cast<float*>(ws);
+    ws += align256((size_t)2 * a.workers * a.rows * 2 * sizeof(float));
+    a.part_o = reinterpret_cast<float*>(ws);
+}
+
+int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
+{
+    const int rc = check_dims(d);
+    if (rc != PDEC_OK) return rc;
+    PagedArgs a{};
+    a.num_seqs = d->num_seqs;
+    a.num_tokens = d->num_tokens;
+    a.H_q = d->num_q_heads;
+    a.H_kv = d->num_kv_heads;
+    a.G = d->num_q_heads / d->num_kv_heads;
+    a.page_shift = shift_of(d->page_size);
+    a.num_pages = d->num_pages;
+    a.max_pages = d->max_pages;
+    a.max_chunk = chunk_bound(d);
+    a.max_len = len_bound(d);
+    a.causal = d->causal;
+    const float scale = d->softmax_scale > 0.f ? d->softmax_scale : 1.f / std::sqrt((float)d->head_dim);
+    a.qscale = scale * 1.44269504088896340736f;
+    const int64_t R = (int64_t)a.max_chunk * a.G;
+    a.rows_from = 0;
+    a.rows_to = INT32_MAX;
+    p.few = a;
+    p.use_few = true;
+    p.few.rows = R <= 16 ? 16 : 32;
+    if (!divide(d, p.few, 512, 2, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+    return PDEC_OK;
+}
+
+// What the three cache calls share of their pointers' checks.
+bool cache_pointers(const pdec_paged_dims* d, const void* k, const void* v, const uint8_t* ks, const uint8_t* vs)
+{
+    if (!aligned(k, 16) || !aligned(v, 16)) return false;
+    return d->cache_dtype != PDEC_DTYPE_E4M3 || (aligned(ks, 4) && aligned(vs, 4));
+}
+
+// PDEC_DEBUG=1: the lengths of a call, copied and checked (synchronises).
+int debug_check(const pdec_paged_dims* d, const int32_t* cu, const int32_t* lens, int attn, void* stream)
+{
+    std::vector<int32_t> c((size_t)d->num_seqs + 1), l((size_t)d->num_seqs);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (hipMemcpyAsync(c.data(), cu, c.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+        hipMemcpyAsync(l.data(), lens, l.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+        hipStreamSynchronize(s) != hipSuccess)
+        return PDEC_ERR_HIP;
+    return pdec_check_paged_lengths(d, c.data(), l.data(), attn);
+}
+
+PagedIoArgs io_args(const pdec_paged_dims* d)
+{
+    PagedIoArgs a{};
+    a.num_seqs = d->num_seqs;
+    a.num_tokens = d->num_tokens;
+    a.H_kv = d->num_kv_heads;
+    a.page_shift = shift_of(d->page_size);
+    a.num_pages = d->num_pages;
+    a.max_pages = d->max_pages;
+    a.max_len = len_bound(d);
+    return a;
+}
+
+template <int D, typename T, bool QUANT>
+void launch_append(const PagedIoArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)std::max(a.num_tokens, (a.num_seqs + 63) / 64), 2);
+    hipLaunchKernelGGL((paged_append_kernel<D, T, QUANT>), grid, dim3(64), 0, s, a);
+}
+
+template <int D, typename T, bool QUANT>
+void launch_read(const PagedIoArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.num_tokens + 4 * kReadRows - 1) / (4 * kReadRows)), 2);
+    hipLaunchKernelGGL((paged_read_kernel<D, T, QUANT>), grid, dim3(256), 0, s, a);
+}
+
+// f.template operator()<D, T, QUANT>() for the dims' types
+template <typename F>
+void for_types(const pdec_paged_dims* d, F f)
+{
+    const bool q = d->cache_dtype == PDEC_DTYPE_E4M3, f32 = d->dtype == PDEC_DTYPE_F32;
+    auto types = [&](auto dim) {
+        if (f32) q ? f(dim, float{}, std::true_type{}) : f(dim, float{}, std::false_type{});
+        else q ? f(dim, uint16_t{}, std::true_type{}) : f(dim, uint16_t{}, std::false_type{});
+    };
+    if (d->head_dim == 128) types(std::integral_constant<int, 128>{});
+    else types(std::integral_constant<int, 64>{});
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? PDEC_OK : PDEC_ERR_HIP; }
+
+}  // namespace
+
+extern "C" {
+
+int pdec_check_paged_lengths(const pdec_paged_dims* d, const int32_t* cu, const int32_t* seq_lens, int32_t attn)
+{
+    const int rc = check_dims(d);
+    if (rc != PDEC_OK) return rc;
+    if (!cu || !seq_lens) return PDEC_ERR_INVALID_ARG;
+    if (cu[0] != 0 || cu[d->num_seqs] > d->num_tokens) return PDEC_ERR_BAD_LENGTHS;
+    for (int s = 0; s < d->num_seqs; ++s) {
+        if (cu[s + 1] < cu[s] || seq_lens[s] < 0 || seq_lens[s] > len_bound(d)) return PDEC_ERR_BAD_LENGTHS;
+        if (attn && cu[s + 1] - cu[s] > chunk_bound(d)) return PDEC_ERR_BAD_LENGTHS;
+    }
+    return PDEC_OK;
+}
+
+int pdec_paged_kv_append(const pdec_paged_dims* d, const void* k_new, const void* v_new, const int32_t* cu_tokens,
+                         const int32_t* block_table, const int32_t* lens_in, int32_t* lens_out, void* k_pages,
+                         void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream)
+{
+    int rc = check_dims(d);
+    if (rc != PDEC_OK) return rc;
+    if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(cu_tokens, 4) || !aligned(block_table, 4) ||
+        !aligned(lens_in, 4) || !aligned(lens_out, 4) || lens_in == lens_out ||
+        !cache_pointers(d, k_pages, v_pages, k_scales, v_scales))
+        return PDEC_ERR_INVALID_ARG;
+    if (debug_mode() && (rc = debug_check(d, cu_tokens, lens_in, 0, stream)) != PDEC_OK) return rc;
+    PagedIoArgs a = io_args(d);
+    a.k_rows = k_new;
+    a.v_rows = v_new;
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.block_table = block_table;
+    a.cu = cu_tokens;
+    a.lens = lens_in;
+    a.lens_out = lens_out;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    for_types(d, [&](auto dim, auto t, auto q) { launch_append<dim(), decltype(t), q()>(a, s); });
+    return launched();
+}
+
+int pdec_paged_kv_read(const pdec_paged_dims* d, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                       const uint8_t* v_scales, const int32_t* block_table, const int32_t* seq_lens,
+                       const int32_t* cu_rows, void* k_out, void* v_out, void* stream)
+{
+    int rc = check_dims(d);
+    if (rc != PDEC_OK) return rc;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(cu_rows, 4) || !aligned(block_table, 4) ||
+        !aligned(seq_lens, 4) || !cache_pointers(d, k_pages, v_pages, k_scales, v_scales))
+        return PDEC_ERR_INVALID_ARG;
+    if (debug_mode() && (rc = debug_check(d, cu_rows, seq_lens, 0, stream)) != PDEC_OK) return rc;
+    PagedIoArgs a = io_args(d);
+    a.k_rows = k_out;
+    a.v_rows = v_out;
+    a.k_pages = const_cast<void*>(k_pages);
+    a.v_pages = const_cast<void*>(v_pages);
+    a.k_scales = const_cast<uint8_t*>(k_scales);
+    a.v_scales = const_cast<uint8_t*>(v_scales);
+    a.block_table = block_table;
+    a.cu = cu_rows;
+    a.lens = seq_lens;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    for_types(d, [&](auto dim, auto t, auto q) { launch_read<dim(), decltype(t), q()>(a, s); });
+    return launched();
+}
+
+size_t pdec_paged_workspace_size(const pdec_paged_dims* d)
+{
+    AttnPlan p;
+    return plan_attn(d, p) == PDEC_OK ? std::max<size_t>(align256(p.few_bytes) + p.many_bytes, 16) : 0;
+}
+
+int pdec_query_paged_plan(const pdec_paged_dims* d, pdec_paged_plan* plan)
+{
+    if (!plan) return PDEC_ERR_INVALID_ARG;
+    AttnPlan p;
+    const int rc = plan_attn(d, p);
+    if (rc != PDEC_OK) return rc;
+    plan->rows_few = p.use_few ? p.few.rows : 0;
+    plan->rows_many = p.use_many ? p.many.rows : 0;
+    plan->workers = p.use_few ? p.few.workers : p.many.workers;
+    plan->merge_pass = (p.use_few && !p.few.whole) || (p.use_many && !p.many.whole) ? 1 : 0;
+    return PDEC_OK;
+}
+
+int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages, const void* v_pages,
+                    const uint8_t* k_scales, const uint8_t* v_scales, const int32_t* block_table,
+                    const int32_t* cu_tokens, const int32_t* seq_lens, void* out, float* lse, void* workspace,
+                    size_t workspace_bytes, void* stream)
+{
+    AttnPlan p;
+    int rc = plan_attn(d, p);
+    if (rc != PDEC_OK) return rc;
+    if (!aligned(q, 16) || !aligned(out, 16) || (lse && !aligned(lse, 4)) || !aligned(block_table, 4) ||
+        !aligned(cu_tokens, 4) || !aligned(seq_lens, 4) || !aligned(workspace, 16) ||
+        !cache_pointers(d, k_pages, v_pages, k_scales, v_scales))
+        return PDEC_ERR_INVALID_ARG;
+    if (workspace_bytes < align256(p.few_bytes) + p.many_bytes) return PDEC_ERR_WORKSPACE;
+    if (debug_mode() && (rc = debug_check(d, cu_tokens, seq_lens, 1, stream)) != PDEC_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    for (PagedArgs* a : {&p.few, &p.many}) {
+        a->q = q;
+        a->k_pages = k_pages;
+        a->v_pages = v_pages;
+        a->k_scales = k_scales;
+        a->v_scales = v_scales;
+        a->block_table = block_table;
+        a->cu_tokens = cu_tokens;
+        a->seq_lens = seq_lens;
+        a->out = out;
+        a->lse = lse;
+    }
+    if (p.use_few) {
+        place(p.few, static_cast<char*>(workspace));
+        launch_paged_f32(p.few, d->head_dim, d->dtype, d->cache_dtype, s);
+        if (launched() != PDEC_OK) return PDEC_ERR_HIP;
+        if (!p.few.whole) {
+            launch_paged_finish(p.few, d->head_dim, d->dtype, s);
+            if (launched() != PDEC_OK) return PDEC_ERR_HIP;
+        }
+    }
+    return PDEC_OK;
+}
+
+int pdec_merge_states(int64_t num_rows, int32_t head_dim, int32_t dtype, const void* out_a, const float* lse_a,
+                      const void* out_b, const float* lse_b, void* out, float* lse, void* stream)
+{
+    if (num_rows < 1 || !aligned(out_a, 16) || !aligned(out_b, 16) || !aligned(out, 16) || !aligned(lse_a, 4) ||
+        !aligned(lse_b, 4) || (lse && !aligned(lse, 4)))
+        return PDEC_ERR_INVALID_ARG;
+    if (dtype != PDEC_DTYPE_F32 && dtype != PDEC_DTYPE_BF16) return PDEC_ERR_UNSUPPORTED;
+    if (head_dim != 64 && head_dim != 128) return PDEC_ERR_UNSUPPORTED;
+    const int64_t blocks = (num_rows * (head_dim / 8) + 255) / 256;
+    if (num_rows > ((int64_t)1 << 40) || blocks > INT32_MAX) return PDEC_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)blocks), block(256);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool f32 = dtype == PDEC_DTYPE_F32;
+    if (head_dim == 128) {
+        if (f32) hipLaunchKernelGGL((merge_states_kernel<128, float>), grid, block, 0, s, (long)num_rows, out_a, lse_a, out_b, lse_b, out, lse);
+        else hipLaunchKernelGGL((merge_states_kernel<128, uint16_t>), grid, block, 0, s, (long)num_rows, out_a, lse_a, out_b, lse_b, out, lse);
+    } else {
+        if (f32) hipLaunchKernelGGL((merge_states_kernel<64, float>), grid, block, 0, s, (long)num_rows, out_a, lse_a, out_b, lse_b, out, lse);
+        else hipLaunchKernelGGL((merge_states_kernel<64, uint16_t>), grid, block, 0, s, (long)num_rows, out_a, lse_a, out_b, lse_b, out, lse);
+    }
+    return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,220 @@
+// Attention over paged caches: arguments, the division of the work, and what
+// its kernels share.
+//
+// A sequence's new tokens have R = n G query rows per kv head (r = token * G +
+// head of the group), all against the same keys.  They are cut into groups of
+// `rows` rows; a (kv head, sequence, row group) is a pair of rows and keys that
+// one work-group can take, in 64-key units up to the last key that the group's
+// last row sees.  The units of all pairs, one after another (by head, then
+// sequence, then row group), are dealt in equal runs to `workers` work-groups.
+// Lengths are known on the device only, and differ: a sequence of 100 keys and
+// one of 30000 in one batch, or the row groups of a causal chunk, still give
+// every work-group the same number of units.  A run is a few whole pairs and
+// at most one cut pair at each end; a work-group writes whole pairs to the
+// output and a cut pair's state (reference max, normaliser, unnormalised
+// output, all float32) to one of its two slots, and a finish pass joins a cut
+// pair's slots in the order of the work-groups.  So the workspace depends on
+// the number of work-groups only, and repeated calls agree bit for bit.
+#pragma once
+
+#include "pdec_common.h"
+
+namespace pdec {
+
+constexpr int kPagedFinishRows = 4;  // rows per work-group of the finish pass
+
+// One launch's arguments.
+struct PagedArgs {
+    const void* q;
+    const void* k_pages;
+    const void* v_pages;
+    const uint8_t* k_scales;
+    const uint8_t* v_scales;
+    const int32_t* block_table;
+    const int32_t* cu_tokens;
+    const int32_t* seq_lens;
+    void* out;
+    float* lse;       // may be null
+    float* part_o;    // [2 workers, rows, D]
+    float* part_ml;   // [2 workers, rows, 2]
+    int4* cut;        // a cut pair's (first work-group, last, pair of its head, head); first = -1: not cut
+    int num_seqs, num_tokens, H_q, H_kv, G;
+    int page_shift, num_pages, max_pages, max_chunk, max_len, causal;
+    float qscale;     // softmax scale * log2(e)
+    int rows;         // query rows per item
+    int groups;       // row groups per (kv head, sequence), at most
+    int rows_from;    // this launch serves the sequences with rows_from <= R <= rows_to
+    int rows_to;
+    int workers;      // work-groups that share the units, a multiple of 8
+    int least;        // units per work-group, at least
+    int whole;        // 1: work-group i takes pair i whole, nothing is cut
+    int by_pair;      // 1: cut[] is indexed by pair, 0: by the work-group a pair begins in
+};
+
+struct PagedSeq {
+    int t0, n, L;  // first new token, their number, keys
+};
+
+__device__ inline PagedSeq paged_seq(const PagedArgs& a, int s)
+{
+    PagedSeq x;
+    x.t0 = min(max(a.cu_tokens[s], 0), a.num_tokens);
+    const int t1 = min(max(a.cu_tokens[s + 1], 0), a.num_tokens);
+    x.n = min(max(t1 - x.t0, 0), a.max_chunk);
+    x.L = min(max(a.seq_lens[s], 0), a.max_len);
+    return x;
+}
+
+// Keys that new token i sees: the first so many.
+__device__ inline int paged_seen(const PagedArgs& a, const PagedSeq& x, int i)
+{
+    return a.causal ? min(max(x.L - x.n + i + 1, 0), x.L) : x.L;
+}
+
+// Units of pair j = sequence * groups + row group (the same for every head);
+// 0 where there are no such rows, at least 1 where there are.
+__device__ inline int paged_units(const PagedArgs& a, int j)
+{
+    const int s = j / a.groups, row0 = (j - s * a.groups) * a.rows;
+    const PagedSeq x = paged_seq(a, s);
+    const int R = x.n * a.G;
+    if (row0 >= R || R < a.rows_from || R > a.rows_to) return 0;
+    const int last = min(R, row0 + a.rows) - 1;
+    return max(1, (paged_seen(a, x, last / a.G) + kUnit - 1) / kUnit);
+}
+
+// A work-group's place in its run of units.  Uniform over the work-group.
+struct PagedRun {
+    int w;          // its number
+    int head, j;    // the pair at hand
+    int u, units;   // next unit of it, and its units
+    int left;       // units left of the run
+    int pos, per;   // position of the next unit in the list of all, units per work-group
+};
+
+// What to do next: units [u0, u1) of a pair.
+struct PagedPart {
+    int head, s, group, u0, u1;
+    bool whole;     // all of the pair
+    int slot;       // where its state goes if not
+};
+
+__device__ inline int paged_lane() { return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
+
+// False if the work-group has nothing to do.  Every wave computes the same.
+__device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r)
+{
+    const int J = a.num_seqs * a.groups, lane = paged_lane();
+    r.w = w;
+    if (a.whole) {
+        if (w >= J * a.H_kv) return false;
+        r.head = w / J;
+        r.j = w - r.head * J;
+        r.u = r.pos = 0;
+        r.units = r.left = r.per = __builtin_amdgcn_readfirstlane(paged_units(a, r.j));
+        return r.units > 0;
+    }
+    auto scan = [&](int x) {  // inclusive, over the lanes
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int y = __shfl_up(x, off);
+            if (lane >= off) x += y;
+        }
+        return x;
+    };
+    int total = 0, n0 = 0, incl0 = 0;
+    for (int j0 = 0; j0 < J; j0 += 64) {
+        const int n = j0 + lane < J ? paged_units(a, j0 + lane) : 0, incl = scan(n);
+        if (j0 == 0) n0 = n, incl0 = incl;
+        total += __shfl(incl, 63);
+    }
+    total = __builtin_amdgcn_readfirstlane(total);
+    r.per = max((total * a.H_kv + a.workers - 1) / a.workers, a.least);
+    r.pos = w * r.per;
+    if (total == 0 || r.pos >= total * a.H_kv) return false;
+    r.left = min(r.per, total * a.H_kv - r.pos);
+    r.head = r.pos / total;
+    int rest = r.pos - r.head * total;
+    for (int j0 = 0;; j0 += 64) {
+        int n = n0, incl = incl0;
+        if (j0 > 0) {
+            n = j0 + lane < J ? paged_units(a, j0 + lane) : 0;
+            incl = scan(n);
+        }
+        const int all = __shfl(incl, 63);
+        if (rest >= all) {
+            rest -= all;
+            continue;
+        }
+        const int at = __builtin_ctzll(__ballot(incl > rest));
+        r.j = __builtin_amdgcn_readfirstlane(j0 + at);
+        r.units = __builtin_amdgcn_readfirstlane(__shfl(n, at));
+        r.u = __builtin_amdgcn_readfirstlane(rest - __shfl(incl - n, at));
+        break;
+    }
+    return true;
+}
+
+// The next part of the run; false at its end.  One lane of the work-group (the
+// caller says which) notes for the finish pass what is cut.
+__device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p, bool note)
+{
+    if (r.left <= 0) return false;
+    const int J = a.num_seqs * a.groups;
+    while (r.u >= r.units) {  // units are left, so another pair follows
+        const int s = r.j / a.groups;
+        const PagedSeq x = paged_seq(a, s);
+        const int R = x.n * a.G, g = r.j - s * a.groups + 1;
+        // the sequence's next group, or the next sequence's first
+        r.j = g < a.groups && g * a.rows < R && R >= a.rows_from && R <= a.rows_to ? r.j + 1 : (s + 1) * a.groups;
+        if (r.j >= J) {
+            r.j = 0;
+            ++r.head;
+        }
+        r.u = 0;
+        r.units = __builtin_amdgcn_readfirstlane(paged_units(a, r.j));
+    }
+    p.head = r.head;
+    p.s = r.j / a.groups;
+    p.group = r.j - p.s * a.groups;
+    p.u0 = r.u;
+    p.u1 = min(r.units, r.u + r.left);
+    p.whole = p.u0 == 0 && p.u1 == r.units;
+    p.slot = 2 * r.w + (p.u0 == 0 ? 1 : 0);
+    if (note && !a.whole) {
+        if (p.u0 == 0 && a.by_pair)
+            a.cut[r.head * J + r.j] = make_int4(p.whole ? -1 : r.w, (r.pos + r.units - 1) / r.per, r.j, r.head);
+        if (!a.by_pair && r.left == p.u1 - p.u0)  // the run's last part
+            a.cut[r.w] = make_int4(p.u0 == 0 && !p.whole ? r.w : -1, (r.pos - r.u + r.units - 1) / r.per, r.j, r.head);
+    }
+    r.pos += p.u1 - p.u0;
+    r.left -= p.u1 - p.u0;
+    r.u = p.u1;
+    return true;
+}
+
+// Number of a work-group: block b runs on XCD b % 8, and neighbours in the
+// list, which read the same keys, share an XCD's cache.
+__device__ inline int paged_worker(const PagedArgs& a, int block, int blocks)
+{
+    return (block % 8) * (blocks / 8) + block / 8;
+}
+
+// Row of q / out / lse of row r of a pair.
+__device__ inline long paged_qrow(const PagedArgs& a, const PagedSeq& x, int head, int r)
+{
+    const int i = r / a.G;
+    return (long)(x.t0 + i) * a.H_q + head * a.G + (r - i * a.G);
+}
+
+// Page of unit-aligned key t of a sequence, -1 if absent.
+__device__ inline int paged_page(const PagedArgs& a, int s, int t)
+{
+    const int p = a.block_table[(long)s * a.max_pages + min(t >> a.page_shift, a.max_pages - 1)];
+    return (uint32_t)p < (uint32_t)a.num_pages ? p : -1;
+}
+
+void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t stream);
+void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t stream);
+
+}  // namespace pdec

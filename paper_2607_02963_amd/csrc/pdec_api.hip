@@ -28,6 +28,20 @@
 #include "kernel_rope.h"
 #include "kernel_valu.h"
 
+namespace pdec {
+
+// Debug mode (PDEC_DEBUG=1): device lengths are checked before each step.
+bool debug_mode()
+{
+    static const bool on = [] {
+        const char* v = std::getenv("PDEC_DEBUG");
+        return v && v[0] == '1' && v[1] == '\0';
+    }();
+    return on;
+}
+
+}  // namespace pdec
+
 namespace {
 
 using namespace pdec;
@@ -83,16 +97,6 @@ void timer_slot_events(hipEvent_t* start, hipEvent_t* stop)
     const int slot = (int)(g_timer_calls++ % g_timer_n);
     *start = static_cast<hipEvent_t>(g_timer_start[slot]);
     *stop = static_cast<hipEvent_t>(g_timer_stop[slot]);
-}
-
-// Debug mode (PDEC_DEBUG=1): device lengths are checked before each step.
-bool debug_mode()
-{
-    static const bool on = [] {
-        const char* v = std::getenv("PDEC_DEBUG");
-        return v && v[0] == '1' && v[1] == '\0';
-    }();
-    return on;
 }
 
 struct Plan {

@@ -91,6 +91,9 @@ struct StepArgs {
     int slot0;
 };
 
+// Whether PDEC_DEBUG=1: device lengths are checked before each call.
+bool debug_mode();
+
 // Launches of the matrix-core split passes (their own translation unit): the
 // decode step's, and whole branches'.
 void launch_split_mfma(const StepArgs& a, int shape, int grid, hipStream_t stream);

@@ -8,6 +8,7 @@ built library is missing, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -25,6 +26,7 @@ PDEC_ERR_SCRATCH = -6
 NOALLOC_SCRATCH_BYTES = 32 << 20
 PDEC_DTYPE_F32 = 0
 PDEC_DTYPE_BF16 = 1
+PDEC_DTYPE_E4M3 = 2
 
 PATH_AUTO, PATH_VALU, PATH_MFMA, PATH_MFMA32 = 0, 1, 2, 3
 
@@ -33,7 +35,8 @@ EXPORTED = ("pdec_strerror", "pdec_workspace_size", "pdec_attn_step", "pdec_attn
             "pdec_set_split_timer", "pdec_describe_plan", "pdec_grounding_workspace_size", "pdec_segment_grounding",
             "pdec_aggregation_workspace_size", "pdec_aggregate", "pdec_backward_workspace_size", "pdec_query_backward_plan",
             "pdec_attn_prefill_backward", "pdec_read_probe", "pdec_issue_probe", "pdec_check_lengths",
-            "pdec_decode_step")
+            "pdec_decode_step", "pdec_paged_kv_append", "pdec_paged_kv_read", "pdec_paged_workspace_size",
+            "pdec_query_paged_plan", "pdec_paged_attn", "pdec_check_paged_lengths", "pdec_merge_states")
 
 AGGR_MODES = {"uniform": 0, "learned": 1, "attention": 2}
 
@@ -72,6 +75,23 @@ class AggrDims(ctypes.Structure):
                 ("num_segments", ctypes.c_int32), ("hidden", ctypes.c_int32), ("mode", ctypes.c_int32),
                 ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class PagedDims(ctypes.Structure):
+    """Mirror of ``pdec_paged_dims``."""
+
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_tokens", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_chunk", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("dtype", ctypes.c_int32), ("cache_dtype", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class PagedPlan(ctypes.Structure):
+    """Mirror of ``pdec_paged_plan``."""
+
+    _fields_ = [("rows_few", ctypes.c_int32), ("rows_many", ctypes.c_int32), ("workers", ctypes.c_int32),
+                ("merge_pass", ctypes.c_int32)]
 
 
 class PdecError(RuntimeError):
@@ -130,6 +150,21 @@ def lib():
         L.pdec_query_backward_plan.argtypes = [dp] + [ctypes.POINTER(i32)] * 3
         L.pdec_attn_prefill_backward.restype = ctypes.c_int
         L.pdec_attn_prefill_backward.argtypes = [dp] + [vp] * 16 + [sz, vp]
+        pp = ctypes.POINTER(PagedDims)
+        L.pdec_paged_kv_append.restype = ctypes.c_int
+        L.pdec_paged_kv_append.argtypes = [pp] + [vp] * 11
+        L.pdec_paged_kv_read.restype = ctypes.c_int
+        L.pdec_paged_kv_read.argtypes = [pp] + [vp] * 10
+        L.pdec_paged_workspace_size.restype = sz
+        L.pdec_paged_workspace_size.argtypes = [pp]
+        L.pdec_query_paged_plan.restype = ctypes.c_int
+        L.pdec_query_paged_plan.argtypes = [pp, ctypes.POINTER(PagedPlan)]
+        L.pdec_paged_attn.restype = ctypes.c_int
+        L.pdec_paged_attn.argtypes = [pp] + [vp] * 11 + [sz, vp]
+        L.pdec_check_paged_lengths.restype = ctypes.c_int
+        L.pdec_check_paged_lengths.argtypes = [pp, vp, vp, i32]
+        L.pdec_merge_states.restype = ctypes.c_int
+        L.pdec_merge_states.argtypes = [ctypes.c_int64, i32, i32] + [vp] * 7
         L.pdec_set_path.restype = ctypes.c_int
         L.pdec_set_path.argtypes = [ctypes.c_int]
         L.pdec_query_plan.restype = ctypes.c_int
@@ -618,6 +653,202 @@ def aggregate(g, x, cu_seg, salient, mode, *, scores=None, q=None, k=None, lse=N
             workspace.nbytes, _stream(stream, g.device)]
     _check("pdec_aggregate", lib().pdec_aggregate(ctypes.byref(dims), *args))
     return out
+
+
+# ---- paged caches ----
+
+def make_paged_dims(num_seqs, num_tokens, H_q, H_kv, D, page_size, num_pages, max_pages, dtype_code, cache_code, *,
+                    max_chunk=0, max_len=0, causal=1, scale=0.0) -> PagedDims:
+    return PagedDims(int(num_seqs), int(num_tokens), int(H_q), int(H_kv), int(D), int(page_size), int(num_pages),
+                     int(max_pages), int(max_chunk), int(max_len), int(dtype_code), int(cache_code), int(causal),
+                     float(scale))
+
+
+def _cache_code(pages: torch.Tensor) -> int:
+    return PDEC_DTYPE_E4M3 if pages.dtype == torch.float8_e4m3fn else _dtype_code(pages)
+
+
+def _paged_dims(rows, H_q, pages, block_table, **kw) -> PagedDims:
+    P, page, H_kv, D = pages.shape
+    return make_paged_dims(block_table.shape[0], rows.shape[0], H_q, H_kv, D, page, P, block_table.shape[1],
+                           _dtype_code(rows), _cache_code(pages), **kw)
+
+
+def paged_dims_of(q, k_pages, block_table, *, causal=True, max_chunk=None, max_len=None, scale=0.0) -> PagedDims:
+    """The dims of a ``paged_attn`` call on these tensors, for ``paged_workspace_size`` and ``query_paged_plan``."""
+    return _paged_dims(q, q.shape[1], k_pages, block_table, max_chunk=max_chunk or 0, max_len=max_len or 0,
+                       causal=bool(causal), scale=scale)
+
+
+def paged_workspace_size(dims: PagedDims) -> int:
+    return int(lib().pdec_paged_workspace_size(ctypes.byref(dims)))
+
+
+def query_paged_plan(dims: PagedDims) -> dict:
+    """The kernels of a ``paged_attn`` call (``pdec_query_paged_plan``) as a dict."""
+    plan = PagedPlan()
+    _check("pdec_query_paged_plan", lib().pdec_query_paged_plan(ctypes.byref(dims), ctypes.byref(plan)))
+    return {name: getattr(plan, name) for name, _ in PagedPlan._fields_}
+
+
+def _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype):
+    """Pointers (k, v, k scales, v scales) of a paged cache, checked."""
+    quant = k_pages.dtype == torch.float8_e4m3fn
+    args = [_dev(k_pages, "k_pages", None if quant else dtype, 4), _dev(v_pages, "v_pages", k_pages.dtype, 4)]
+    if v_pages.shape != k_pages.shape:
+        raise ValueError("k_pages and v_pages must have one shape")
+    if not quant:
+        if k_scales is not None or v_scales is not None:
+            raise ValueError("only an e4m3 cache has scales")
+        return args + [None, None]
+    P, page, H_kv, _ = k_pages.shape
+    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+        args.append(_dev(t, name, torch.uint8, 3))
+        if t.shape != (P, H_kv, page):
+            raise ValueError(f"{name} must be [num_pages, H_kv, page_size]")
+    return args
+
+
+def _one_device(first, *others):
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors on different devices")
+    if first.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {first.device}, but the current device is {torch.cuda.current_device()}")
+
+
+def _on_stream(stream):
+    """Where a call allocates what it was not given: on the stream that will use it, so that the memory is not
+    handed out again on another stream while the call runs."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def paged_kv_append(k_new, v_new, k_pages, v_pages, block_table, cu_tokens, lens_in, lens_out, *, k_scales=None,
+                    v_scales=None, max_len=None, stream=None):
+    """Append the new tokens' keys and values to their sequences' pages (``pdec_paged_kv_append``).
+
+    k_new/v_new [T,H_kv,D] float32 or bf16; k_pages/v_pages [P,page,H_kv,D] of the same dtype, or
+    ``torch.float8_e4m3fn`` with k_scales/v_scales uint8 [P,H_kv,page]; block_table int32 [S,max_pages];
+    cu_tokens int32 [S+1]; lens_in int32 [S] (keys before), lens_out int32 [S] (another tensor: keys after).
+    """
+    T, H_kv, D = k_new.shape
+    S = block_table.shape[0]
+    if v_new.shape != k_new.shape or k_pages.shape[2:] != (H_kv, D):
+        raise ValueError("inconsistent append shapes")
+    if cu_tokens.shape[0] != S + 1 or lens_in.shape[0] != S or lens_out.shape[0] != S:
+        raise ValueError("cu_tokens / lens shape")
+    dims = _paged_dims(k_new, H_kv, k_pages, block_table, max_len=max_len or 0)
+    cache = _paged_cache(k_pages, v_pages, k_scales, v_scales, k_new.dtype)
+    args = [_dev(k_new, "k_new", None, 3), _dev(v_new, "v_new", k_new.dtype, 3),
+            _dev(cu_tokens, "cu_tokens", torch.int32, 1), _dev(block_table, "block_table", torch.int32, 2),
+            _dev(lens_in, "lens_in", torch.int32, 1), _dev(lens_out, "lens_out", torch.int32, 1), *cache]
+    _one_device(k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, cu_tokens, lens_in, lens_out)
+    _check("pdec_paged_kv_append", lib().pdec_paged_kv_append(ctypes.byref(dims), *args,
+                                                              _stream(stream, k_new.device)))
+
+
+def paged_kv_read(k_pages, v_pages, block_table, seq_lens, cu_rows, *, k_out=None, v_out=None, num_rows=None,
+                  dtype=None, k_scales=None, v_scales=None, max_len=None, stream=None):
+    """Pages as dense rows (``pdec_paged_kv_read``); returns (k_out, v_out) [R,H_kv,D].
+
+    Row cu_rows[s] + t receives key t of sequence s, 0 at or beyond seq_lens[s].  Give k_out and v_out, or
+    ``num_rows`` (and ``dtype``, by default bf16 for an e4m3 cache).  Other arguments as for ``paged_kv_append``.
+    """
+    S = block_table.shape[0]
+    H_kv, D = k_pages.shape[2:]
+    quant = k_pages.dtype == torch.float8_e4m3fn
+    if (k_out is None) != (v_out is None):
+        raise ValueError("give both k_out and v_out or neither")
+    if k_out is None:
+        if num_rows is None:
+            raise ValueError("num_rows is required without k_out and v_out")
+        if dtype is None:
+            dtype = torch.bfloat16 if quant else k_pages.dtype
+        with _on_stream(stream):
+            k_out, v_out = (torch.empty((num_rows, H_kv, D), dtype=dtype, device=k_pages.device) for _ in "kv")
+    if k_out.shape[1:] != (H_kv, D) or v_out.shape != k_out.shape:
+        raise ValueError("k_out / v_out shape")
+    if cu_rows.shape[0] != S + 1 or seq_lens.shape[0] != S:
+        raise ValueError("cu_rows / seq_lens shape")
+    dims = _paged_dims(k_out, H_kv, k_pages, block_table, max_len=max_len or 0)
+    cache = _paged_cache(k_pages, v_pages, k_scales, v_scales, k_out.dtype)
+    args = [*cache, _dev(block_table, "block_table", torch.int32, 2), _dev(seq_lens, "seq_lens", torch.int32, 1),
+            _dev(cu_rows, "cu_rows", torch.int32, 1), _dev(k_out, "k_out", None, 3),
+            _dev(v_out, "v_out", k_out.dtype, 3)]
+    _one_device(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, cu_rows, k_out, v_out)
+    _check("pdec_paged_kv_read", lib().pdec_paged_kv_read(ctypes.byref(dims), *args,
+                                                          _stream(stream, k_pages.device)))
+    return k_out, v_out
+
+
+def paged_attn(q, k_pages, v_pages, block_table, cu_tokens, seq_lens, *, causal=True, k_scales=None, v_scales=None,
+               max_chunk=None, max_len=None, out=None, lse=None, workspace=None, scale=0.0, stream=None,
+               want_lse=True):
+    """Attention of the new tokens over their sequences' pages (``pdec_paged_attn``); returns (out, lse).
+
+    q [T,H_q,D]; pages, scales, block_table and cu_tokens as for ``paged_kv_append``; seq_lens int32 [S] counts
+    the new tokens (append first, then attend).  ``causal``: token i of n sees keys 0 .. len - n + i; else all
+    len keys.  ``max_chunk`` and ``max_len`` bound the new tokens and the keys of a sequence (default: T, and
+    what block_table can hold); the tighter, the fewer work-groups without work.
+    """
+    T, H_q, D = q.shape
+    S = block_table.shape[0]
+    if k_pages.shape[3] != D or cu_tokens.shape[0] != S + 1 or seq_lens.shape[0] != S:
+        raise ValueError("inconsistent shapes")
+    dims = paged_dims_of(q, k_pages, block_table, causal=causal, max_chunk=max_chunk, max_len=max_len, scale=scale)
+    cache = _paged_cache(k_pages, v_pages, k_scales, v_scales, q.dtype)
+    if out is None or (lse is None and want_lse) or workspace is None:
+        with _on_stream(stream):
+            if out is None:
+                out = torch.empty_like(q)
+            if lse is None and want_lse:
+                lse = torch.empty((T, H_q), dtype=torch.float32, device=q.device)
+            if workspace is None:
+                workspace = torch.empty(max(paged_workspace_size(dims), 16), dtype=torch.uint8, device=q.device)
+    if out.shape != q.shape or (lse is not None and lse.shape != (T, H_q)):
+        raise ValueError("out / lse shape")
+    args = [_dev(q, "q", None, 3), *cache, _dev(block_table, "block_table", torch.int32, 2),
+            _dev(cu_tokens, "cu_tokens", torch.int32, 1), _dev(seq_lens, "seq_lens", torch.int32, 1),
+            _dev(out, "out", q.dtype, 3), _dev(lse, "lse", torch.float32, 2) if want_lse else None,
+            _dev(workspace, "workspace"), workspace.nbytes]
+    _one_device(q, k_pages, v_pages, k_scales, v_scales, block_table, cu_tokens, seq_lens, out, lse, workspace)
+    _check("pdec_paged_attn", lib().pdec_paged_attn(ctypes.byref(dims), *args, _stream(stream, q.device)))
+    return out, lse if want_lse else None
+
+
+def check_paged_lengths(dims: PagedDims, cu, seq_lens, attn=True) -> int:
+    """pdec_check_paged_lengths on host int32 arrays (numpy or lists); returns PDEC_OK or PDEC_ERR_BAD_LENGTHS."""
+    import numpy as np
+    arrs = [np.ascontiguousarray(np.asarray(x, dtype=np.int32)) for x in (cu, seq_lens)]
+    if arrs[0].shape != (dims.num_seqs + 1,) or arrs[1].shape != (dims.num_seqs,):
+        raise ValueError("cu / seq_lens shape")
+    rc = lib().pdec_check_paged_lengths(ctypes.byref(dims), arrs[0].ctypes.data, arrs[1].ctypes.data, int(bool(attn)))
+    if rc not in (PDEC_OK, PDEC_ERR_BAD_LENGTHS):
+        raise PdecError("pdec_check_paged_lengths", rc)
+    return rc
+
+
+def merge_states(out_a, lse_a, out_b, lse_b, *, out=None, lse=None, stream=None):
+    """Attention over two disjoint sets of keys joined into attention over both (``pdec_merge_states``);
+    returns (out, lse).
+
+    out_a/out_b [...,D] float32 or bf16, lse_a/lse_b float32 [...]; ``out`` and ``lse`` may be one of the sides'.
+    """
+    D = out_a.shape[-1]
+    if out_b.shape != out_a.shape or lse_a.shape != out_a.shape[:-1] or lse_b.shape != lse_a.shape:
+        raise ValueError("inconsistent shapes")
+    if out is None or lse is None:
+        with _on_stream(stream):
+            out = torch.empty_like(out_a) if out is None else out
+            lse = torch.empty_like(lse_a) if lse is None else lse
+    if out.shape != out_a.shape or lse.shape != lse_a.shape:
+        raise ValueError("out / lse shape")
+    args = [_dev(out_a, "out_a"), _dev(lse_a, "lse_a", torch.float32), _dev(out_b, "out_b", out_a.dtype),
+            _dev(lse_b, "lse_b", torch.float32), _dev(out, "out", out_a.dtype), _dev(lse, "lse", torch.float32)]
+    _one_device(out_a, lse_a, out_b, lse_b, out, lse)
+    _check("pdec_merge_states", lib().pdec_merge_states(lse_a.numel(), D, _dtype_code(out_a), *args,
+                                                        _stream(stream, out_a.device)))
+    return out, lse
 
 
 def check_lengths(dims: Dims, num_videos: int, event_lens, prefix_lens=None, cu_prefix=None, cu_events=None) -> int:
