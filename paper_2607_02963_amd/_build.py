@@ -23,7 +23,7 @@ HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # plain v_max/v_max3 without a quieting v_max(x, x) before each operand, a
 # tenth of their vector instructions.  The vector-ALU kernels compile to
 # slower code with the same flags, so they keep the defaults.
-SOURCE_FLAGS = {"split_mfma.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"]}
+SOURCE_FLAGS = {name: ["-fno-honor-nans", "-mno-amdgpu-ieee"] for name in ("split_mfma.hip", "paged_mfma.hip")}
 
 
 def sources():

@@ -36,13 +36,13 @@ void launch_f32_types(const PagedArgs& a, int dtype, int cache_dtype, dim3 grid,
     }
 }
 
-int paged_grid(const PagedArgs& a)
+}  // namespace
+
+static int paged_grid(const PagedArgs& a)
 {
     const long pairs = (long)a.H_kv * a.num_seqs * a.groups;
     return a.whole ? (int)((pairs + 7) / 8 * 8) : a.workers;
 }
-
-}  // namespace
 
 void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t s)
 {
@@ -99,6 +99,9 @@ int chunk_bound(const pdec_paged_dims* d) { return d->max_chunk > 0 ? std::min(d
 int len_bound(const pdec_paged_dims* d) { return d->max_len > 0 ? d->max_len : d->max_pages * d->page_size; }
 int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
+// Sequences of at most so many rows per kv head are the few-row kernel's.
+constexpr int kFewRows = 64;
+
 struct AttnPlan {
     PagedArgs few{}, many{};
     bool use_few = false, use_many = false;
@@ -113,7 +116,7 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, size
 {
     const int64_t R = (int64_t)a.max_chunk * a.G;
     if (R > INT32_MAX / 2) return false;
-    a.groups = (int)((R + a.rows - 1) / a.rows);
+    a.groups = (int)((std::min<int64_t>(R, a.rows_to) + a.rows - 1) / a.rows);
     const int64_t units = (a.max_len + kUnit - 1) / kUnit;
     const int64_t real_groups = (int64_t)d->num_tokens * a.G / a.rows + d->num_seqs;  // at most, over the batch
     const int64_t pairs = (int64_t)d->num_seqs * a.groups * a.H_kv;
@@ -161,10 +164,22 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     const int64_t R = (int64_t)a.max_chunk * a.G;
     a.rows_from = 0;
     a.rows_to = INT32_MAX;
-    p.few = a;
-    p.use_few = true;
-    p.few.rows = R <= 16 ? 16 : 32;
-    if (!divide(d, p.few, 512, 2, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+    p.few = p.many = a;
+    p.use_many = d->dtype == PDEC_DTYPE_BF16 && d->cache_dtype == PDEC_DTYPE_BF16 && R > kFewRows;
+    // one sequence is the many rows' whatever its chunk; of several, each goes by its own
+    p.use_few = !p.use_many || d->num_seqs > 1;
+    if (p.use_many) {
+        p.many.rows = R <= 128 ? 128 : 256;
+        if (p.use_few) {
+            p.many.rows_from = kFewRows + 1;
+            p.few.rows_to = kFewRows;
+        }
+        if (!divide(d, p.many, 256, 4, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
+    }
+    if (p.use_few) {
+        p.few.rows = R <= 16 ? 16 : 32;
+        if (!divide(d, p.few, 512, 2, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+    }
     return PDEC_OK;
 }
 
@@ -344,14 +359,20 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
         a->out = out;
         a->lse = lse;
     }
+    char* const ws = static_cast<char*>(workspace);
+    auto finish = [&](const PagedArgs& a) {
+        if (!a.whole) launch_paged_finish(a, d->head_dim, d->dtype, s);
+        return launched();
+    };
+    if (p.use_many) {
+        place(p.many, ws + align256(p.few_bytes));
+        launch_paged_rows(p.many, d->head_dim, paged_grid(p.many), s);
+        if ((rc = launched()) != PDEC_OK || (rc = finish(p.many)) != PDEC_OK) return rc;
+    }
     if (p.use_few) {
-        place(p.few, static_cast<char*>(workspace));
+        place(p.few, ws);
         launch_paged_f32(p.few, d->head_dim, d->dtype, d->cache_dtype, s);
-        if (launched() != PDEC_OK) return PDEC_ERR_HIP;
-        if (!p.few.whole) {
-            launch_paged_finish(p.few, d->head_dim, d->dtype, s);
-            if (launched() != PDEC_OK) return PDEC_ERR_HIP;
-        }
+        if ((rc = launched()) != PDEC_OK || (rc = finish(p.few)) != PDEC_OK) return rc;
     }
     return PDEC_OK;
 }

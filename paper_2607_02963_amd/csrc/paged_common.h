@@ -126,9 +126,8 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r)
     for (int j0 = 0; j0 < J; j0 += 64) {
         const int n = j0 + lane < J ? paged_units(a, j0 + lane) : 0, incl = scan(n);
         if (j0 == 0) n0 = n, incl0 = incl;
-        total += __shfl(incl, 63);
+        total += __builtin_amdgcn_readlane(incl, 63);
     }
-    total = __builtin_amdgcn_readfirstlane(total);
     r.per = max((total * a.H_kv + a.workers - 1) / a.workers, a.least);
     r.pos = w * r.per;
     if (total == 0 || r.pos >= total * a.H_kv) return false;
@@ -141,15 +140,15 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r)
             n = j0 + lane < J ? paged_units(a, j0 + lane) : 0;
             incl = scan(n);
         }
-        const int all = __shfl(incl, 63);
+        const int all = __builtin_amdgcn_readlane(incl, 63);  // scalar, as everything that leaves the loop
         if (rest >= all) {
             rest -= all;
             continue;
         }
         const int at = __builtin_ctzll(__ballot(incl > rest));
-        r.j = __builtin_amdgcn_readfirstlane(j0 + at);
-        r.units = __builtin_amdgcn_readfirstlane(__shfl(n, at));
-        r.u = __builtin_amdgcn_readfirstlane(rest - __shfl(incl - n, at));
+        r.j = j0 + at;
+        r.units = __builtin_amdgcn_readlane(n, at);
+        r.u = rest - __builtin_amdgcn_readlane(incl - n, at);
         break;
     }
     return true;
@@ -207,14 +206,35 @@ __device__ inline long paged_qrow(const PagedArgs& a, const PagedSeq& x, int hea
     return (long)(x.t0 + i) * a.H_q + head * a.G + (r - i * a.G);
 }
 
-// Page of unit-aligned key t of a sequence, -1 if absent.
+// Entry i (uniform) of a row of the block table, through the scalar cache.
+__device__ inline int paged_entry(const int32_t* row, int i)
+{
+    typedef __attribute__((address_space(4))) const int32_t const_i32_t;
+    return ((const_i32_t*)(uintptr_t)row)[i];
+}
+
+// Page of key t of a sequence, -1 if absent.
 __device__ inline int paged_page(const PagedArgs& a, int s, int t)
 {
     const int p = a.block_table[(long)s * a.max_pages + min(t >> a.page_shift, a.max_pages - 1)];
     return (uint32_t)p < (uint32_t)a.num_pages ? p : -1;
 }
 
+// First unit in [u0, u1) of a sequence that has a page (any: some of its
+// keys', not any: lacks one), u1 if there is none.  Uniform over the wave, every lane active.
+__device__ inline int paged_find(const PagedArgs& a, int s, int u0, int u1, bool any)
+{
+    const int lane = paged_lane();
+    for (int t0 = u0 * kUnit; t0 < u1 * kUnit; t0 += 16 * 64) {  // a lane per 16 keys
+        const int t = t0 + 16 * lane;
+        const uint64_t b = __ballot(t < u1 * kUnit && (paged_page(a, s, t) >= 0) == any);
+        if (b) return (t0 + 16 * __builtin_ctzll(b)) / kUnit;
+    }
+    return u1;
+}
+
 void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t stream);
+void launch_paged_rows(const PagedArgs& a, int head_dim, int grid, hipStream_t stream);
 void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t stream);
 
 }  // namespace pdec
