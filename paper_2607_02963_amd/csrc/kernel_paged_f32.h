@@ -54,9 +54,6 @@ struct PagedRaw {
     }
 };
 
-// 2^(byte - 127) of byte i of a word; 0 for a byte of 0
-__device__ inline float paged_scale(uint32_t word, int i) { return __uint_as_float(((word >> (8 * i)) & 255u) << 23); }
-
 __device__ inline f32x4_t paged_mfma4(float a, float b, f32x4_t c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);

@@ -12,6 +12,13 @@
 // scores of block b + 1 multiplied under the exponentials of block b and the
 // P V products of block b under the maxima of block b + 1.
 //
+// 8-bit pages: a wave moves its 32 keys as they are into three raw slots of its
+// own, and between two barriers turns those of stage st + 2 into a bfloat16 slot
+// of the ring (one v_cvt_scalef32_pk_bf16_fp8 per pair, the key's power of two
+// with it: exact), spread over the steps of the P V phases, whose vector work is
+// light.  Turning them where they are read would do it once per wave, four times
+// in all.  The products and all that follows are the same.
+//
 // Units that all rows of a wave see whole take that pipelined loop.  Units
 // with hidden keys (the chunk's own tokens, the sequence's end, absent pages)
 // take a plain one, tile by tile, where a value that is not finite meets only
@@ -46,16 +53,25 @@ __device__ inline void dma_16B_page(uint64_t base, uint32_t off, uint32_t lds_ba
                  : "memory");
 }
 
-template <int D, int NT>
+typedef __attribute__((ext_vector_type(2))) __bf16 paged_bf16x2_t;
+
+template <int D, int NT, bool FP8>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
 {
     constexpr int NW = 4;
     using C = BranchCfg<D, NT, NW>;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[C::NSTAGE * C::STAGE];
+    constexpr int NB = FP8 ? 3 : C::NSTAGE;       // bfloat16 slots of the ring
+    constexpr int NRAW = 3, RAW = FP8 ? 32 * D : 0;  // raw slots of a wave, and their bytes
+    constexpr int ESZ = FP8 ? 1 : 2;
+    constexpr int CPK = D * ESZ / 16;             // 16-byte chunks per key in memory
+    constexpr int KPI = 64 / CPK;                 // keys per piece of a DMA instruction
+    constexpr int PPW = 32 / KPI;                 // pieces of a wave per stage, a half's one after the other's
+    constexpr int AHEAD = FP8 ? 5 : 3;            // stage moved behind the barrier of stage st: st + AHEAD
+    constexpr int FLIGHT = FP8 ? 2 * PPW : PPW;   // pieces that may be under way at a barrier
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NB * C::STAGE + NW * NRAW * RAW];
 
     const int tid = wi_id();
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const float c = a.qscale;
     PagedRun run;
     PagedPart part;
@@ -65,49 +81,63 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         return;
     }
 
-    // ---- DMA: this wave moves keys 32 (w % 2) .. + 31 of a unit, of K (w < 2) or V ----
-    const bool w_is_v = w >= NW / 2;
-    const uint32_t strideB = (uint32_t)a.H_kv * D * 2;
-    const int pkey = lane / C::CH;  // key of the lane within a piece
-    const int key0 = 32 * (w % 2) + pkey;
-    uint32_t off[4];  // byte offset of the lane's chunk in piece i of a half, of period 4 in i
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int key = key0 + i * C::KPI;
-        off[i] = (uint32_t)(pkey + (i % (C::PPW / 2)) * C::KPI) * strideB +
-                 16u * ((lane % C::CH) ^ (w_is_v ? branch_vswz<D>(key) : branch_kswz<D>(key)));
-    }
-    static_assert(16 % C::KPI == 0 && C::PPW * C::KPI == 32, "a wave's pieces are two halves of 16 keys");
-    const uint32_t m_base = lds_u32(lds) + (w_is_v ? C::STAGE_K : 0) + 32 * (w % 2) * C::ROWB;
-    const uint64_t pool = sgpr_base(w_is_v ? a.v_pages : a.k_pages);
-
-    // operand reads, as for whole branches
-    const int koff = l32 * C::ROWB + 16 * (hi ^ branch_kswz<D>(l32));
-    int voff[C::DT];
-    {
-        const int q = lane >> 4, i = lane & 15;
-        const int key = 4 * (q >> 1) + (i >> 2);
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-            voff[dt] = key * C::ROWB + 16 * ((4 * dt + 2 * (q & 1) + ((i & 3) >> 1)) ^ branch_vswz<D>(key)) + 8 * (i & 1);
-    }
-    auto slot = [&](int st) __attribute__((always_inline)) { return lds + (st % C::NSTAGE) * C::STAGE; };
-    auto read_k = [&](u32x4_t (&kf)[C::KS], const unsigned char* buf, int kb, int t) __attribute__((always_inline)) {
-        kf[t] = *reinterpret_cast<const u32x4_t*>(buf + kb * C::ROWB + (koff ^ (32 * t)));
-    };
-    // half r (8 keys) of V operand (s, dt), index j = 2 (DT s + dt) + r: lane's keys 16 s + 8 r + 4 (l / 32) .. + 3
-    auto read_v = [&](u32x2_t (&vf)[4 * C::DT], const unsigned char* buf, int kb, int j) __attribute__((always_inline)) {
-        const int s = j / (2 * C::DT), dt = (j / 2) % C::DT;
-        const unsigned char* va = buf + C::STAGE_K + (kb + 16 * s + 8 * (j & 1)) * C::ROWB + voff[dt];
-        vf[j] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                (__attribute__((address_space(3))) s16x4_t*)va));
-    };
-    auto v_op = [&](const u32x2_t (&vf)[4 * C::DT], int s, int dt) __attribute__((always_inline)) {
-        const u32x2_t x0 = vf[2 * (C::DT * s + dt)], x1 = vf[2 * (C::DT * s + dt) + 1];
-        return u32x4_t{x0.x, x0.y, x1.x, x1.y};
-    };
-
     while (paged_next(a, run, part, tid == 0)) {
+        // The lane's offsets belong to the part: kept over the loop they would take
+        // the registers that the pipelined loop needs (the compiler hoists what it can,
+        // and spills).
+        int lane = tid & 63;
+        asm volatile("" : "+v"(lane));
+        const int l32 = lane & 31, hi = lane >> 5;
+
+        // ---- DMA: this wave moves keys 32 (w % 2) .. + 31 of a unit, of K (w < 2) or V ----
+        const bool w_is_v = w >= NW / 2;
+        const uint32_t strideB = (uint32_t)a.H_kv * D * ESZ;
+        const int pkey = lane / CPK;  // key of the lane within a piece
+        uint32_t off[4];  // byte offset of the lane's chunk in piece i, of period 4 in i
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int key = 32 * (w % 2) + pkey + i * KPI;
+            // bfloat16 pieces land in the ring's permuted places, raw ones in a row
+            const int ch = FP8 ? lane % CPK : (lane % CPK) ^ (w_is_v ? branch_vswz<D>(key) : branch_kswz<D>(key));
+            off[i] = (uint32_t)(pkey + (i % (PPW / 2)) * KPI) * strideB + 16u * ch;
+        }
+        static_assert(16 % KPI == 0 && PPW * KPI == 32 && (PPW / 2 <= 4), "a wave's pieces are two halves of 16 keys");
+        unsigned char* const ring_w = lds + (w_is_v ? C::STAGE_K : 0) + 32 * (w % 2) * C::ROWB;  // its keys of slot 0
+        unsigned char* const raw_w = lds + NB * C::STAGE + w * NRAW * RAW;                       // its raw slots
+        const uint32_t m_base = lds_u32(FP8 ? raw_w : ring_w);
+        // 8-bit pages: the lane's first chunk, of key pkey, in raw slot 0 and in slot 0 of
+        // the ring; the keys of every second piece have bit 3, which permutes K chunks
+        const uint32_t raw0 = lds_u32(raw_w) + 16 * lane;
+        const uint32_t ring0 = lds_u32(ring_w) + pkey * C::ROWB + 16 * ((2 * (lane % CPK)) ^ (w_is_v ? branch_vswz<D>(pkey) : branch_kswz<D>(pkey)));
+        const uint32_t kflip = w_is_v ? 0 : 128;
+        static_assert(!FP8 || D == 64 || KPI == 8, "branch_kswz takes bits 0 to 3 of a key at D = 128, 1 to 3 at D = 64");
+        const uint64_t pool = sgpr_base(w_is_v ? a.v_pages : a.k_pages);
+        const uint64_t scales = FP8 ? sgpr_base(w_is_v ? a.v_scales : a.k_scales) : 0;
+
+        // operand reads, as for whole branches.  A K step t, and a V tile dt, flip bits
+        // of the address that nothing else sets: an address is its slot's and the
+        // lane's sum, formed once a stage, with those bits flipped.
+        const uint32_t koff = lds_u32(lds) + l32 * C::ROWB + 16 * (hi ^ branch_kswz<D>(l32));
+        const int vq = lane >> 4, vi = lane & 15, vkey = 4 * (vq >> 1) + (vi >> 2);
+        const uint32_t voff = lds_u32(lds) + C::STAGE_K + vkey * C::ROWB +
+                              16 * ((2 * (vq & 1) + ((vi & 3) >> 1)) ^ branch_vswz<D>(vkey)) + 8 * (vi & 1);
+        auto slot = [&](int st) __attribute__((always_inline)) { return (uint32_t)((st % NB) * C::STAGE); };
+        auto read_k = [&](u32x4_t (&kf)[C::KS], uint32_t kbuf, int kb, int t) __attribute__((always_inline)) {
+            typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
+            kf[t] = *(lds_u32x4_t*)(uintptr_t)((kbuf ^ (32 * t)) + kb * C::ROWB);
+        };
+        // half r (8 keys) of V operand (s, dt), index j = 2 (DT s + dt) + r: lane's keys 16 s + 8 r + 4 (l / 32) .. + 3
+        auto read_v = [&](u32x2_t (&vf)[4 * C::DT], uint32_t vbuf, int kb, int j) __attribute__((always_inline)) {
+            const int s = j / (2 * C::DT), dt = (j / 2) % C::DT;
+            vf[j] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                    (__attribute__((address_space(3))) s16x4_t*)(uintptr_t)(
+                                                        (vbuf ^ (64 * dt)) + (kb + 16 * s + 8 * (j & 1)) * C::ROWB)));
+        };
+        auto v_op = [&](const u32x2_t (&vf)[4 * C::DT], int s, int dt) __attribute__((always_inline)) {
+            const u32x2_t x0 = vf[2 * (C::DT * s + dt)], x1 = vf[2 * (C::DT * s + dt) + 1];
+            return u32x4_t{x0.x, x0.y, x1.x, x1.y};
+        };
+
         const PagedSeq sq = paged_seq(a, part.s);
         const int R = sq.n * a.G, row0 = part.group * C::RT, nrows = min(C::RT, R - row0);
         const int32_t* table = a.block_table + (long)part.s * a.max_pages;
@@ -116,7 +146,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         const int nst = part.u1 - u0, t0 = u0 * kUnit;
         const int wrow0 = C::WROWS * w;
         const bool active = wrow0 < nrows;
-        const uint64_t base0 = pool + 2 * (uint64_t)part.head * D;
+        const uint64_t base0 = pool + (uint64_t)part.head * D * ESZ;
 
         // Pages of stage st's two halves that this wave moves.  Stages past the last repeat it.
         struct Pages { int half[2]; };
@@ -138,16 +168,71 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 const int row = (t + 16 * h) & ((1 << a.page_shift) - 1);
                 p.base[h] = base0 + (((uint64_t)(uint32_t)page << a.page_shift) + (uint32_t)row) * strideB;
             }
-            p.dst = m_base + (st % C::NSTAGE) * C::STAGE;
+            p.dst = m_base + (FP8 ? (st % NRAW) * RAW : (st % NB) * C::STAGE);
             p.lanes = ring_lanes(st, nst);
             return p;
         };
         auto issue_piece = [&](const Pending& pd, int i) __attribute__((always_inline)) {
-            dma_16B_page(pd.base[i / (C::PPW / 2)], off[i & 3], pd.dst + 1024 * i, pd.lanes);
+            dma_16B_page(pd.base[i / (PPW / 2)], off[i & 3], pd.dst + 1024 * i, pd.lanes);
         };
         auto issue_stage = [&](const Pending& pd) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < C::PPW; ++i) issue_piece(pd, i);
+            for (int i = 0; i < PPW; ++i) issue_piece(pd, i);
+        };
+
+        // 8-bit pages: the scale bytes of the wave's two halves of stage st, and the
+        // turning of a raw stage.  Item m of 4 PPW: word m % 4 of chunk m / 4.
+        struct Scales { u32x4_t half[2]; };
+        auto load_scales = [&](int st, const Pages& x) __attribute__((always_inline)) {
+            const int t = t0 + max(min(st, nst - 1), 0) * kUnit + 32 * (w & 1);
+            Scales sc;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int page = (uint32_t)x.half[h] < (uint32_t)a.num_pages ? x.half[h] : 0;
+                const int row = (t + 16 * h) & ((1 << a.page_shift) - 1);
+                typedef __attribute__((address_space(4))) const u32x4_t const_u32x4_t;
+                sc.half[h] = *(const_u32x4_t*)(scales + ((((uint64_t)(uint32_t)page * a.H_kv + part.head) << a.page_shift) + (uint32_t)row));
+            }
+            return sc;
+        };
+        // A lane's scale bytes of its PPW chunks, chunk i in byte i.  Its key of a
+        // half's chunk i is byte i KPI + pkey of the half.
+        auto lane_scales = [&](const Scales& sc) __attribute__((always_inline)) {
+            uint32_t bytes = 0;
+#pragma unroll
+            for (int i = 0; i < PPW; ++i) {
+                const u32x4_t b = sc.half[i / (PPW / 2)];
+                const int b0 = (i % (PPW / 2)) * KPI / 4;
+                uint32_t word;
+                if constexpr (KPI == 8) word = pkey < 4 ? b[b0] : b[b0 + 1];
+                else word = pkey < 8 ? (pkey < 4 ? b[0] : b[1]) : (pkey < 12 ? b[2] : b[3]);
+                bytes |= ((word >> (8 * (pkey & 3))) & 255u) << (8 * i);
+            }
+            return bytes;
+        };
+        // from: the lane's 16 bytes of chunk 0 in the raw slot; to: the place of the
+        // first half of its first key's chunk in the ring.  The second half is beside
+        // it, and chunk i's key i KPI rows on, its K chunks permuted by one bit more.
+        u32x4_t raw, wide;
+        auto turn = [&](uint32_t bytes, uint32_t from, uint32_t to, int m) __attribute__((always_inline)) {
+            typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+            const int i = m / 4, j = m % 4;
+            if (j == 0) raw = *reinterpret_cast<const lds_u32x4_t*>((uintptr_t)(from + 1024 * i));
+            const float scale = paged_scale(bytes, i);
+            wide[2 * (j & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], scale, false));
+            wide[2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], scale, true));
+            if (j & 1) {
+                const uint32_t flip = (D == 128 && (i & 1) ? kflip : 0) + 16 * (j >> 1);
+                *reinterpret_cast<lds_u32x4_t*>((uintptr_t)((to ^ flip) + i * KPI * C::ROWB)) = wide;
+            }
+        };
+        constexpr int ITEMS = 4 * PPW;
+        auto raw_of = [&](int st) __attribute__((always_inline)) { return raw0 + (st % NRAW) * RAW; };
+        auto ring_of = [&](int st) __attribute__((always_inline)) { return ring0 + (st % NB) * C::STAGE; };
+        auto turn_stage = [&](int st, const Scales& sc) __attribute__((always_inline)) {
+            const uint32_t bytes = lane_scales(sc);
+#pragma unroll
+            for (int m = 0; m < ITEMS; ++m) turn(bytes, raw_of(st), ring_of(st), m);
         };
 
         // ---- this lane's rows: 32 nt + l % 32 of the wave ----
@@ -166,12 +251,29 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         // The wave's first nd stages are seen whole by all of its rows.
         const int nd = !active ? 0 : max(min(paged_find(a, part.s, u0, min(part.u1, least / kUnit), false), least / kUnit) - u0, 0);
         lds_barrier();  // no wave reads the ring for the part before any more
+        // Pages of the stages to come: ahead[i] of stage st + AHEAD - i before the barrier of stage st.
+        constexpr int HIST = FP8 ? 3 : 1;
+        Pages ahead[HIST];
+        Scales next;  // of stage st + 2
+        if (nst > 0) {
 #pragma unroll
-        for (int st = 0; st < C::NSTAGE - 1; ++st)
-            if (nst > 0) issue_stage(pending(st, pages(st)));
-        Pages ahead = pages(C::NSTAGE - 1);  // the pages of the next stage to move
+            for (int st = 0; st < 3; ++st) issue_stage(pending(st, pages(st)));
+        }
         // the query loads and the DMA complete in no order relative to each other
         wait_vmcnt<0>();
+        if constexpr (FP8) {
+            // a wave reads only its own raw slots: no barrier
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+                if (nst > 0) {
+                    turn_stage(st, load_scales(st, pages(st)));
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    issue_stage(pending(st + 3, pages(st + 3)));
+                }
+            next = load_scales(2, pages(2));
+        }
+#pragma unroll
+        for (int i = 0; i < HIST; ++i) ahead[i] = pages(AHEAD - i);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -239,7 +341,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         // The two phases of a block (kernel_branch.h).
         // A: the next block's scores sn under this block's exponentials.
         auto phase_a = [&](bf32x16_t (&sn)[NT], const bf32x16_t (&sc)[NT], u32x4_t (&pk)[NT][2],
-                           const u32x4_t (&kf)[C::KS], u32x2_t (&vf)[4 * C::DT], const unsigned char* buf,
+                           const u32x4_t (&kf)[C::KS], u32x2_t (&vf)[4 * C::DT], uint32_t vbuf,
                            int kb) __attribute__((always_inline)) {
             constexpr int STEPS = NT * C::KS;
             __builtin_amdgcn_sched_barrier(0);
@@ -247,27 +349,24 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             for (int i = 0; i < STEPS; ++i) {
                 score_step(sn, kf, i);
 #pragma unroll
-                for (int j = i * 4 * C::DT / STEPS; j < (i + 1) * 4 * C::DT / STEPS; ++j) read_v(vf, buf, kb, j);
+                for (int j = i * 4 * C::DT / STEPS; j < (i + 1) * 4 * C::DT / STEPS; ++j) read_v(vf, vbuf, kb, j);
 #pragma unroll
                 for (int j = i * 8 * NT / STEPS; j < (i + 1) * 8 * NT / STEPS; ++j) prob_step(pk, sc, j);
             }
         };
         // B: this block's P V products under the next block's maxima, the K
-        // operands of the block after it and, with DMA, a later stage's pieces.
-        auto phase_b = [&](auto dma, const u32x4_t (&pk)[NT][2], const u32x2_t (&vf)[4 * C::DT],
-                           const bf32x16_t (&sn)[NT], float (&mx)[NT], u32x4_t (&kf)[C::KS], const unsigned char* nbuf,
-                           int nkb, const Pending& pd) __attribute__((always_inline)) {
+        // operands of the block after it, and extra(i, steps) at step i.
+        auto phase_b = [&](auto extra, const u32x4_t (&pk)[NT][2], const u32x2_t (&vf)[4 * C::DT],
+                           const bf32x16_t (&sn)[NT], float (&mx)[NT], u32x4_t (&kf)[C::KS], uint32_t kbuf,
+                           int nkb) __attribute__((always_inline)) {
             constexpr int STEPS = 2 * C::DT * NT;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 pv_step(pk, vf, i);
 #pragma unroll
-                for (int j = i * C::KS / STEPS; j < (i + 1) * C::KS / STEPS; ++j) read_k(kf, nbuf, nkb, j);
-                if constexpr (decltype(dma)::value) {
-#pragma unroll
-                    for (int j = i * C::PPW / STEPS; j < (i + 1) * C::PPW / STEPS; ++j) issue_piece(pd, j);
-                }
+                for (int j = i * C::KS / STEPS; j < (i + 1) * C::KS / STEPS; ++j) read_k(kf, kbuf, nkb, j);
+                extra(i, STEPS);
 #pragma unroll
                 for (int j = i * 8 * NT / STEPS; j < (i + 1) * 8 * NT / STEPS; ++j) max_step(mx, sn, j);
             }
@@ -275,10 +374,21 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             for (int nt = 0; nt < NT; ++nt) asm volatile("" : "+v"(mx[nt]));
         };
         // Every wave passes one barrier per stage, in either loop; behind the one of
-        // stage st, stage st + 1 has landed and stage st - 1 been consumed for all of
-        // them, and the slot of the latter takes stage st + 3, whose pages were read
-        // one stage ago.
-        if (nst > 0) lds_barrier();  // the first three stages have landed
+        // stage st, stage st + 1 is in the ring and stage st - 1 been consumed for all
+        // of them.  bfloat16 pages: the slot of the latter takes stage st + 3.  8-bit
+        // pages: stage st + 2 has landed in the wave's raw slot; it goes to the slot of
+        // stage st - 1, and its raw slot then takes stage st + 5.
+        auto before_barrier = [&](int st, Pending& pd, Scales& sc) __attribute__((always_inline)) {
+            pd = pending(st + AHEAD, ahead[0]);
+            if constexpr (FP8) {
+                sc = next;
+                next = load_scales(st + 3, ahead[2]);
+            }
+#pragma unroll
+            for (int i = HIST - 1; i > 0; --i) ahead[i] = ahead[i - 1];
+            ahead[0] = pages(st + AHEAD + 1);
+        };
+        if (nst > 0) lds_barrier();  // stages 0 and 1 are in the ring
         if (nd > 0) {
             // Entering stage st: sa holds block 0's scores (reference set), kf block 1's K operands.
             bf32x16_t sa[NT], sb[NT];
@@ -286,36 +396,62 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             u32x2_t vf[4 * C::DT];
             float mx[NT];
 #pragma unroll
-            for (int t = 0; t < C::KS; ++t) read_k(kf, slot(0), 0, t);
+            for (int t = 0; t < C::KS; ++t) read_k(kf, koff + slot(0), 0, t);
 #pragma unroll
             for (int i = 0; i < NT * C::KS; ++i) score_step(sa, kf, i);
 #pragma unroll
             for (int i = 0; i < 8 * NT; ++i) max_step(mx, sa, i);
             rescale(mx);
 #pragma unroll
-            for (int t = 0; t < C::KS; ++t) read_k(kf, slot(0), 32, t);
+            for (int t = 0; t < C::KS; ++t) read_k(kf, koff + slot(0), 32, t);
             for (int st = 0; st < nd; ++st) {
-                const unsigned char* buf = slot(st);
-                const unsigned char* nbuf = slot(st + 1);
-                phase_a(sb, sa, pk, kf, vf, buf, 0);
-                const Pending pd = pending(st + 3, ahead);
-                ahead = pages(st + 4);
-                stage_barrier<C::PPW>();
-                phase_b(std::true_type{}, pk, vf, sb, mx, kf, nbuf, 0, pd);
+                const uint32_t vbuf = voff + slot(st), kbuf = koff + slot(st + 1);
+                phase_a(sb, sa, pk, kf, vf, vbuf, 0);
+                Pending pd;
+                Scales sc;
+                before_barrier(st, pd, sc);
+                stage_barrier<FLIGHT>();
+                uint32_t bytes = 0;
+                if constexpr (FP8) bytes = lane_scales(sc);
+                const uint32_t from = raw_of(st + 2), to = ring_of(st + 2);
+                phase_b(
+                    [&](int i, int steps) __attribute__((always_inline)) {
+                        if constexpr (FP8) {
+#pragma unroll
+                            for (int m = i * (ITEMS / 2) / steps; m < (i + 1) * (ITEMS / 2) / steps; ++m) turn(bytes, from, to, m);
+                        } else {
+#pragma unroll
+                            for (int j = i * PPW / steps; j < (i + 1) * PPW / steps; ++j) issue_piece(pd, j);
+                        }
+                    },
+                    pk, vf, sb, mx, kf, kbuf, 0);
                 rescale(mx);
-                phase_a(sa, sb, pk, kf, vf, buf, 32);
-                phase_b(std::false_type{}, pk, vf, sa, mx, kf, nbuf, 32, pd);
+                phase_a(sa, sb, pk, kf, vf, vbuf, 32);
+                phase_b(
+                    [&](int i, int steps) __attribute__((always_inline)) {
+                        if constexpr (FP8) {
+#pragma unroll
+                            for (int m = i * (ITEMS / 2) / steps; m < (i + 1) * (ITEMS / 2) / steps; ++m) turn(bytes, from, to, ITEMS / 2 + m);
+                        }
+                    },
+                    pk, vf, sa, mx, kf, kbuf, 32);
+                if constexpr (FP8) issue_stage(pd);  // the raw slot has been read
                 if (st + 1 < nd) rescale(mx);
             }
         }
         for (int st = nd; st < nst; ++st) {
             {
-                const Pending pd = pending(st + 3, ahead);
-                ahead = pages(st + 4);
-                stage_barrier<C::PPW>();
+                Pending pd;
+                Scales sc;
+                before_barrier(st, pd, sc);
+                stage_barrier<FLIGHT>();
+                if constexpr (FP8) {
+                    turn_stage(st + 2, sc);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the raw slot has been read
+                }
                 issue_stage(pd);
             }
-            const unsigned char* buf = slot(st);
+            const uint32_t vbuf = voff + slot(st), kbuf = koff + slot(st);
             const int t = t0 + st * kUnit;
             int most = 0;
 #pragma unroll
@@ -331,9 +467,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 bf32x16_t s[NT];
                 float mx[NT];
 #pragma unroll
-                for (int i = 0; i < C::KS; ++i) read_k(kf, buf, kb, i);
+                for (int i = 0; i < C::KS; ++i) read_k(kf, kbuf, kb, i);
 #pragma unroll
-                for (int j = 0; j < 4 * C::DT; ++j) read_v(vf, buf, kb, j);
+                for (int j = 0; j < 4 * C::DT; ++j) read_v(vf, vbuf, kb, j);
                 uint32_t odd = 0;
 #pragma unroll
                 for (int j = 0; j < 4 * C::DT; ++j) odd |= strange_bf16x2(vf[j].x) | strange_bf16x2(vf[j].y);
@@ -371,24 +507,26 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                         }
                     if (!apart) continue;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                    for (int j = 0; j < 2 * C::DT; ++j) {
+                        const int k = j / C::DT, dt = j % C::DT;
+                        const u32x4_t v0 = v_op(vf, k, dt);
+                        bf32x16_t sum = o[nt][dt];
 #pragma unroll 1
                         for (int key = 0; key < 16; ++key) {
                             const bool sees = (16 * k + key < lim) & (k ? there1 : there0);
                             const bool mine = hi == ((key >> 2) & 1);
                             const int word = 2 * (key >> 3) + ((key & 3) >> 1);
                             const uint32_t half = (key & 1) ? 0xffff0000u : 0xffffu;
+                            u32x4_t v = v0;
+                            asm volatile("" : "+v"(v));  // nothing of this rare loop before it
 #pragma unroll
-                            for (int dt = 0; dt < C::DT; ++dt) {
-                                u32x4_t v = v_op(vf, k, dt);
-                                asm volatile("" : "+v"(v));  // nothing of this rare loop before it
+                            for (int e = 0; e < 4; ++e) v[e] &= strange_bf16x2(v[e]) & ((mine & (e == word)) ? half : 0u);
+                            const bf32x16_t x = branch_mfma(v, pk[nt][k], sum);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) v[e] &= strange_bf16x2(v[e]) & ((mine & (e == word)) ? half : 0u);
-                                const bf32x16_t x = branch_mfma(v, pk[nt][k], o[nt][dt]);
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[nt][dt][i] = sees ? x[i] : o[nt][dt][i];
-                            }
+                            for (int i = 0; i < 16; ++i) sum[i] = sees ? x[i] : sum[i];
                         }
+                        o[nt][dt] = sum;
+                    }
                 }
             }
         }

@@ -165,7 +165,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     a.rows_from = 0;
     a.rows_to = INT32_MAX;
     p.few = p.many = a;
-    p.use_many = d->dtype == PDEC_DTYPE_BF16 && d->cache_dtype == PDEC_DTYPE_BF16 && R > kFewRows;
+    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > kFewRows;
     // one sequence is the many rows' whatever its chunk; of several, each goes by its own
     p.use_few = !p.use_many || d->num_seqs > 1;
     if (p.use_many) {
@@ -366,7 +366,7 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
     };
     if (p.use_many) {
         place(p.many, ws + align256(p.few_bytes));
-        launch_paged_rows(p.many, d->head_dim, paged_grid(p.many), s);
+        launch_paged_rows(p.many, d->head_dim, d->cache_dtype == PDEC_DTYPE_E4M3, paged_grid(p.many), s);
         if ((rc = launched()) != PDEC_OK || (rc = finish(p.many)) != PDEC_OK) return rc;
     }
     if (p.use_few) {

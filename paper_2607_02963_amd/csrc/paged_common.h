@@ -233,8 +233,11 @@ __device__ inline int paged_find(const PagedArgs& a, int s, int u0, int u1, bool
     return u1;
 }
 
+// 2^(byte - 127) of byte i of a word; 0 for a byte of 0
+__device__ inline float paged_scale(uint32_t word, int i) { return __uint_as_float(((word >> (8 * i)) & 255u) << 23); }
+
 void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t stream);
-void launch_paged_rows(const PagedArgs& a, int head_dim, int grid, hipStream_t stream);
+void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, int grid, hipStream_t stream);
 void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t stream);
 
 }  // namespace pdec

@@ -7,16 +7,21 @@
 
 namespace pdec {
 
-void launch_paged_rows(const PagedArgs& a, int head_dim, int grid, hipStream_t s)
+namespace {
+
+template <int D, bool FP8>
+void launch_rows(const PagedArgs& a, int grid, hipStream_t s)
 {
-    const dim3 g((unsigned)grid), b(256);
-    if (head_dim == 128) {
-        if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<128, 2>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((paged_rows_kernel<128, 1>), g, b, 0, s, a);
-    } else {
-        if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<64, 2>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((paged_rows_kernel<64, 1>), g, b, 0, s, a);
-    }
+    if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<D, 2, FP8>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8>), dim3((unsigned)grid), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, int grid, hipStream_t s)
+{
+    if (head_dim == 128) fp8 ? launch_rows<128, true>(a, grid, s) : launch_rows<128, false>(a, grid, s);
+    else fp8 ? launch_rows<64, true>(a, grid, s) : launch_rows<64, false>(a, grid, s);
 }
 
 }  // namespace pdec
