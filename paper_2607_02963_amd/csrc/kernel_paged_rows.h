@@ -53,7 +53,13 @@ __device__ inline void dma_16B_page(uint64_t base, uint32_t off, uint32_t lds_ba
                  : "memory");
 }
 
-typedef __attribute__((ext_vector_type(2))) __bf16 paged_bf16x2_t;
+// The same for the scales: one dword per lane from the lane's own address.
+__device__ inline void dma_4B_lanes(uint64_t addr, uint32_t lds_base, uint64_t lanes)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b64 exec, -1" :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(addr), "s"(sgpr_base(reinterpret_cast<const void*>(lanes)))
+                 : "memory");
+}
 
 template <int D, int NT, bool FP8>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
@@ -67,8 +73,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
     constexpr int KPI = 64 / CPK;                 // keys per piece of a DMA instruction
     constexpr int PPW = 32 / KPI;                 // pieces of a wave per stage, a half's one after the other's
     constexpr int AHEAD = FP8 ? 5 : 3;            // stage moved behind the barrier of stage st: st + AHEAD
-    constexpr int FLIGHT = FP8 ? 2 * PPW : PPW;   // pieces that may be under way at a barrier
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[NB * C::STAGE + NW * NRAW * RAW];
+    constexpr int FLIGHT = FP8 ? 2 * (PPW + 1) : PPW;  // pieces that may be under way at a barrier
+    constexpr int SCALES = FP8 ? 64 : 0;          // bytes for the 32 scales of a raw slot
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NB * C::STAGE + NW * NRAW * (RAW + SCALES)];
 
     const int tid = wi_id();
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -110,6 +117,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         const uint32_t raw0 = lds_u32(raw_w) + 16 * lane;
         const uint32_t ring0 = lds_u32(ring_w) + pkey * C::ROWB + 16 * ((2 * (lane % CPK)) ^ (w_is_v ? branch_vswz<D>(pkey) : branch_kswz<D>(pkey)));
         const uint32_t kflip = w_is_v ? 0 : 128;
+        const uint32_t sc_base = lds_u32(lds) + NB * C::STAGE + NW * NRAW * RAW + w * NRAW * SCALES;
         static_assert(!FP8 || D == 64 || KPI == 8, "branch_kswz takes bits 0 to 3 of a key at D = 128, 1 to 3 at D = 64");
         const uint64_t pool = sgpr_base(w_is_v ? a.v_pages : a.k_pages);
         const uint64_t scales = FP8 ? sgpr_base(w_is_v ? a.v_scales : a.k_scales) : 0;
@@ -158,18 +166,24 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             return x;
         };
         // An absent page is read as page 0; its keys are masked.
-        struct Pending { uint64_t base[2]; uint32_t dst; uint64_t lanes; };
+        struct Pending { uint64_t base[2]; uint32_t dst; uint64_t lanes; uint64_t scale; uint32_t scale_dst; };
         auto pending = [&](int st, const Pages& x) __attribute__((always_inline)) {
             const int t = t0 + min(st, nst - 1) * kUnit + 32 * (w & 1);
             Pending p;
+            uint64_t sc[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int page = (uint32_t)x.half[h] < (uint32_t)a.num_pages ? x.half[h] : 0;
                 const int row = (t + 16 * h) & ((1 << a.page_shift) - 1);
                 p.base[h] = base0 + (((uint64_t)(uint32_t)page << a.page_shift) + (uint32_t)row) * strideB;
+                sc[h] = scales + ((((uint64_t)(uint32_t)page * a.H_kv + part.head) << a.page_shift) + (uint32_t)row);
             }
             p.dst = m_base + (FP8 ? (st % NRAW) * RAW : (st % NB) * C::STAGE);
             p.lanes = ring_lanes(st, nst);
+            if constexpr (FP8) {  // lanes 0 .. 3 the first half's 16 bytes, 4 .. 7 the second's
+                p.scale = (lane & 4 ? sc[1] : sc[0]) + 4 * (lane & 3);
+                p.scale_dst = sc_base + (st % NRAW) * SCALES;
+            }
             return p;
         };
         auto issue_piece = [&](const Pending& pd, int i) __attribute__((always_inline)) {
@@ -178,61 +192,44 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         auto issue_stage = [&](const Pending& pd) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < PPW; ++i) issue_piece(pd, i);
+            if constexpr (FP8) dma_4B_lanes(pd.scale, pd.scale_dst, pd.lanes & 255u);
         };
 
-        // 8-bit pages: the scale bytes of the wave's two halves of stage st, and the
-        // turning of a raw stage.  Item m of 4 PPW: word m % 4 of chunk m / 4.
-        struct Scales { u32x4_t half[2]; };
-        auto load_scales = [&](int st, const Pages& x) __attribute__((always_inline)) {
-            const int t = t0 + max(min(st, nst - 1), 0) * kUnit + 32 * (w & 1);
-            Scales sc;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int page = (uint32_t)x.half[h] < (uint32_t)a.num_pages ? x.half[h] : 0;
-                const int row = (t + 16 * h) & ((1 << a.page_shift) - 1);
-                typedef __attribute__((address_space(4))) const u32x4_t const_u32x4_t;
-                sc.half[h] = *(const_u32x4_t*)(scales + ((((uint64_t)(uint32_t)page * a.H_kv + part.head) << a.page_shift) + (uint32_t)row));
-            }
-            return sc;
+        // 8-bit pages, the turning of a raw stage: item m of 4 PPW is word m % 4 of
+        // chunk m / 4.  from: the lane's 16 bytes of chunk 0 in the raw slot; sc: its
+        // key's scale byte; to: the place of the first half of its first key's chunk in
+        // the ring.  The second half is beside it, and chunk i's key i KPI rows on, its
+        // K chunks permuted by one bit more.  A chunk is read while the one before it is
+        // turned.
+        typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+        typedef __attribute__((address_space(3))) uint8_t lds_u8_t;
+        u32x4_t raw[2], wide;
+        float scale[2];
+        struct Turn { uint32_t from, sc, to; };
+        auto turn_of = [&](int st) __attribute__((always_inline)) {
+            return Turn{raw0 + (st % NRAW) * RAW, sc_base + (st % NRAW) * SCALES + pkey, ring0 + (st % NB) * C::STAGE};
         };
-        // A lane's scale bytes of its PPW chunks, chunk i in byte i.  Its key of a
-        // half's chunk i is byte i KPI + pkey of the half.
-        auto lane_scales = [&](const Scales& sc) __attribute__((always_inline)) {
-            uint32_t bytes = 0;
-#pragma unroll
-            for (int i = 0; i < PPW; ++i) {
-                const u32x4_t b = sc.half[i / (PPW / 2)];
-                const int b0 = (i % (PPW / 2)) * KPI / 4;
-                uint32_t word;
-                if constexpr (KPI == 8) word = pkey < 4 ? b[b0] : b[b0 + 1];
-                else word = pkey < 8 ? (pkey < 4 ? b[0] : b[1]) : (pkey < 12 ? b[2] : b[3]);
-                bytes |= ((word >> (8 * (pkey & 3))) & 255u) << (8 * i);
-            }
-            return bytes;
+        auto read_raw = [&](const Turn& u, int i) __attribute__((always_inline)) {
+            raw[i & 1] = *reinterpret_cast<const lds_u32x4_t*>((uintptr_t)(u.from + 1024 * i));
+            scale[i & 1] = paged_scale(*reinterpret_cast<const lds_u8_t*>((uintptr_t)(u.sc + KPI * i)), 0);
         };
-        // from: the lane's 16 bytes of chunk 0 in the raw slot; to: the place of the
-        // first half of its first key's chunk in the ring.  The second half is beside
-        // it, and chunk i's key i KPI rows on, its K chunks permuted by one bit more.
-        u32x4_t raw, wide;
-        auto turn = [&](uint32_t bytes, uint32_t from, uint32_t to, int m) __attribute__((always_inline)) {
-            typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+        auto turn = [&](const Turn& u, int m) __attribute__((always_inline)) {
             const int i = m / 4, j = m % 4;
-            if (j == 0) raw = *reinterpret_cast<const lds_u32x4_t*>((uintptr_t)(from + 1024 * i));
-            const float scale = paged_scale(bytes, i);
-            wide[2 * (j & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], scale, false));
-            wide[2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], scale, true));
+            if (j == 0 && i + 1 < PPW) read_raw(u, i + 1);
+            const uint32_t word = raw[i & 1][j];
+            wide[2 * (j & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, scale[i & 1], false));
+            wide[2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, scale[i & 1], true));
             if (j & 1) {
                 const uint32_t flip = (D == 128 && (i & 1) ? kflip : 0) + 16 * (j >> 1);
-                *reinterpret_cast<lds_u32x4_t*>((uintptr_t)((to ^ flip) + i * KPI * C::ROWB)) = wide;
+                *reinterpret_cast<lds_u32x4_t*>((uintptr_t)((u.to ^ flip) + i * KPI * C::ROWB)) = wide;
             }
         };
         constexpr int ITEMS = 4 * PPW;
-        auto raw_of = [&](int st) __attribute__((always_inline)) { return raw0 + (st % NRAW) * RAW; };
-        auto ring_of = [&](int st) __attribute__((always_inline)) { return ring0 + (st % NB) * C::STAGE; };
-        auto turn_stage = [&](int st, const Scales& sc) __attribute__((always_inline)) {
-            const uint32_t bytes = lane_scales(sc);
+        auto turn_stage = [&](int st) __attribute__((always_inline)) {
+            const Turn u = turn_of(st);
+            read_raw(u, 0);
 #pragma unroll
-            for (int m = 0; m < ITEMS; ++m) turn(bytes, raw_of(st), ring_of(st), m);
+            for (int m = 0; m < ITEMS; ++m) turn(u, m);
         };
 
         // ---- this lane's rows: 32 nt + l % 32 of the wave ----
@@ -251,10 +248,8 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         // The wave's first nd stages are seen whole by all of its rows.
         const int nd = !active ? 0 : max(min(paged_find(a, part.s, u0, min(part.u1, least / kUnit), false), least / kUnit) - u0, 0);
         lds_barrier();  // no wave reads the ring for the part before any more
-        // Pages of the stages to come: ahead[i] of stage st + AHEAD - i before the barrier of stage st.
-        constexpr int HIST = FP8 ? 3 : 1;
-        Pages ahead[HIST];
-        Scales next;  // of stage st + 2
+        // Pages of stage st + AHEAD before the barrier of stage st, read one stage ago.
+        Pages ahead;
         if (nst > 0) {
 #pragma unroll
             for (int st = 0; st < 3; ++st) issue_stage(pending(st, pages(st)));
@@ -266,14 +261,12 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
 #pragma unroll
             for (int st = 0; st < 2; ++st)
                 if (nst > 0) {
-                    turn_stage(st, load_scales(st, pages(st)));
+                    turn_stage(st);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     issue_stage(pending(st + 3, pages(st + 3)));
                 }
-            next = load_scales(2, pages(2));
         }
-#pragma unroll
-        for (int i = 0; i < HIST; ++i) ahead[i] = pages(AHEAD - i);
+        ahead = pages(AHEAD);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -378,16 +371,6 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         // of them.  bfloat16 pages: the slot of the latter takes stage st + 3.  8-bit
         // pages: stage st + 2 has landed in the wave's raw slot; it goes to the slot of
         // stage st - 1, and its raw slot then takes stage st + 5.
-        auto before_barrier = [&](int st, Pending& pd, Scales& sc) __attribute__((always_inline)) {
-            pd = pending(st + AHEAD, ahead[0]);
-            if constexpr (FP8) {
-                sc = next;
-                next = load_scales(st + 3, ahead[2]);
-            }
-#pragma unroll
-            for (int i = HIST - 1; i > 0; --i) ahead[i] = ahead[i - 1];
-            ahead[0] = pages(st + AHEAD + 1);
-        };
         if (nst > 0) lds_barrier();  // stages 0 and 1 are in the ring
         if (nd > 0) {
             // Entering stage st: sa holds block 0's scores (reference set), kf block 1's K operands.
@@ -407,18 +390,16 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             for (int st = 0; st < nd; ++st) {
                 const uint32_t vbuf = voff + slot(st), kbuf = koff + slot(st + 1);
                 phase_a(sb, sa, pk, kf, vf, vbuf, 0);
-                Pending pd;
-                Scales sc;
-                before_barrier(st, pd, sc);
+                const Pending pd = pending(st + AHEAD, ahead);
+                ahead = pages(st + AHEAD + 1);
                 stage_barrier<FLIGHT>();
-                uint32_t bytes = 0;
-                if constexpr (FP8) bytes = lane_scales(sc);
-                const uint32_t from = raw_of(st + 2), to = ring_of(st + 2);
+                const Turn u = turn_of(st + 2);
+                if constexpr (FP8) read_raw(u, 0);
                 phase_b(
                     [&](int i, int steps) __attribute__((always_inline)) {
                         if constexpr (FP8) {
 #pragma unroll
-                            for (int m = i * (ITEMS / 2) / steps; m < (i + 1) * (ITEMS / 2) / steps; ++m) turn(bytes, from, to, m);
+                            for (int m = i * (ITEMS / 2) / steps; m < (i + 1) * (ITEMS / 2) / steps; ++m) turn(u, m);
                         } else {
 #pragma unroll
                             for (int j = i * PPW / steps; j < (i + 1) * PPW / steps; ++j) issue_piece(pd, j);
@@ -431,7 +412,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                     [&](int i, int steps) __attribute__((always_inline)) {
                         if constexpr (FP8) {
 #pragma unroll
-                            for (int m = i * (ITEMS / 2) / steps; m < (i + 1) * (ITEMS / 2) / steps; ++m) turn(bytes, from, to, ITEMS / 2 + m);
+                            for (int m = i * (ITEMS / 2) / steps; m < (i + 1) * (ITEMS / 2) / steps; ++m) turn(u, ITEMS / 2 + m);
                         }
                     },
                     pk, vf, sa, mx, kf, kbuf, 32);
@@ -441,12 +422,11 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         }
         for (int st = nd; st < nst; ++st) {
             {
-                Pending pd;
-                Scales sc;
-                before_barrier(st, pd, sc);
+                const Pending pd = pending(st + AHEAD, ahead);
+                ahead = pages(st + AHEAD + 1);
                 stage_barrier<FLIGHT>();
                 if constexpr (FP8) {
-                    turn_stage(st + 2, sc);
+                    turn_stage(st + 2);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the raw slot has been read
                 }
                 issue_stage(pd);

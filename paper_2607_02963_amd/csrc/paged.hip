@@ -51,19 +51,26 @@ void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dty
     else launch_f32_types<64>(a, dtype, cache_dtype, grid, s);
 }
 
+namespace {
+
+template <int D, typename T>
+void launch_finish(const PagedArgs& a, hipStream_t s)
+{
+    const int pairs = a.H_kv * a.num_seqs * a.groups, rows = (int)std::min<long>(a.rows, (long)a.max_chunk * a.G);
+    const unsigned x = (unsigned)(a.by_pair ? pairs : a.workers);
+    const dim3 block(64 * kPagedFinishWaves);
+    // eight states or more per pair, if all work-groups have work: a row's waves share them
+    if (pairs <= a.workers / 8) hipLaunchKernelGGL((paged_finish_kernel<D, T, 4>), dim3(x, (unsigned)rows), block, 0, s, a);
+    else hipLaunchKernelGGL((paged_finish_kernel<D, T, 1>), dim3(x, (unsigned)((rows + kPagedFinishWaves - 1) / kPagedFinishWaves)), block, 0, s, a);
+}
+
+}  // namespace
+
 void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t s)
 {
-    const int rows = (int)std::min<long>(a.rows, (long)a.max_chunk * a.G);
-    const dim3 grid((unsigned)(a.by_pair ? a.H_kv * a.num_seqs * a.groups : a.workers),
-                    (unsigned)((rows + kPagedFinishRows - 1) / kPagedFinishRows)),
-        block(64 * kPagedFinishRows);
-    if (head_dim == 128) {
-        if (dtype == PDEC_DTYPE_F32) hipLaunchKernelGGL((paged_finish_kernel<128, float>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((paged_finish_kernel<128, uint16_t>), grid, block, 0, s, a);
-    } else {
-        if (dtype == PDEC_DTYPE_F32) hipLaunchKernelGGL((paged_finish_kernel<64, float>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((paged_finish_kernel<64, uint16_t>), grid, block, 0, s, a);
-    }
+    const bool f32 = dtype == PDEC_DTYPE_F32;
+    if (head_dim == 128) f32 ? launch_finish<128, float>(a, s) : launch_finish<128, uint16_t>(a, s);
+    else f32 ? launch_finish<64, float>(a, s) : launch_finish<64, uint16_t>(a, s);
 }
 
 }  // namespace pdec

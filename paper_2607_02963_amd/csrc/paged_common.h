@@ -21,7 +21,7 @@
 
 namespace pdec {
 
-constexpr int kPagedFinishRows = 4;  // rows per work-group of the finish pass
+constexpr int kPagedFinishWaves = 4;  // waves per work-group of the finish pass
 
 // One launch's arguments.
 struct PagedArgs {
