@@ -76,16 +76,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
     const int lane = tid & 63, l16 = lane & 15, lg = lane >> 4;
     PagedRun run;
     PagedPart part;
-    const int worker = paged_worker(a, blockIdx.x, gridDim.x);
-    if (!paged_begin(a, worker, run)) {
-        if (tid == 0 && !a.whole && !a.by_pair) a.cut[worker] = make_int4(-1, 0, 0, 0);
-        return;
-    }
+    if (!paged_begin(a, paged_worker(a, blockIdx.x), run, tid == 0)) return;
     const float c = a.qscale;
     const long rowb = (long)a.H_kv * D * ESZ;  // bytes of one token's row in a page
 
     while (paged_next(a, run, part, tid == 0)) {
-        const PagedSeq sq = paged_seq(a, part.s);
+        const PagedSeq sq = part.seq;
         const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);
         int seen[NT];  // keys that the lane's row sees; none for rows past the last
         float qv[NT][KPL];

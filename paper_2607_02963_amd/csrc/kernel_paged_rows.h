@@ -77,24 +77,21 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
     constexpr int SCALES = FP8 ? 64 : 0;          // bytes for the 32 scales of a raw slot
     __shared__ __attribute__((aligned(1024))) unsigned char lds[NB * C::STAGE + NW * NRAW * (RAW + SCALES)];
 
-    const int tid = wi_id();
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const float c = a.qscale;
+    const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
     PagedRun run;
     PagedPart part;
-    const int worker = paged_worker(a, wg_id(), (int)__builtin_amdgcn_grid_size_x() / 256);
-    if (!paged_begin(a, worker, run)) {
-        if (tid == 0 && !a.whole && !a.by_pair) a.cut[worker] = make_int4(-1, 0, 0, 0);
-        return;
-    }
+    if (!paged_begin(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
+    __shared__ int find_s[2][2][NW];  // see below; two sets, used in turn
+    int turn_s = 0;
 
-    while (paged_next(a, run, part, tid == 0)) {
+    while (paged_next(a, run, part, w == 0 && paged_lane() == 0)) {
         // The lane's offsets belong to the part: kept over the loop they would take
         // the registers that the pipelined loop needs (the compiler hoists what it can,
         // and spills).
-        int lane = tid & 63;
+        int lane = paged_lane();
         asm volatile("" : "+v"(lane));
         const int l32 = lane & 31, hi = lane >> 5;
+        const float c = a.qscale;
 
         // ---- DMA: this wave moves keys 32 (w % 2) .. + 31 of a unit, of K (w < 2) or V ----
         const bool w_is_v = w >= NW / 2;
@@ -146,12 +143,42 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             return u32x4_t{x0.x, x0.y, x1.x, x1.y};
         };
 
-        const PagedSeq sq = paged_seq(a, part.s);
+        const PagedSeq sq = part.seq;
         const int R = sq.n * a.G, row0 = part.group * C::RT, nrows = min(C::RT, R - row0);
         const int32_t* table = a.block_table + (long)part.s * a.max_pages;
+        // The first page that is there, and the first that is not, among the part's
+        // table entries; every lane looks at every 256th.
+        auto find = [&](int e0, int e1, int& there, int& absent) __attribute__((always_inline)) {
+            int first[2] = {e1, e1};
+            for (int e = e0 + 64 * w; e < e1; e += 64 * NW) {
+                const bool in = e + lane < e1;
+                const bool ok = in && (uint32_t)table[min(e + lane, e1 - 1)] < (uint32_t)a.num_pages;
+                const uint64_t b[2] = {__ballot(ok), __ballot(in && !ok)};
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (b[k] && first[k] == e1) first[k] = e + __builtin_ctzll(b[k]);
+            }
+            if (lane < 2) find_s[turn_s][lane][w] = lane ? first[1] : first[0];
+            lds_barrier();  // also: no wave reads the ring for the part before any more
+            there = absent = e1;
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                there = min(there, __builtin_amdgcn_readfirstlane(find_s[turn_s][0][k]));
+                absent = min(absent, __builtin_amdgcn_readfirstlane(find_s[turn_s][1][k]));
+            }
+            turn_s ^= 1;
+        };
+        const int e1 = min((part.u1 * kUnit - 1) >> a.page_shift, a.max_pages - 1) + 1;
+        int there0, absent0;
+        find(min((part.u0 * kUnit) >> a.page_shift, e1 - 1), e1, there0, absent0);
         // units at the front without a page (a cache that drops its oldest pages) are left out
-        const int u0 = min(paged_find(a, part.s, part.u0, part.u1, true), part.u1);
-        const int nst = part.u1 - u0, t0 = u0 * kUnit;
+        const int u0 = there0 == e1 ? part.u1 : max(part.u0, (there0 << a.page_shift) / kUnit);
+        if (absent0 < there0 && u0 < part.u1) {
+            find(there0, e1, there0, absent0);
+            // the first page may begin inside its unit
+            if ((there0 << a.page_shift) > u0 * kUnit) absent0 = (u0 * kUnit) >> a.page_shift;
+        }
+        const int nst = __builtin_amdgcn_readfirstlane(part.u1 - u0), t0 = __builtin_amdgcn_readfirstlane(u0 * kUnit);
         const int wrow0 = C::WROWS * w;
         const bool active = wrow0 < nrows;
         const uint64_t base0 = pool + (uint64_t)part.head * D * ESZ;
@@ -233,21 +260,20 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         };
 
         // ---- this lane's rows: 32 nt + l % 32 of the wave ----
-        int seen[NT];  // keys that the lane's row sees
         u32x4_t qf[NT][C::KS];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             // rows past the item's last repeat it; their results are not stored
             const int r = row0 + min(wrow0 + 32 * nt + l32, nrows - 1);
-            seen[nt] = paged_seen(a, sq, r / a.G);
             const uint16_t* q = static_cast<const uint16_t*>(a.q) + paged_qrow(a, sq, part.head, r) * D + 8 * hi;
 #pragma unroll
             for (int t = 0; t < C::KS; ++t) qf[nt][t] = *reinterpret_cast<const u32x4_t*>(q + 16 * t);
         }
         const int least = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, (row0 + min(wrow0, nrows - 1)) / a.G));
         // The wave's first nd stages are seen whole by all of its rows.
-        const int nd = !active ? 0 : max(min(paged_find(a, part.s, u0, min(part.u1, least / kUnit), false), least / kUnit) - u0, 0);
-        lds_barrier();  // no wave reads the ring for the part before any more
+        const bool holes = absent0 < e1;
+        const int nd = __builtin_amdgcn_readfirstlane(
+            !active ? 0 : max(min(min(least / kUnit, part.u1), holes ? (absent0 << a.page_shift) / kUnit : part.u1) - u0, 0));
         // Pages of stage st + AHEAD before the barrier of stage st, read one stage ago.
         Pages ahead;
         if (nst > 0) {
@@ -420,6 +446,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 if (st + 1 < nd) rescale(mx);
             }
         }
+        int seen[NT];  // keys that the lane's rows see
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) seen[nt] = paged_seen(a, sq, (row0 + min(wrow0 + 32 * nt + l32, nrows - 1)) / a.G);
         for (int st = nd; st < nst; ++st) {
             {
                 const Pending pd = pending(st + AHEAD, ahead);
@@ -440,7 +469,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
 #pragma unroll 1
             for (int kb = 0; kb < kUnit; kb += 32) {
                 auto there = [&](int x) { return (uint32_t)paged_entry(table, min(x >> a.page_shift, a.max_pages - 1)) < (uint32_t)a.num_pages; };
-                const bool there0 = there(t + kb), there1 = there(t + kb + 16);
+                const bool there0 = !holes || there(t + kb), there1 = !holes || there(t + kb + 16);
                 if (!(there0 | there1) || !__any(most > t + kb)) continue;
                 u32x4_t kf[C::KS], pk[NT][2];
                 u32x2_t vf[4 * C::DT];
@@ -450,10 +479,14 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 for (int i = 0; i < C::KS; ++i) read_k(kf, kbuf, kb, i);
 #pragma unroll
                 for (int j = 0; j < 4 * C::DT; ++j) read_v(vf, vbuf, kb, j);
-                uint32_t odd = 0;
+                typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+                u16x2_t top = {0, 0};  // the largest magnitudes, as their bits
 #pragma unroll
-                for (int j = 0; j < 4 * C::DT; ++j) odd |= strange_bf16x2(vf[j].x) | strange_bf16x2(vf[j].y);
-                const bool apart = __any(odd != 0);
+                for (int j = 0; j < 4 * C::DT; ++j) {
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, vf[j].x & 0x7fff7fffu));
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, vf[j].y & 0x7fff7fffu));
+                }
+                const bool apart = __any(max(top.x, top.y) >= 0x7f80);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const int lim = seen[nt] - t - kb;  // visible keys of the lane's row in the block

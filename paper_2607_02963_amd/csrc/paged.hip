@@ -38,15 +38,9 @@ void launch_f32_types(const PagedArgs& a, int dtype, int cache_dtype, dim3 grid,
 
 }  // namespace
 
-static int paged_grid(const PagedArgs& a)
-{
-    const long pairs = (long)a.H_kv * a.num_seqs * a.groups;
-    return a.whole ? (int)((pairs + 7) / 8 * 8) : a.workers;
-}
-
 void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t s)
 {
-    const dim3 grid((unsigned)paged_grid(a));
+    const dim3 grid((unsigned)a.blocks);
     if (head_dim == 128) launch_f32_types<128>(a, dtype, cache_dtype, grid, s);
     else launch_f32_types<64>(a, dtype, cache_dtype, grid, s);
 }
@@ -119,7 +113,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // The division of one launch's work over `workers` work-groups (paged_common.h),
 // and its workspace bytes; false if its unit count passes 32 bits.
-bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, size_t* bytes)
+bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int pad, size_t* bytes)
 {
     const int64_t R = (int64_t)a.max_chunk * a.G;
     if (R > INT32_MAX / 2) return false;
@@ -127,12 +121,14 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, size
     const int64_t units = (a.max_len + kUnit - 1) / kUnit;
     const int64_t real_groups = (int64_t)d->num_tokens * a.G / a.rows + d->num_seqs;  // at most, over the batch
     const int64_t pairs = (int64_t)d->num_seqs * a.groups * a.H_kv;
-    if (pairs > INT32_MAX / 2 || real_groups * a.H_kv * std::max<int64_t>(units, 1) > INT32_MAX / 2) return false;
+    if (pairs > INT32_MAX / 2 || real_groups * a.H_kv * (units + pad + 1) > INT32_MAX / 2) return false;
     a.workers = workers;
     a.least = least;
+    a.pad = pad;
     // where no pair has more than a work-group's least there is nothing to cut
     a.whole = units <= least ? 1 : 0;
     a.by_pair = pairs <= workers ? 1 : 0;
+    a.blocks = a.whole ? (int)((pairs + 7) / 8 * 8) : workers;
     *bytes = 0;
     if (!a.whole)
         *bytes = align256((size_t)workers * sizeof(int4)) + align256((size_t)2 * workers * a.rows * 2 * sizeof(float)) +
@@ -181,11 +177,11 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
             p.many.rows_from = kFewRows + 1;
             p.few.rows_to = kFewRows;
         }
-        if (!divide(d, p.many, 256, 4, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
+        if (!divide(d, p.many, 256, 4, 6, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     if (p.use_few) {
         p.few.rows = R <= 16 ? 16 : 32;
-        if (!divide(d, p.few, 512, 2, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+        if (!divide(d, p.few, 512, 2, 1, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;
 }
@@ -373,7 +369,7 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
     };
     if (p.use_many) {
         place(p.many, ws + align256(p.few_bytes));
-        launch_paged_rows(p.many, d->head_dim, d->cache_dtype == PDEC_DTYPE_E4M3, paged_grid(p.many), s);
+        launch_paged_rows(p.many, d->head_dim, d->cache_dtype == PDEC_DTYPE_E4M3, s);
         if ((rc = launched()) != PDEC_OK || (rc = finish(p.many)) != PDEC_OK) return rc;
     }
     if (p.use_few) {

@@ -7,6 +7,9 @@
 // one work-group can take, in 64-key units up to the last key that the group's
 // last row sees.  The units of all pairs, one after another (by head, then
 // sequence, then row group), are dealt in equal runs to `workers` work-groups.
+// Heads come first so that neighbours, which share an XCD's cache, read the same
+// keys (by head last, 2048 tokens over 32768 keys took 1140 us for 1084 at 8 kv
+// heads, 992 for 981 at 4).
 // Lengths are known on the device only, and differ: a sequence of 100 keys and
 // one of 30000 in one batch, or the row groups of a causal chunk, still give
 // every work-group the same number of units.  A run is a few whole pairs and
@@ -15,6 +18,8 @@
 // output, all float32) to one of its two slots, and a finish pass joins a cut
 // pair's slots in the order of the work-groups.  So the workspace depends on
 // the number of work-groups only, and repeated calls agree bit for bit.
+// A pair's start has a price beside its units (`pad` units: its queries, an
+// empty ring, the plain loop at its end), which counts in the deal.
 #pragma once
 
 #include "pdec_common.h"
@@ -47,6 +52,8 @@ struct PagedArgs {
     int rows_to;
     int workers;      // work-groups that share the units, a multiple of 8
     int least;        // units per work-group, at least
+    int pad;          // price of a pair's start, in units
+    int blocks;       // work-groups of the launch, a multiple of 8
     int whole;        // 1: work-group i takes pair i whole, nothing is cut
     int by_pair;      // 1: cut[] is indexed by pair, 0: by the work-group a pair begins in
 };
@@ -71,133 +78,158 @@ __device__ inline int paged_seen(const PagedArgs& a, const PagedSeq& x, int i)
     return a.causal ? min(max(x.L - x.n + i + 1, 0), x.L) : x.L;
 }
 
-// Units of pair j = sequence * groups + row group (the same for every head);
-// 0 where there are no such rows, at least 1 where there are.
-__device__ inline int paged_units(const PagedArgs& a, int j)
-{
-    const int s = j / a.groups, row0 = (j - s * a.groups) * a.rows;
-    const PagedSeq x = paged_seq(a, s);
-    const int R = x.n * a.G;
-    if (row0 >= R || R < a.rows_from || R > a.rows_to) return 0;
-    const int last = min(R, row0 + a.rows) - 1;
-    return max(1, (paged_seen(a, x, last / a.G) + kUnit - 1) / kUnit);
-}
-
-// A work-group's place in its run of units.  Uniform over the work-group.
+// A work-group's place in its run.  Positions count every pair's pad and units,
+// the pad first.  Uniform over the work-group.
 struct PagedRun {
     int w;          // its number
-    int head, j;    // the pair at hand
-    int u, units;   // next unit of it, and its units
-    int left;       // units left of the run
-    int pos, per;   // position of the next unit in the list of all, units per work-group
+    int head, s, group;  // the pair at hand: kv head, sequence, row group
+    PagedSeq seq;
+    int u, units;   // next position in it, and its units
+    int left;       // positions left of the run
+    int pos, per;   // next position in the list of all, positions per work-group
 };
 
 // What to do next: units [u0, u1) of a pair.
 struct PagedPart {
     int head, s, group, u0, u1;
+    PagedSeq seq;
     bool whole;     // all of the pair
     int slot;       // where its state goes if not
 };
 
 __device__ inline int paged_lane() { return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
 
-// False if the work-group has nothing to do.  Every wave computes the same.
-__device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r)
+__device__ inline int paged_units_of(const PagedArgs& a, const PagedSeq& x, int group)
+{
+    const int R = x.n * a.G, row0 = group * a.rows;
+    if (row0 >= R || R < a.rows_from || R > a.rows_to) return 0;
+    const int last = min(R, row0 + a.rows) - 1;
+    return max(1, (paged_seen(a, x, last / a.G) + kUnit - 1) / kUnit);
+}
+
+// Units of pair j = sequence * groups + row group (the same for every head);
+// 0 where there are no such rows, at least 1 where there are.
+__device__ inline int paged_units(const PagedArgs& a, int j)
+{
+    const int s = j / a.groups;
+    return paged_units_of(a, paged_seq(a, s), j - s * a.groups);
+}
+
+// False if the work-group has nothing to do.  Every wave computes the same; one
+// lane of the work-group (the caller says which) notes for the finish pass what is cut.
+__device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool note)
 {
     const int J = a.num_seqs * a.groups, lane = paged_lane();
+    if (note && !a.whole && !a.by_pair) a.cut[w] = make_int4(-1, 0, 0, 0);  // unless a pair is cut below
+    int j;
     r.w = w;
+    r.u = 0;
     if (a.whole) {
         if (w >= J * a.H_kv) return false;
         r.head = w / J;
-        r.j = w - r.head * J;
-        r.u = r.pos = 0;
-        r.units = r.left = r.per = __builtin_amdgcn_readfirstlane(paged_units(a, r.j));
-        return r.units > 0;
-    }
-    auto scan = [&](int x) {  // inclusive, over the lanes
+        j = w - r.head * J;
+        r.pos = 0;
+    } else {
+        auto scan = [&](int x) {  // inclusive, over the lanes
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int y = __shfl_up(x, off);
-            if (lane >= off) x += y;
+            for (int off = 1; off < 64; off <<= 1) {
+                const int y = __shfl_up(x, off);
+                if (lane >= off) x += y;
+            }
+            return x;
+        };
+        auto cost = [&](int j) {
+            const int n = j < J ? paged_units(a, j) : 0;
+            return n > 0 ? n + a.pad : 0;
+        };
+        int total = 0, n0 = 0, incl0 = 0;
+        for (int j0 = 0; j0 < J; j0 += 64) {
+            const int n = cost(j0 + lane), incl = scan(n);
+            if (j0 == 0) n0 = n, incl0 = incl;
+            total += __builtin_amdgcn_readlane(incl, 63);
         }
-        return x;
-    };
-    int total = 0, n0 = 0, incl0 = 0;
-    for (int j0 = 0; j0 < J; j0 += 64) {
-        const int n = j0 + lane < J ? paged_units(a, j0 + lane) : 0, incl = scan(n);
-        if (j0 == 0) n0 = n, incl0 = incl;
-        total += __builtin_amdgcn_readlane(incl, 63);
+        r.per = max((total * a.H_kv + a.workers - 1) / a.workers, a.least);
+        r.pos = w * r.per;
+        if (r.pos >= total * a.H_kv) return false;
+        r.left = min(r.per, total * a.H_kv - r.pos);
+        r.head = r.pos / total;
+        int rest = r.pos - r.head * total;
+        for (int j0 = 0;; j0 += 64) {
+            int n = n0, incl = incl0;
+            if (j0 > 0) {
+                n = cost(j0 + lane);
+                incl = scan(n);
+            }
+            const int all = __builtin_amdgcn_readlane(incl, 63);  // scalar, as everything that leaves the loop
+            if (rest >= all) {
+                rest -= all;
+                continue;
+            }
+            const int at = __builtin_ctzll(__ballot(incl > rest));
+            j = j0 + at;
+            rest -= __builtin_amdgcn_readlane(incl - n, at);
+            r.u = rest;
+            break;
+        }
     }
-    r.per = max((total * a.H_kv + a.workers - 1) / a.workers, a.least);
-    r.pos = w * r.per;
-    if (total == 0 || r.pos >= total * a.H_kv) return false;
-    r.left = min(r.per, total * a.H_kv - r.pos);
-    r.head = r.pos / total;
-    int rest = r.pos - r.head * total;
-    for (int j0 = 0;; j0 += 64) {
-        int n = n0, incl = incl0;
-        if (j0 > 0) {
-            n = j0 + lane < J ? paged_units(a, j0 + lane) : 0;
-            incl = scan(n);
-        }
-        const int all = __builtin_amdgcn_readlane(incl, 63);  // scalar, as everything that leaves the loop
-        if (rest >= all) {
-            rest -= all;
-            continue;
-        }
-        const int at = __builtin_ctzll(__ballot(incl > rest));
-        r.j = j0 + at;
-        r.units = __builtin_amdgcn_readlane(n, at);
-        r.u = rest - __builtin_amdgcn_readlane(incl - n, at);
-        break;
-    }
-    return true;
+    r.s = j / a.groups;
+    r.group = j - r.s * a.groups;
+    r.seq = paged_seq(a, r.s);
+    r.units = paged_units_of(a, r.seq, r.group);
+    if (a.whole) r.left = r.per = r.units;
+    return r.units > 0;
 }
 
-// The next part of the run; false at its end.  One lane of the work-group (the
-// caller says which) notes for the finish pass what is cut.
+// The next part of the run; false at its end.
 __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p, bool note)
 {
-    if (r.left <= 0) return false;
-    const int J = a.num_seqs * a.groups;
-    while (r.u >= r.units) {  // units are left, so another pair follows
-        const int s = r.j / a.groups;
-        const PagedSeq x = paged_seq(a, s);
-        const int R = x.n * a.G, g = r.j - s * a.groups + 1;
-        // the sequence's next group, or the next sequence's first
-        r.j = g < a.groups && g * a.rows < R && R >= a.rows_from && R <= a.rows_to ? r.j + 1 : (s + 1) * a.groups;
-        if (r.j >= J) {
-            r.j = 0;
-            ++r.head;
+    const int J = a.num_seqs * a.groups, pad = a.whole ? 0 : a.pad;
+    while (r.left > 0) {
+        while (r.u >= r.units + pad || r.units == 0) {  // positions are left, so another pair follows
+            r.u = 0;
+            ++r.group;
+            if (r.group >= a.groups || (r.units = paged_units_of(a, r.seq, r.group)) == 0) {
+                // the next sequence's first group
+                r.group = 0;
+                if (++r.s >= a.num_seqs) {
+                    r.s = 0;
+                    if (++r.head >= a.H_kv) return false;  // lengths that changed under the call
+                }
+                r.seq = paged_seq(a, r.s);
+                r.units = paged_units_of(a, r.seq, 0);
+            }
         }
-        r.u = 0;
-        r.units = __builtin_amdgcn_readfirstlane(paged_units(a, r.j));
+        const int take = min(r.left, r.units + pad - r.u);
+        // (read as scalars, which the compiler does not conclude by itself)
+        p.u0 = __builtin_amdgcn_readfirstlane(max(r.u - pad, 0));
+        p.u1 = __builtin_amdgcn_readfirstlane(max(r.u + take - pad, 0));
+        p.head = __builtin_amdgcn_readfirstlane(r.head);
+        p.s = __builtin_amdgcn_readfirstlane(r.s);
+        p.group = __builtin_amdgcn_readfirstlane(r.group);
+        p.seq = r.seq;
+        p.whole = p.u0 == 0 && p.u1 == r.units;
+        p.slot = 2 * r.w + (p.u0 == 0 ? 1 : 0);
+        const int end = r.pos - r.u + r.units + pad;  // of the pair
+        r.pos += take;
+        r.left -= take;
+        r.u += take;
+        if (p.u1 == p.u0) continue;  // of the pair's price only
+        if (note && !a.whole && p.u0 == 0) {  // a pair begins here; a cut one is the run's last
+            const int j = r.s * a.groups + r.group;
+            const int4 cut = make_int4(p.whole ? -1 : r.w, (end - 1) / r.per, j, r.head);
+            if (a.by_pair) a.cut[r.head * J + j] = cut;
+            else if (!p.whole) a.cut[r.w] = cut;
+        }
+        return true;
     }
-    p.head = r.head;
-    p.s = r.j / a.groups;
-    p.group = r.j - p.s * a.groups;
-    p.u0 = r.u;
-    p.u1 = min(r.units, r.u + r.left);
-    p.whole = p.u0 == 0 && p.u1 == r.units;
-    p.slot = 2 * r.w + (p.u0 == 0 ? 1 : 0);
-    if (note && !a.whole) {
-        if (p.u0 == 0 && a.by_pair)
-            a.cut[r.head * J + r.j] = make_int4(p.whole ? -1 : r.w, (r.pos + r.units - 1) / r.per, r.j, r.head);
-        if (!a.by_pair && r.left == p.u1 - p.u0)  // the run's last part
-            a.cut[r.w] = make_int4(p.u0 == 0 && !p.whole ? r.w : -1, (r.pos - r.u + r.units - 1) / r.per, r.j, r.head);
-    }
-    r.pos += p.u1 - p.u0;
-    r.left -= p.u1 - p.u0;
-    r.u = p.u1;
-    return true;
+    return false;
 }
 
 // Number of a work-group: block b runs on XCD b % 8, and neighbours in the
-// list, which read the same keys, share an XCD's cache.
-__device__ inline int paged_worker(const PagedArgs& a, int block, int blocks)
-{
-    return (block % 8) * (blocks / 8) + block / 8;
-}
+// list, which read the same keys, share an XCD's cache.  (The number of blocks
+// is an argument: the grid's size stands in the dispatch packet, in host memory,
+// and 256 work-groups that read it start over 13 us.)
+__device__ inline int paged_worker(const PagedArgs& a, int block) { return (block % 8) * (a.blocks / 8) + block / 8; }
 
 // Row of q / out / lse of row r of a pair.
 __device__ inline long paged_qrow(const PagedArgs& a, const PagedSeq& x, int head, int r)
@@ -220,24 +252,11 @@ __device__ inline int paged_page(const PagedArgs& a, int s, int t)
     return (uint32_t)p < (uint32_t)a.num_pages ? p : -1;
 }
 
-// First unit in [u0, u1) of a sequence that has a page (any: some of its
-// keys', not any: lacks one), u1 if there is none.  Uniform over the wave, every lane active.
-__device__ inline int paged_find(const PagedArgs& a, int s, int u0, int u1, bool any)
-{
-    const int lane = paged_lane();
-    for (int t0 = u0 * kUnit; t0 < u1 * kUnit; t0 += 16 * 64) {  // a lane per 16 keys
-        const int t = t0 + 16 * lane;
-        const uint64_t b = __ballot(t < u1 * kUnit && (paged_page(a, s, t) >= 0) == any);
-        if (b) return (t0 + 16 * __builtin_ctzll(b)) / kUnit;
-    }
-    return u1;
-}
-
 // 2^(byte - 127) of byte i of a word; 0 for a byte of 0
 __device__ inline float paged_scale(uint32_t word, int i) { return __uint_as_float(((word >> (8 * i)) & 255u) << 23); }
 
 void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t stream);
-void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, int grid, hipStream_t stream);
+void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, hipStream_t stream);
 void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t stream);
 
 }  // namespace pdec

@@ -10,18 +10,18 @@ namespace pdec {
 namespace {
 
 template <int D, bool FP8>
-void launch_rows(const PagedArgs& a, int grid, hipStream_t s)
+void launch_rows(const PagedArgs& a, hipStream_t s)
 {
-    if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<D, 2, FP8>), dim3((unsigned)grid), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<D, 2, FP8>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
-void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, int grid, hipStream_t s)
+void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
 {
-    if (head_dim == 128) fp8 ? launch_rows<128, true>(a, grid, s) : launch_rows<128, false>(a, grid, s);
-    else fp8 ? launch_rows<64, true>(a, grid, s) : launch_rows<64, false>(a, grid, s);
+    if (head_dim == 128) fp8 ? launch_rows<128, true>(a, s) : launch_rows<128, false>(a, s);
+    else fp8 ? launch_rows<64, true>(a, s) : launch_rows<64, false>(a, s);
 }
 
 }  // namespace pdec
