@@ -45,7 +45,6 @@ struct PagedRaw {
     __device__ inline float get(int i) const
     {
         if constexpr (sizeof(TC) == 4) return __uint_as_float(w[i]);
-        else if constexpr (sizeof(TC) == 2) return __uint_as_float((i & 1) ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
         else {
             const f32x2_t x = (i & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i >> 2], true)
                                       : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i >> 2], false);
@@ -59,7 +58,7 @@ __device__ inline f32x4_t paged_mfma4(float a, float b, f32x4_t c)
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <int D, int NT, typename TQ, typename TC>
+template <int D, int NT, typename TC>
 __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedArgs a)
 {
     constexpr int NW = 4, RT = 16 * NT;
@@ -89,8 +88,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
         for (int nt = 0; nt < NT; ++nt) {
             const int r = 16 * nt + l16, rr = row0 + min(r, nrows - 1);
             seen[nt] = r < nrows ? paged_seen(a, sq, rr / a.G) : 0;
-            PagedRaw<TQ, KPL> x;
-            x.load(static_cast<const unsigned char*>(a.q) + (paged_qrow(a, sq, part.head, rr) * D + KPL * lg) * (int)sizeof(TQ));
+            PagedRaw<float, KPL> x;
+            x.load(static_cast<const unsigned char*>(a.q) + (paged_qrow(a, sq, part.head, rr) * D + KPL * lg) * 4);
 #pragma unroll
             for (int j = 0; j < KPL; ++j) qv[nt][j] = x.get(j);
         }
@@ -267,10 +266,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
             const long qr = paged_qrow(a, sq, part.head, row0 + r);
             const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
             acc *= inv;
-            if constexpr (sizeof(TQ) == 4) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + qr * D + 4 * d4) = acc;
-            else
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + qr * D + 4 * d4) =
-                    make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+            *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + qr * D + 4 * d4) = acc;
             if (d4 == 0 && a.lse) a.lse[qr] = L > 0.f || L != L ? kLn2 * (M + log2f(L)) : kNegInf;
         }
     }

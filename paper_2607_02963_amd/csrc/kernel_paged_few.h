@@ -1,0 +1,378 @@
+// Attention over paged caches, few query rows per kv head (single tokens,
+// drafted tokens, short chunks), bfloat16, on v_mfma_f32_16x16x32_bf16.
+//
+// What bounds it: the bytes of the pages.  A key meets 16 NT rows at most, so
+// nothing is shared between waves: each of a work-group's four waves takes every
+// fourth 32-key block of the part through a ring of its own in LDS (32 KB,
+// filled by global_load_lds_dwordx4), with a softmax state of its own, and never
+// waits for another wave until the four states are joined at the part's end.
+// A block's 16-key halves are each on one page: a scalar base and fixed lane
+// offsets per half, the pages of the block after the ring's read one block ahead.
+// 128 KB in flight per compute unit is more than the latency of the memory asks.
+//
+// Per block, products and layouts as in the decode step (kernel_mfma.h):
+//   S^T  = K  Q^T    A = 16 keys x 32 d from LDS, B = Q^T (registers)
+//   O^T += V^T P^T   A = V^T by a transposing LDS read, B = P^T (registers)
+// Rows are permuted 16 bytes at a time in LDS so that the reads of one phase
+// meet different banks.
+//
+// 8-bit pages stay 8 bits in LDS, and their operands are widened in registers:
+// each is used by one wave only, so once each.  A lane's 16 bytes of a key row
+// are the operands of two steps (the contraction over d is taken in that order,
+// Q's too); ds_read_b64_tr_b8 gives 8 keys of one d.  A key's power of two
+// multiplies its scores, a value's its probability before that is rounded.
+#pragma once
+
+#include "kernel_paged_rows.h"
+
+namespace pdec {
+
+// 16-byte chunk permutations of the rows in LDS: chunk ch of key k sits at ch ^ swizzle(k).
+template <int D, bool FP8>
+__device__ inline int few_kswz(int key)
+{
+    if constexpr (FP8) return D == 128 ? (key & 7) : ((key >> 1) & 3);
+    return key & (D / 8 - 1);
+}
+template <int D, bool FP8>
+__device__ inline int few_vswz(int key)
+{
+    // 8-bit: a phase of the transposing read is keys 4 q .. + 3 and 16 + 4 q .. + 3
+    if constexpr (FP8) return D == 128 ? ((key & 3) | ((key >> 2) & 4)) : (((key >> 1) & 1) | ((key >> 3) & 2));
+    return (2 * key) & (D == 128 ? 14 : 6);
+}
+
+// Eight e4m3 values as bf16
+__device__ inline u32x4_t widen8(uint32_t lo, uint32_t hi)
+{
+    u32x4_t r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+    return r;
+}
+
+template <int D, int NT, bool FP8>
+__global__ __launch_bounds__(256) void paged_few_kernel(PagedArgs a)
+{
+    constexpr int NW = 4, RT = 16 * NT;
+    constexpr int ESZ = FP8 ? 1 : 2, ROWB = D * ESZ;
+    constexpr int KB = 32;                       // keys per block
+    constexpr int TENSOR = KB * ROWB, SLOT = 2 * TENSOR;
+    constexpr int NS = 32768 / SLOT;             // ring slots of a wave
+    constexpr int CPK = ROWB / 16;               // 16-byte chunks per key
+    constexpr int KPI = 64 / CPK;                // keys per DMA instruction
+    constexpr int PPH = 16 / KPI;                // instructions per half of a tensor
+    constexpr int PB = 4 * PPH + (FP8 ? 1 : 0);  // and per block, its scales with them
+    constexpr int KS = D / 32, DT = D / 16;
+    constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
+    constexpr int MT = NT < 2 ? NT : 2;          // tiles merged at a time
+    static_assert((NS - 1) * PB < 64, "the wait counts them");
+    static_assert(NW * 16 * MT * OROW * 4 <= NW * 32768, "merge buffer");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * 32768 + (FP8 ? NW * NS * 64 : 0)];
+    __shared__ float m_s[NW][16 * MT], l_s[NW][16 * MT];
+
+    const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
+    const int lane = paged_lane(), l16 = lane & 15, lg = lane >> 4;
+    PagedRun run;
+    PagedPart part;
+    if (!paged_begin(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
+
+    const float c = a.qscale;
+    const uint32_t strideB = (uint32_t)a.H_kv * ROWB;
+    const uint32_t ring = lds_u32(lds) + w * 32768, sc_ring = lds_u32(lds) + NW * 32768 + w * NS * 64;
+    // byte offset of the lane's chunk in piece i of half h of a tensor
+    uint32_t koffs[2][PPH], voffs[2][PPH];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < PPH; ++i) {
+            const int k = i * KPI + lane / CPK, key = 16 * h + k;
+            koffs[h][i] = (uint32_t)k * strideB + 16 * ((lane % CPK) ^ few_kswz<D, FP8>(key));
+            voffs[h][i] = (uint32_t)k * strideB + 16 * ((lane % CPK) ^ few_vswz<D, FP8>(key));
+        }
+    // operand reads, relative to a slot
+    uint32_t kread[FP8 ? KS / 2 : KS], vread[DT];
+#pragma unroll
+    for (int t = 0; t < (FP8 ? KS / 2 : KS); ++t) kread[t] = l16 * ROWB + 16 * ((4 * t + lg) ^ few_kswz<D, FP8>(l16));
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        if constexpr (FP8) {
+            const int j = l16 >> 1, key = (j < 4 ? 0 : 12) + 4 * lg + j;
+            vread[dt] = TENSOR + key * ROWB + 16 * (dt ^ few_vswz<D, FP8>(key)) + 8 * (l16 & 1);
+        } else {
+            const int key = 4 * lg + (l16 >> 2);
+            vread[dt] = TENSOR + key * ROWB + 16 * ((2 * dt + ((l16 & 3) >> 1)) ^ few_vswz<D, FP8>(key)) + 8 * (l16 & 1);
+        }
+    }
+    typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
+    typedef __attribute__((address_space(3))) const uint32_t lds_u32_t;
+
+    while (paged_next(a, run, part, w == 0 && lane == 0)) {
+        const PagedSeq sq = part.seq;
+        const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);
+        const int tiles = (nrows + 15) / 16;
+        const int nb = 2 * (part.u1 - part.u0), mine = nb > w ? (nb - w + NW - 1) / NW : 0;  // blocks: of the part, of the wave
+        const int t0 = part.u0 * kUnit;
+        const int32_t* table = a.block_table + (long)part.s * a.max_pages;
+        const uint64_t kbase = sgpr_base(a.k_pages) + (uint64_t)part.head * ROWB, vbase = sgpr_base(a.v_pages) + (uint64_t)part.head * ROWB;
+
+        // the wave's block b: its first key, and its halves' pages
+        auto first = [&](int b) __attribute__((always_inline)) { return t0 + KB * (w + NW * b); };
+        struct Pages { int half[2]; };
+        auto pages = [&](int b) __attribute__((always_inline)) {
+            Pages x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x.half[h] = paged_entry(table, min((first(b) + 16 * h) >> a.page_shift, a.max_pages - 1));
+            return x;
+        };
+        auto there = [&](const Pages& x, int h) __attribute__((always_inline)) { return (uint32_t)x.half[h] < (uint32_t)a.num_pages; };
+        // blocks past the last are pieces of one lane, so that every wait counts the same
+        // (ring.h); an absent page is read as page 0, and its keys masked
+        auto issue = [&](int b, const Pages& x) __attribute__((always_inline)) {
+            const uint64_t lanes = b < mine ? ~0ull : 1ull;
+            const uint32_t dst = ring + (b % NS) * SLOT;
+            uint64_t ksc[2], vsc[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int page = there(x, h) && b < mine ? x.half[h] : 0;
+                const int row = (first(b) + 16 * h) & ((1 << a.page_shift) - 1);
+                const uint64_t at = (((uint64_t)(uint32_t)page << a.page_shift) + (uint32_t)row) * strideB;
+#pragma unroll
+                for (int i = 0; i < PPH; ++i) {
+                    dma_16B_page(kbase + at, koffs[h][i], dst + 1024 * (h * PPH + i), lanes);
+                    dma_16B_page(vbase + at, voffs[h][i], dst + TENSOR + 1024 * (h * PPH + i), lanes);
+                }
+                if constexpr (FP8) {
+                    const uint64_t sc = (((uint64_t)(uint32_t)page * a.H_kv + part.head) << a.page_shift) + (uint32_t)row;
+                    ksc[h] = sgpr_base(a.k_scales) + sc;
+                    vsc[h] = sgpr_base(a.v_scales) + sc;
+                }
+            }
+            if constexpr (FP8) {  // 16 bytes each of K's halves, then of V's, four lanes to a half
+                const uint64_t from = lane & 8 ? (lane & 4 ? vsc[1] : vsc[0]) : (lane & 4 ? ksc[1] : ksc[0]);
+                dma_4B_lanes(from + 4 * (lane & 3), sc_ring + (b % NS) * 64, lanes & 0xffffu);
+            }
+        };
+
+        // ---- this lane's rows: 16 nt + l % 16; those past the last see nothing ----
+        int seen[NT];
+        u32x4_t qf[NT][KS];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = 16 * nt + l16, rr = row0 + min(r, nrows - 1);
+            seen[nt] = r < nrows ? paged_seen(a, sq, rr / a.G) : 0;
+            const uint16_t* q = static_cast<const uint16_t*>(a.q) + paged_qrow(a, sq, part.head, rr) * D;
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+                qf[nt][t] = *reinterpret_cast<const u32x4_t*>(q + (FP8 ? 64 * (t / 2) + 16 * lg + 8 * (t & 1) : 32 * t + 8 * lg));
+        }
+        // keys that every row sees (rows past the last are masked or not, their results are not stored)
+        const int least = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, row0 / a.G));
+        const int most = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, (row0 + nrows - 1) / a.G));
+#pragma unroll
+        for (int b = 0; b < NS; ++b)
+            if (mine > 0) issue(b, pages(min(b, mine - 1)));
+        Pages ahead = pages(min(NS, max(mine - 1, 0)));
+        Pages now = pages(0);
+
+        f32x4_t o[NT][DT];
+        float m_ref[NT], lsum[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m_ref[nt] = kMinRef;
+            lsum[nt] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        // the query loads and the DMA complete in no order relative to each other
+        wait_vmcnt<0>();
+
+        for (int b = 0; b < mine; ++b) {
+            wave_wait_vmcnt<(NS - 1) * PB>();  // block b has landed
+            const uint32_t slot = ring + (b % NS) * SLOT;
+            const int t = first(b);
+            const bool there0 = there(now, 0), there1 = there(now, 1);
+            if ((there0 | there1) && t < most) {
+                u32x4_t kf[2][KS], vf[DT];
+                uint32_t ks[2], vs[2];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    if constexpr (FP8) {
+#pragma unroll
+                        for (int u = 0; u < KS / 2; ++u) {
+                            const u32x4_t x = *(lds_u32x4_t*)(uintptr_t)(slot + kread[u] + 16 * kt * ROWB);
+                            kf[kt][2 * u] = widen8(x[0], x[1]);
+                            kf[kt][2 * u + 1] = widen8(x[2], x[3]);
+                        }
+                        ks[kt] = *(lds_u32_t*)(uintptr_t)(sc_ring + (b % NS) * 64 + 16 * kt + 4 * lg);
+                        vs[kt] = *(lds_u32_t*)(uintptr_t)(sc_ring + (b % NS) * 64 + 32 + 16 * kt + 4 * lg);
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < KS; ++s) kf[kt][s] = *(lds_u32x4_t*)(uintptr_t)(slot + kread[s] + 16 * kt * ROWB);
+                    }
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    if constexpr (FP8) {
+                        typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+                        const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)(uintptr_t)(slot + vread[dt]));
+                        vf[dt] = widen8((uint32_t)x.x, (uint32_t)x.y);
+                    } else {
+                        typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+                        const u32x2_t x0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)(slot + vread[dt])));
+                        const u32x2_t x1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)(slot + vread[dt] + 16 * ROWB)));
+                        vf[dt] = u32x4_t{x0.x, x0.y, x1.x, x1.y};
+                    }
+                }
+                const bool full = t + KB <= least && there0 && there1;
+                // 0 times an infinite or NaN value is NaN: where a key is hidden from a row,
+                // such values are left out of the products, then added key by key to the rows
+                // that see the key
+                bool apart = false;
+                if (!full) {
+                    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+                    u16x2_t top = {0, 0};  // the largest magnitudes, as their bits
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, vf[dt][e] & 0x7fff7fffu));
+                    apart = __any(max(top.x, top.y) >= 0x7f80);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (nt >= tiles) break;
+                    f32x4_t s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                    for (int i = 0; i < KS; ++i)
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt) s[kt] = mfma_16x16x32(as_bf16x8(kf[kt][i]), as_bf16x8(qf[nt][i]), s[kt]);
+                    float p[8], vp[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        p[i] = s[i >> 2][i & 3];
+                        if constexpr (FP8) p[i] *= paged_scale(ks[i >> 2], i & 3);
+                    }
+                    if (!full) {
+                        const int lim = seen[nt] - t - 4 * lg;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            p[i] = ((16 * (i >> 2) + (i & 3) >= lim) | !(i < 4 ? there0 : there1)) ? kNegInf : p[i];
+                    }
+                    float mx = p[0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[i]);
+                    if (__any(mx * c > m_ref[nt] + 8.f)) {  // rare after a row's first keys
+                        const float mt = max_over_groups(mx) * c;
+                        const bool up = mt > m_ref[nt] + 8.f;
+                        const float alpha = up ? fast_exp2(m_ref[nt] - mt) : 1.f;
+                        m_ref[nt] = up ? mt : m_ref[nt];
+                        lsum[nt] *= alpha;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        p[i] = fast_exp2(fmaf(p[i], c, -m_ref[nt]));  // 0 for a hidden key
+                        vp[i] = p[i];
+                        // (a hidden key's scale may be anything, 0 times infinity among it)
+                        if constexpr (FP8) vp[i] = full || p[i] > 0.f ? p[i] * paged_scale(vs[i >> 2], i & 3) : p[i];
+                    }
+                    // the row sums take P unrounded, the product rounded to bf16
+                    lsum[nt] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                    const bf16x8_t pf = as_bf16x8(u32x4_t{pack_bf16x2(vp[0], vp[1]), pack_bf16x2(vp[2], vp[3]),
+                                                          pack_bf16x2(vp[4], vp[5]), pack_bf16x2(vp[6], vp[7])});
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        u32x4_t v = vf[dt];
+                        if (apart) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] &= ~strange_bf16x2(v[e]);
+                        }
+                        o[nt][dt] = mfma_16x16x32(as_bf16x8(v), pf, o[nt][dt]);
+                    }
+                    if (!apart) continue;
+#pragma unroll 1
+                    for (int key = 0; key < KB; ++key) {
+                        const int x = key & 15;
+                        const bool sees = (t + key < seen[nt]) & (key < 16 ? there0 : there1);
+                        const bool mine_k = lg == (x >> 2);
+                        const int word = 2 * (key >> 4) + ((x & 3) >> 1);
+                        const uint32_t half = (x & 1) ? 0xffff0000u : 0xffffu;
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            u32x4_t v = vf[dt];
+                            asm volatile("" : "+v"(v));  // nothing of this rare loop before it
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] &= strange_bf16x2(v[e]) & ((mine_k & (e == word)) ? half : 0u);
+                            const f32x4_t y = mfma_16x16x32(as_bf16x8(v), pf, o[nt][dt]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[nt][dt][i] = sees ? y[i] : o[nt][dt][i];
+                        }
+                    }
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+            issue(b + NS, ahead);
+            ahead = pages(min(b + NS + 1, mine - 1));
+            now = pages(min(b + 1, mine - 1));
+        }
+
+        // ---- the four waves' states joined; lane: row l % 16 of tile nt, d = 16 dt + 4 (l / 16) + i ----
+        wait_vmcnt<0>();  // no DMA into the ring outlives the part
+        float* const o_s = reinterpret_cast<float*>(lds);
+#pragma unroll
+        for (int n0 = 0; n0 < NT; n0 += MT) {
+            if (n0 >= tiles) break;
+            lds_barrier();  // the ring, or the tiles before, have been read
+#pragma unroll
+            for (int k = 0; k < MT; ++k) {
+                const int nt = n0 + k, r = 16 * k + l16;
+                float l = lsum[nt];
+                l += __shfl_xor(l, 16);
+                l += __shfl_xor(l, 32);
+                if (lg == 0) {
+                    m_s[w][r] = m_ref[nt];
+                    l_s[w][r] = l;
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+                    *reinterpret_cast<f32x4_t*>(o_s + (w * 16 * MT + r) * OROW + 16 * dt + 4 * lg) = o[nt][dt];
+            }
+            lds_barrier();
+            const int rows = min(nrows - 16 * n0, 16 * MT);
+            for (int i = 64 * w + lane; i < rows * (D / 4); i += 256) {
+                const int r = i / (D / 4), d4 = i % (D / 4);
+                float M = m_s[0][r];
+#pragma unroll
+                for (int x = 1; x < NW; ++x) M = fmaxf(M, m_s[x][r]);
+                float L = 0.f;
+                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < NW; ++x) {
+                    const float f = fast_exp2(m_s[x][r] - M);  // 0 for a wave that saw none of the row's keys
+                    L += f * l_s[x][r];
+                    acc += f * *reinterpret_cast<const f32x4_t*>(o_s + (x * 16 * MT + r) * OROW + 4 * d4);
+                }
+                const int row = 16 * n0 + r;
+                if (!part.whole) {
+                    const long at = (long)part.slot * RT + row;
+                    *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 4 * d4) = acc;
+                    if (d4 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(M, L);
+                    continue;
+                }
+                const long qr = paged_qrow(a, sq, part.head, row0 + row);
+                const bool any = __float_as_uint(L) != 0;  // L is 0, positive or NaN
+                const float inv = any ? 1.f / L : 0.f;
+                acc *= inv;
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + qr * D + 4 * d4) =
+                    make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+                if (d4 == 0 && a.lse) a.lse[qr] = any ? kLn2 * (M + __log2f(L)) : kNegInf;
+            }
+        }
+        lds_barrier();  // the states have been read: the next part's DMA may come
+    }
+}
+
+}  // namespace pdec

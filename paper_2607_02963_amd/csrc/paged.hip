@@ -17,32 +17,20 @@ namespace pdec {
 
 namespace {
 
-template <int D, typename TQ, typename TC>
-void launch_f32_rows(const PagedArgs& a, dim3 grid, hipStream_t s)
+template <int D, typename TC>
+void launch_f32_rows(const PagedArgs& a, hipStream_t s)
 {
-    if (a.rows == 16) hipLaunchKernelGGL((paged_f32_kernel<D, 1, TQ, TC>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_f32_kernel<D, 2, TQ, TC>), grid, dim3(256), 0, s, a);
-}
-
-template <int D>
-void launch_f32_types(const PagedArgs& a, int dtype, int cache_dtype, dim3 grid, hipStream_t s)
-{
-    if (dtype == PDEC_DTYPE_F32) {
-        if (cache_dtype == PDEC_DTYPE_F32) launch_f32_rows<D, float, float>(a, grid, s);
-        else launch_f32_rows<D, float, fp8_t>(a, grid, s);
-    } else {
-        if (cache_dtype == PDEC_DTYPE_BF16) launch_f32_rows<D, uint16_t, uint16_t>(a, grid, s);
-        else launch_f32_rows<D, uint16_t, fp8_t>(a, grid, s);
-    }
+    const dim3 grid((unsigned)a.blocks), block(256);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_f32_kernel<D, 1, TC>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_f32_kernel<D, 2, TC>), grid, block, 0, s, a);
 }
 
 }  // namespace
 
-void launch_paged_f32(const PagedArgs& a, int head_dim, int dtype, int cache_dtype, hipStream_t s)
+void launch_paged_f32(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.blocks);
-    if (head_dim == 128) launch_f32_types<128>(a, dtype, cache_dtype, grid, s);
-    else launch_f32_types<64>(a, dtype, cache_dtype, grid, s);
+    if (head_dim == 128) fp8 ? launch_f32_rows<128, fp8_t>(a, s) : launch_f32_rows<128, float>(a, s);
+    else fp8 ? launch_f32_rows<64, fp8_t>(a, s) : launch_f32_rows<64, float>(a, s);
 }
 
 namespace {
@@ -180,8 +168,10 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         if (!divide(d, p.many, 256, 4, 6, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     if (p.use_few) {
-        p.few.rows = R <= 16 ? 16 : 32;
-        if (!divide(d, p.few, 512, 2, 1, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+        const int64_t most = std::min<int64_t>(R, p.few.rows_to);
+        const bool f32 = d->dtype == PDEC_DTYPE_F32;
+        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : 64;
+        if (!divide(d, p.few, f32 ? 512 : 256, 2, 1, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;
 }
@@ -374,7 +364,9 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
     }
     if (p.use_few) {
         place(p.few, ws);
-        launch_paged_f32(p.few, d->head_dim, d->dtype, d->cache_dtype, s);
+        const bool fp8 = d->cache_dtype == PDEC_DTYPE_E4M3;
+        if (d->dtype == PDEC_DTYPE_F32) launch_paged_f32(p.few, d->head_dim, fp8, s);
+        else launch_paged_few(p.few, d->head_dim, fp8, s);
         if ((rc = launched()) != PDEC_OK || (rc = finish(p.few)) != PDEC_OK) return rc;
     }
     return PDEC_OK;

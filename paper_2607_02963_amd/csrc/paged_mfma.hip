@@ -3,6 +3,7 @@
 // clear and without NaN semantics.
 #include <hip/hip_runtime.h>
 
+#include "kernel_paged_few.h"
 #include "kernel_paged_rows.h"
 
 namespace pdec {
@@ -16,7 +17,22 @@ void launch_rows(const PagedArgs& a, hipStream_t s)
     else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
 }
 
+template <int D, bool FP8>
+void launch_few(const PagedArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)a.blocks), block(256);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8>), grid, block, 0, s, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8>), grid, block, 0, s, a);
+}
+
 }  // namespace
+
+void launch_paged_few(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
+{
+    if (head_dim == 128) fp8 ? launch_few<128, true>(a, s) : launch_few<128, false>(a, s);
+    else fp8 ? launch_few<64, true>(a, s) : launch_few<64, false>(a, s);
+}
 
 void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
 {

@@ -88,6 +88,8 @@ class Paged:
             x[~live] = junk
             if self.cache == "e4m3":
                 bits, byte = quantise(x)
+                if junk != 0:  # nor have the scales of those rows a meaning
+                    byte[~live] = 255
                 self.raw[name], self.scales[name] = bits, np.ascontiguousarray(byte.transpose(0, 2, 1))
                 self.vals[name] = e4m3_values(bits) * 2.0 ** (byte.astype(np.float64) - 127)[..., None]
             else:
