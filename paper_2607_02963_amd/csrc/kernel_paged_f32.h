@@ -79,7 +79,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
     const float c = a.qscale;
     const long rowb = (long)a.H_kv * D * ESZ;  // bytes of one token's row in a page
 
-    while (paged_next(a, run, part, tid == 0)) {
+    while (paged_next(a, run, part)) {
+        if (tid == 0) paged_note(a, run, part);
         const PagedSeq sq = part.seq;
         const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);
         int seen[NT];  // keys that the lane's row sees; none for rows past the last

@@ -53,24 +53,25 @@ __device__ inline u32x4_t widen8(uint32_t lo, uint32_t hi)
     return r;
 }
 
-template <int D, int NT, bool FP8>
-__global__ __launch_bounds__(256) void paged_few_kernel(PagedArgs a)
+template <int D, int NT, bool FP8, int NW>
+__global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
 {
-    constexpr int NW = 4, RT = 16 * NT;
+    constexpr int RT = 16 * NT;
+    constexpr int RING = 131072 / NW;            // bytes of a wave's ring
     constexpr int ESZ = FP8 ? 1 : 2, ROWB = D * ESZ;
     constexpr int KB = 32;                       // keys per block
     constexpr int TENSOR = KB * ROWB, SLOT = 2 * TENSOR;
-    constexpr int NS = 32768 / SLOT;             // ring slots of a wave
+    constexpr int NS = RING / SLOT;              // ring slots of a wave
     constexpr int CPK = ROWB / 16;               // 16-byte chunks per key
     constexpr int KPI = 64 / CPK;                // keys per DMA instruction
     constexpr int PPH = 16 / KPI;                // instructions per half of a tensor
     constexpr int PB = 4 * PPH + (FP8 ? 1 : 0);  // and per block, its scales with them
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
-    constexpr int MT = NT < 2 ? NT : 2;          // tiles merged at a time
+    constexpr int MT = NT < 2 || NW == 8 ? 1 : 2;  // tiles merged at a time
     static_assert((NS - 1) * PB < 64, "the wait counts them");
-    static_assert(NW * 16 * MT * OROW * 4 <= NW * 32768, "merge buffer");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * 32768 + (FP8 ? NW * NS * 64 : 0)];
+    static_assert(NW * 16 * MT * OROW * 4 <= NW * RING, "merge buffer");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + (FP8 ? NW * NS * 64 : 0)];
     __shared__ float m_s[NW][16 * MT], l_s[NW][16 * MT];
 
     const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256) void paged_few_kernel(PagedArgs a)
 
     const float c = a.qscale;
     const uint32_t strideB = (uint32_t)a.H_kv * ROWB;
-    const uint32_t ring = lds_u32(lds) + w * 32768, sc_ring = lds_u32(lds) + NW * 32768 + w * NS * 64;
+    const uint32_t ring = lds_u32(lds) + w * RING, sc_ring = lds_u32(lds) + NW * RING + w * NS * 64;
     // byte offset of the lane's chunk in piece i of half h of a tensor
     uint32_t koffs[2][PPH], voffs[2][PPH];
 #pragma unroll
@@ -109,7 +110,8 @@ __global__ __launch_bounds__(256) void paged_few_kernel(PagedArgs a)
     typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
     typedef __attribute__((address_space(3))) const uint32_t lds_u32_t;
 
-    while (paged_next(a, run, part, w == 0 && lane == 0)) {
+    while (paged_next(a, run, part)) {
+        if (w == 0 && lane == 0) paged_note(a, run, part);
         const PagedSeq sq = part.seq;
         const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);
         const int tiles = (nrows + 15) / 16;
@@ -342,7 +344,7 @@ __global__ __launch_bounds__(256) void paged_few_kernel(PagedArgs a)
             }
             lds_barrier();
             const int rows = min(nrows - 16 * n0, 16 * MT);
-            for (int i = 64 * w + lane; i < rows * (D / 4); i += 256) {
+            for (int i = 64 * w + lane; i < rows * (D / 4); i += 64 * NW) {
                 const int r = i / (D / 4), d4 = i % (D / 4);
                 float M = m_s[0][r];
 #pragma unroll

@@ -84,7 +84,8 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
     __shared__ int find_s[2][2][NW];  // see below; two sets, used in turn
     int turn_s = 0;
 
-    while (paged_next(a, run, part, w == 0 && paged_lane() == 0)) {
+    while (paged_next(a, run, part)) {
+        if (w == 0 && paged_lane() == 0) paged_note(a, run, part);
         // The lane's offsets belong to the part: kept over the loop they would take
         // the registers that the pipelined loop needs (the compiler hoists what it can,
         // and spills).

@@ -95,6 +95,7 @@ struct PagedPart {
     PagedSeq seq;
     bool whole;     // all of the pair
     int slot;       // where its state goes if not
+    int end;        // position behind the pair
 };
 
 __device__ inline int paged_lane() { return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
@@ -180,10 +181,11 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
     return r.units > 0;
 }
 
-// The next part of the run; false at its end.
-__device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p, bool note)
+// The next part of the run; false at its end.  (No branch here is by the lane:
+// one inside the loop would make everything that leaves it a vector value.)
+__device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
 {
-    const int J = a.num_seqs * a.groups, pad = a.whole ? 0 : a.pad;
+    const int pad = a.whole ? 0 : a.pad;
     while (r.left > 0) {
         while (r.u >= r.units + pad || r.units == 0) {  // positions are left, so another pair follows
             r.u = 0;
@@ -200,29 +202,32 @@ __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p,
             }
         }
         const int take = min(r.left, r.units + pad - r.u);
-        // (read as scalars, which the compiler does not conclude by itself)
-        p.u0 = __builtin_amdgcn_readfirstlane(max(r.u - pad, 0));
-        p.u1 = __builtin_amdgcn_readfirstlane(max(r.u + take - pad, 0));
-        p.head = __builtin_amdgcn_readfirstlane(r.head);
-        p.s = __builtin_amdgcn_readfirstlane(r.s);
-        p.group = __builtin_amdgcn_readfirstlane(r.group);
+        p.u0 = max(r.u - pad, 0);
+        p.u1 = max(r.u + take - pad, 0);
+        p.head = r.head;
+        p.s = r.s;
+        p.group = r.group;
         p.seq = r.seq;
         p.whole = p.u0 == 0 && p.u1 == r.units;
         p.slot = 2 * r.w + (p.u0 == 0 ? 1 : 0);
-        const int end = r.pos - r.u + r.units + pad;  // of the pair
+        p.end = r.pos - r.u + r.units + pad;
         r.pos += take;
         r.left -= take;
         r.u += take;
-        if (p.u1 == p.u0) continue;  // of the pair's price only
-        if (note && !a.whole && p.u0 == 0) {  // a pair begins here; a cut one is the run's last
-            const int j = r.s * a.groups + r.group;
-            const int4 cut = make_int4(p.whole ? -1 : r.w, (end - 1) / r.per, j, r.head);
-            if (a.by_pair) a.cut[r.head * J + j] = cut;
-            else if (!p.whole) a.cut[r.w] = cut;
-        }
-        return true;
+        if (p.u1 > p.u0) return true;  // else of the pair's price only
     }
     return false;
+}
+
+// One lane of the work-group notes for the finish pass whether a pair that begins
+// with this part is cut.
+__device__ inline void paged_note(const PagedArgs& a, const PagedRun& r, const PagedPart& p)
+{
+    if (a.whole || p.u0 > 0) return;
+    const int j = p.s * a.groups + p.group;
+    const int4 cut = make_int4(p.whole ? -1 : r.w, (p.end - 1) / r.per, j, p.head);
+    if (a.by_pair) a.cut[p.head * a.num_seqs * a.groups + j] = cut;
+    else if (!p.whole) a.cut[r.w] = cut;
 }
 
 // Number of a work-group: block b runs on XCD b % 8, and neighbours in the

@@ -20,10 +20,10 @@ void launch_rows(const PagedArgs& a, hipStream_t s)
 template <int D, bool FP8>
 void launch_few(const PagedArgs& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.blocks), block(256);
-    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8>), grid, block, 0, s, a);
-    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8>), grid, block, 0, s, a);
+    const dim3 grid((unsigned)a.blocks);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8, 8>), grid, dim3(512), 0, s, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8, 8>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, 4>), grid, dim3(256), 0, s, a);
 }
 
 }  // namespace
