@@ -99,6 +99,10 @@ struct AttnPlan {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Where no pair has more units than this nothing is cut, a work-group takes a pair
+// and there is no finish pass: one token over 250 keys 10.9 us, cut 13.8.
+constexpr int kWholeUnits = 4;
+
 // The division of one launch's work over `workers` work-groups (paged_common.h),
 // and its workspace bytes; false if its unit count passes 32 bits.
 bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int pad, size_t* bytes)
@@ -113,8 +117,7 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int 
     a.workers = workers;
     a.least = least;
     a.pad = pad;
-    // where no pair has more than a work-group's least there is nothing to cut
-    a.whole = units <= least ? 1 : 0;
+    a.whole = units <= kWholeUnits ? 1 : 0;
     a.by_pair = pairs <= workers ? 1 : 0;
     a.blocks = a.whole ? (int)((pairs + 7) / 8 * 8) : workers;
     *bytes = 0;
@@ -171,7 +174,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
         const bool f32 = d->dtype == PDEC_DTYPE_F32;
         p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : 64;
-        if (!divide(d, p.few, f32 ? 512 : 256, 2, 1, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+        if (!divide(d, p.few, f32 ? 512 : 256, 2, f32 ? 1 : 4, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;
 }

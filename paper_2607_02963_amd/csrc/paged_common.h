@@ -86,7 +86,8 @@ struct PagedRun {
     PagedSeq seq;
     int u, units;   // next position in it, and its units
     int left;       // positions left of the run
-    int pos, per;   // next position in the list of all, positions per work-group
+    int pos;        // next position in the list of all
+    int per, more;  // positions per work-group, the first `more` one more
 };
 
 // What to do next: units [u0, u1) of a pair.
@@ -139,45 +140,50 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             }
             return x;
         };
-        auto cost = [&](int j) {
-            const int n = j < J ? paged_units(a, j) : 0;
+        // a lane's pair: its sequence, and its price
+        PagedSeq x = {0, 0, 0};
+        auto cost = [&](int k) {
+            if (k >= J) return 0;
+            const int s = k / a.groups;
+            x = paged_seq(a, s);
+            const int n = paged_units_of(a, x, k - s * a.groups);
             return n > 0 ? n + a.pad : 0;
         };
-        int total = 0, n0 = 0, incl0 = 0;
-        for (int j0 = 0; j0 < J; j0 += 64) {
-            const int n = cost(j0 + lane), incl = scan(n);
-            if (j0 == 0) n0 = n, incl0 = incl;
-            total += __builtin_amdgcn_readlane(incl, 63);
-        }
-        r.per = max((total * a.H_kv + a.workers - 1) / a.workers, a.least);
-        r.pos = w * r.per;
-        if (r.pos >= total * a.H_kv) return false;
-        r.left = min(r.per, total * a.H_kv - r.pos);
+        int total = 0, n = cost(lane), incl = scan(n);
+        total = __builtin_amdgcn_readlane(incl, 63);
+        for (int j0 = 64; j0 < J; j0 += 64) total += __builtin_amdgcn_readlane(scan(cost(j0 + lane)), 63);
+        const int workers = min(a.workers, max(total * a.H_kv / a.least, 1));
+        if (w >= workers || total == 0) return false;
+        r.per = total * a.H_kv / workers;
+        r.more = total * a.H_kv - r.per * workers;
+        r.pos = w * r.per + min(w, r.more);
+        r.left = r.per + (w < r.more ? 1 : 0);
         r.head = r.pos / total;
-        int rest = r.pos - r.head * total;
-        for (int j0 = 0;; j0 += 64) {
-            int n = n0, incl = incl0;
-            if (j0 > 0) {
-                n = cost(j0 + lane);
-                incl = scan(n);
-            }
+        int rest = r.pos - r.head * total, j0 = 0;
+        if (J > 64) incl = scan(n = cost(lane));
+        while (true) {
             const int all = __builtin_amdgcn_readlane(incl, 63);  // scalar, as everything that leaves the loop
-            if (rest >= all) {
-                rest -= all;
-                continue;
-            }
-            const int at = __builtin_ctzll(__ballot(incl > rest));
-            j = j0 + at;
-            rest -= __builtin_amdgcn_readlane(incl - n, at);
-            r.u = rest;
-            break;
+            if (rest < all) break;
+            rest -= all;
+            j0 += 64;
+            incl = scan(n = cost(j0 + lane));
         }
+        const int at = __builtin_ctzll(__ballot(incl > rest));
+        j = j0 + at;
+        r.u = rest - __builtin_amdgcn_readlane(incl - n, at);
+        r.s = j / a.groups;
+        r.group = j - r.s * a.groups;
+        r.seq.t0 = __builtin_amdgcn_readlane(x.t0, at);
+        r.seq.n = __builtin_amdgcn_readlane(x.n, at);
+        r.seq.L = __builtin_amdgcn_readlane(x.L, at);
+        r.units = __builtin_amdgcn_readlane(n, at) - a.pad;
+        return true;
     }
     r.s = j / a.groups;
     r.group = j - r.s * a.groups;
     r.seq = paged_seq(a, r.s);
     r.units = paged_units_of(a, r.seq, r.group);
-    if (a.whole) r.left = r.per = r.units;
+    r.left = r.units;
     return r.units > 0;
 }
 
@@ -225,7 +231,9 @@ __device__ inline void paged_note(const PagedArgs& a, const PagedRun& r, const P
 {
     if (a.whole || p.u0 > 0) return;
     const int j = p.s * a.groups + p.group;
-    const int4 cut = make_int4(p.whole ? -1 : r.w, (p.end - 1) / r.per, j, p.head);
+    const int at = p.end - 1, first = r.more * (r.per + 1);  // the work-group of the pair's last position
+    const int last = at < first ? at / (r.per + 1) : r.more + (at - first) / r.per;
+    const int4 cut = make_int4(p.whole ? -1 : r.w, last, j, p.head);
     if (a.by_pair) a.cut[p.head * a.num_seqs * a.groups + j] = cut;
     else if (!p.whole) a.cut[r.w] = cut;
 }

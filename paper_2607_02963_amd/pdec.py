@@ -8,8 +8,8 @@ built library is missing, every call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 import os
 
 import torch
@@ -227,6 +227,7 @@ def _stream(stream, device) -> int:
 # alone, which builds a Stream object, takes more than a tenth of that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def make_dims(num_events, H_q, H_kv, D, cap, max_prefix_len, dtype_code, scale=0.0,
@@ -668,16 +669,20 @@ def _cache_code(pages: torch.Tensor) -> int:
     return PDEC_DTYPE_E4M3 if pages.dtype == torch.float8_e4m3fn else _dtype_code(pages)
 
 
-def _paged_dims(rows, H_q, pages, block_table, **kw) -> PagedDims:
-    P, page, H_kv, D = pages.shape
-    return make_paged_dims(block_table.shape[0], rows.shape[0], H_q, H_kv, D, page, P, block_table.shape[1],
-                           _dtype_code(rows), _cache_code(pages), **kw)
+@functools.lru_cache(maxsize=256)
+def _paged_dims(num_tokens, H_q, pool, table, dtype_code, cache_code, max_chunk, max_len, causal, scale) -> PagedDims:
+    """The dims of a call by its sizes (a serving loop makes the same few over and over); not to be written to."""
+    P, page, H_kv, D = pool
+    return make_paged_dims(table[0], num_tokens, H_q, H_kv, D, page, P, table[1], dtype_code, cache_code,
+                           max_chunk=max_chunk, max_len=max_len, causal=causal, scale=scale)
 
 
 def paged_dims_of(q, k_pages, block_table, *, causal=True, max_chunk=None, max_len=None, scale=0.0) -> PagedDims:
     """The dims of a ``paged_attn`` call on these tensors, for ``paged_workspace_size`` and ``query_paged_plan``."""
-    return _paged_dims(q, q.shape[1], k_pages, block_table, max_chunk=max_chunk or 0, max_len=max_len or 0,
-                       causal=bool(causal), scale=scale)
+    P, page, H_kv, D = k_pages.shape
+    return make_paged_dims(block_table.shape[0], q.shape[0], q.shape[1], H_kv, D, page, P, block_table.shape[1],
+                           _dtype_code(q), _cache_code(k_pages), max_chunk=max_chunk or 0, max_len=max_len or 0,
+                           causal=bool(causal), scale=scale)
 
 
 def paged_workspace_size(dims: PagedDims) -> int:
@@ -691,36 +696,64 @@ def query_paged_plan(dims: PagedDims) -> dict:
     return {name: getattr(plan, name) for name, _ in PagedPlan._fields_}
 
 
-def _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype):
-    """Pointers (k, v, k scales, v scales) of a paged cache, checked."""
-    quant = k_pages.dtype == torch.float8_e4m3fn
-    args = [_dev(k_pages, "k_pages", None if quant else dtype, 4), _dev(v_pages, "v_pages", k_pages.dtype, 4)]
-    if v_pages.shape != k_pages.shape:
-        raise ValueError("k_pages and v_pages must have one shape")
-    if not quant:
+# The checks of a call's tensors are a good part of its time on the host, which is
+# as long as a small call's on the GPU: one expression per tensor, and what is
+# wrong with it is found out afterwards.
+
+def _device_of(t, name, rows=True):
+    """Index of the device that a call's first tensor is on, which is the current one, and (of a tensor of rows)
+    its dtype's code."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    code = _dtype_code(t) if rows else None
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be in device memory")
+    if dev != _current_device():
+        raise ValueError(f"{name} is on device {dev}, but the current device is {_current_device()}")
+    return dev, code
+
+
+def _ptr(t, name, dev, dtype, shape):
+    """Address of a contiguous tensor of this device, dtype and shape."""
+    try:
+        if t.get_device() == dev and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, name, dtype)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on another device")
+    raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, shape):
+    """Addresses (k, v, k scales, v scales) of a paged cache."""
+    if k_pages.dtype is not torch.float8_e4m3fn:
         if k_scales is not None or v_scales is not None:
             raise ValueError("only an e4m3 cache has scales")
-        return args + [None, None]
-    P, page, H_kv, _ = k_pages.shape
-    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
-        args.append(_dev(t, name, torch.uint8, 3))
-        if t.shape != (P, H_kv, page):
-            raise ValueError(f"{name} must be [num_pages, H_kv, page_size]")
-    return args
+        return _ptr(k_pages, "k_pages", dev, dtype, shape), _ptr(v_pages, "v_pages", dev, dtype, shape), None, None
+    sc = (shape[0], shape[2], shape[1])
+    return (_ptr(k_pages, "k_pages", dev, torch.float8_e4m3fn, shape), _ptr(v_pages, "v_pages", dev, torch.float8_e4m3fn, shape),
+            _ptr(k_scales, "k_scales", dev, torch.uint8, sc), _ptr(v_scales, "v_scales", dev, torch.uint8, sc))
 
 
-def _one_device(first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("tensors on different devices")
-    if first.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {first.device}, but the current device is {torch.cuda.current_device()}")
+def _paged_sizes(pages, name, block_table):
+    """Shape of a pool of pages (a tuple of four) and of its block table."""
+    if not isinstance(pages, torch.Tensor) or pages.dim() != 4:
+        raise ValueError(f"{name} must be a [num_pages, page_size, H_kv, D] tensor")
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be a [num_seqs, max_pages] tensor")
+    return tuple(pages.shape), tuple(block_table.shape)
 
 
-def _on_stream(stream):
-    """Where a call allocates what it was not given: on the stream that will use it, so that the memory is not
+def _empty(stream, shape, dtype, device):
+    """What a call allocates where it was given nothing: on the stream that will use it, so that the memory is not
     handed out again on another stream while the call runs."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def paged_kv_append(k_new, v_new, k_pages, v_pages, block_table, cu_tokens, lens_in, lens_out, *, k_scales=None,
@@ -731,20 +764,19 @@ def paged_kv_append(k_new, v_new, k_pages, v_pages, block_table, cu_tokens, lens
     ``torch.float8_e4m3fn`` with k_scales/v_scales uint8 [P,H_kv,page]; block_table int32 [S,max_pages];
     cu_tokens int32 [S+1]; lens_in int32 [S] (keys before), lens_out int32 [S] (another tensor: keys after).
     """
-    T, H_kv, D = k_new.shape
-    S = block_table.shape[0]
-    if v_new.shape != k_new.shape or k_pages.shape[2:] != (H_kv, D):
-        raise ValueError("inconsistent append shapes")
-    if cu_tokens.shape[0] != S + 1 or lens_in.shape[0] != S or lens_out.shape[0] != S:
-        raise ValueError("cu_tokens / lens shape")
-    dims = _paged_dims(k_new, H_kv, k_pages, block_table, max_len=max_len or 0)
-    cache = _paged_cache(k_pages, v_pages, k_scales, v_scales, k_new.dtype)
-    args = [_dev(k_new, "k_new", None, 3), _dev(v_new, "v_new", k_new.dtype, 3),
-            _dev(cu_tokens, "cu_tokens", torch.int32, 1), _dev(block_table, "block_table", torch.int32, 2),
-            _dev(lens_in, "lens_in", torch.int32, 1), _dev(lens_out, "lens_out", torch.int32, 1), *cache]
-    _one_device(k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, cu_tokens, lens_in, lens_out)
-    _check("pdec_paged_kv_append", lib().pdec_paged_kv_append(ctypes.byref(dims), *args,
-                                                              _stream(stream, k_new.device)))
+    dev, code = _device_of(k_new, "k_new")
+    pool, table = _paged_sizes(k_pages, "k_pages", block_table)
+    S, shape = table[0], (k_new.shape[0],) + pool[2:]
+    dtype, i32 = k_new.dtype, torch.int32
+    dims = _paged_dims(shape[0], pool[2], pool, table, code, _cache_code(k_pages), 0, max_len or 0, 1, 0.0)
+    k, v, ks, vs = _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, pool)
+    rc = lib().pdec_paged_kv_append(
+        dims, _ptr(k_new, "k_new", dev, dtype, shape), _ptr(v_new, "v_new", dev, dtype, shape),
+        _ptr(cu_tokens, "cu_tokens", dev, i32, (S + 1,)), _ptr(block_table, "block_table", dev, i32, table),
+        _ptr(lens_in, "lens_in", dev, i32, (S,)), _ptr(lens_out, "lens_out", dev, i32, (S,)), k, v, ks, vs,
+        _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_paged_kv_append", rc)
 
 
 def paged_kv_read(k_pages, v_pages, block_table, seq_lens, cu_rows, *, k_out=None, v_out=None, num_rows=None,
@@ -754,30 +786,26 @@ def paged_kv_read(k_pages, v_pages, block_table, seq_lens, cu_rows, *, k_out=Non
     Row cu_rows[s] + t receives key t of sequence s, 0 at or beyond seq_lens[s].  Give k_out and v_out, or
     ``num_rows`` (and ``dtype``, by default bf16 for an e4m3 cache).  Other arguments as for ``paged_kv_append``.
     """
-    S = block_table.shape[0]
-    H_kv, D = k_pages.shape[2:]
-    quant = k_pages.dtype == torch.float8_e4m3fn
+    dev, _ = _device_of(k_pages, "k_pages", rows=False)
+    pool, table = _paged_sizes(k_pages, "k_pages", block_table)
+    S, i32 = table[0], torch.int32
     if (k_out is None) != (v_out is None):
         raise ValueError("give both k_out and v_out or neither")
     if k_out is None:
         if num_rows is None:
             raise ValueError("num_rows is required without k_out and v_out")
         if dtype is None:
-            dtype = torch.bfloat16 if quant else k_pages.dtype
-        with _on_stream(stream):
-            k_out, v_out = (torch.empty((num_rows, H_kv, D), dtype=dtype, device=k_pages.device) for _ in "kv")
-    if k_out.shape[1:] != (H_kv, D) or v_out.shape != k_out.shape:
-        raise ValueError("k_out / v_out shape")
-    if cu_rows.shape[0] != S + 1 or seq_lens.shape[0] != S:
-        raise ValueError("cu_rows / seq_lens shape")
-    dims = _paged_dims(k_out, H_kv, k_pages, block_table, max_len=max_len or 0)
-    cache = _paged_cache(k_pages, v_pages, k_scales, v_scales, k_out.dtype)
-    args = [*cache, _dev(block_table, "block_table", torch.int32, 2), _dev(seq_lens, "seq_lens", torch.int32, 1),
-            _dev(cu_rows, "cu_rows", torch.int32, 1), _dev(k_out, "k_out", None, 3),
-            _dev(v_out, "v_out", k_out.dtype, 3)]
-    _one_device(k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, cu_rows, k_out, v_out)
-    _check("pdec_paged_kv_read", lib().pdec_paged_kv_read(ctypes.byref(dims), *args,
-                                                          _stream(stream, k_pages.device)))
+            dtype = torch.bfloat16 if k_pages.dtype == torch.float8_e4m3fn else k_pages.dtype
+        k_out, v_out = (_empty(stream, (num_rows,) + pool[2:], dtype, k_pages.device) for _ in "kv")
+    dtype, shape = k_out.dtype, (k_out.shape[0],) + pool[2:]
+    dims = _paged_dims(shape[0], pool[2], pool, table, _dtype_code(k_out), _cache_code(k_pages), 0, max_len or 0, 1, 0.0)
+    k, v, ks, vs = _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, pool)
+    rc = lib().pdec_paged_kv_read(
+        dims, k, v, ks, vs, _ptr(block_table, "block_table", dev, i32, table), _ptr(seq_lens, "seq_lens", dev, i32, (S,)),
+        _ptr(cu_rows, "cu_rows", dev, i32, (S + 1,)), _ptr(k_out, "k_out", dev, dtype, shape),
+        _ptr(v_out, "v_out", dev, dtype, shape), _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_paged_kv_read", rc)
     return k_out, v_out
 
 
@@ -791,28 +819,29 @@ def paged_attn(q, k_pages, v_pages, block_table, cu_tokens, seq_lens, *, causal=
     len keys.  ``max_chunk`` and ``max_len`` bound the new tokens and the keys of a sequence (default: T, and
     what block_table can hold); the tighter, the fewer work-groups without work.
     """
+    dev, code = _device_of(q, "q")
+    pool, table = _paged_sizes(k_pages, "k_pages", block_table)
+    if q.dim() != 3:
+        raise ValueError(f"q must have 3 dims, got {tuple(q.shape)}")
     T, H_q, D = q.shape
-    S = block_table.shape[0]
-    if k_pages.shape[3] != D or cu_tokens.shape[0] != S + 1 or seq_lens.shape[0] != S:
-        raise ValueError("inconsistent shapes")
-    dims = paged_dims_of(q, k_pages, block_table, causal=causal, max_chunk=max_chunk, max_len=max_len, scale=scale)
-    cache = _paged_cache(k_pages, v_pages, k_scales, v_scales, q.dtype)
-    if out is None or (lse is None and want_lse) or workspace is None:
-        with _on_stream(stream):
-            if out is None:
-                out = torch.empty_like(q)
-            if lse is None and want_lse:
-                lse = torch.empty((T, H_q), dtype=torch.float32, device=q.device)
-            if workspace is None:
-                workspace = torch.empty(max(paged_workspace_size(dims), 16), dtype=torch.uint8, device=q.device)
-    if out.shape != q.shape or (lse is not None and lse.shape != (T, H_q)):
-        raise ValueError("out / lse shape")
-    args = [_dev(q, "q", None, 3), *cache, _dev(block_table, "block_table", torch.int32, 2),
-            _dev(cu_tokens, "cu_tokens", torch.int32, 1), _dev(seq_lens, "seq_lens", torch.int32, 1),
-            _dev(out, "out", q.dtype, 3), _dev(lse, "lse", torch.float32, 2) if want_lse else None,
-            _dev(workspace, "workspace"), workspace.nbytes]
-    _one_device(q, k_pages, v_pages, k_scales, v_scales, block_table, cu_tokens, seq_lens, out, lse, workspace)
-    _check("pdec_paged_attn", lib().pdec_paged_attn(ctypes.byref(dims), *args, _stream(stream, q.device)))
+    S, dtype, i32, shape = table[0], q.dtype, torch.int32, (T, H_q, pool[3])
+    dims = _paged_dims(T, H_q, pool, table, code, _cache_code(k_pages), max_chunk or 0, max_len or 0,
+                       int(bool(causal)), scale)
+    k, v, ks, vs = _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, pool)
+    if out is None:
+        out = _empty(stream, shape, dtype, q.device)
+    if lse is None and want_lse:
+        lse = _empty(stream, (T, H_q), torch.float32, q.device)
+    if workspace is None:
+        workspace = _empty(stream, max(int(lib().pdec_paged_workspace_size(dims)), 16), torch.uint8, q.device)
+    rc = lib().pdec_paged_attn(
+        dims, _ptr(q, "q", dev, dtype, shape), k, v, ks, vs, _ptr(block_table, "block_table", dev, i32, table),
+        _ptr(cu_tokens, "cu_tokens", dev, i32, (S + 1,)), _ptr(seq_lens, "seq_lens", dev, i32, (S,)),
+        _ptr(out, "out", dev, dtype, shape), _ptr(lse, "lse", dev, torch.float32, (T, H_q)) if want_lse else None,
+        _ptr(workspace, "workspace", dev, workspace.dtype, workspace.shape), workspace.nbytes,
+        _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_paged_attn", rc)
     return out, lse if want_lse else None
 
 
@@ -834,20 +863,20 @@ def merge_states(out_a, lse_a, out_b, lse_b, *, out=None, lse=None, stream=None)
 
     out_a/out_b [...,D] float32 or bf16, lse_a/lse_b float32 [...]; ``out`` and ``lse`` may be one of the sides'.
     """
-    D = out_a.shape[-1]
-    if out_b.shape != out_a.shape or lse_a.shape != out_a.shape[:-1] or lse_b.shape != lse_a.shape:
-        raise ValueError("inconsistent shapes")
-    if out is None or lse is None:
-        with _on_stream(stream):
-            out = torch.empty_like(out_a) if out is None else out
-            lse = torch.empty_like(lse_a) if lse is None else lse
-    if out.shape != out_a.shape or lse.shape != lse_a.shape:
-        raise ValueError("out / lse shape")
-    args = [_dev(out_a, "out_a"), _dev(lse_a, "lse_a", torch.float32), _dev(out_b, "out_b", out_a.dtype),
-            _dev(lse_b, "lse_b", torch.float32), _dev(out, "out", out_a.dtype), _dev(lse, "lse", torch.float32)]
-    _one_device(out_a, lse_a, out_b, lse_b, out, lse)
-    _check("pdec_merge_states", lib().pdec_merge_states(lse_a.numel(), D, _dtype_code(out_a), *args,
-                                                        _stream(stream, out_a.device)))
+    dev, code = _device_of(out_a, "out_a")
+    shape, dtype, f32 = out_a.shape, out_a.dtype, torch.float32
+    rows = shape[:-1]
+    if out is None:
+        out = _empty(stream, shape, dtype, out_a.device)
+    if lse is None:
+        lse = _empty(stream, rows, f32, out_a.device)
+    rc = lib().pdec_merge_states(
+        rows.numel(), shape[-1], code, _ptr(out_a, "out_a", dev, dtype, shape),
+        _ptr(lse_a, "lse_a", dev, f32, rows), _ptr(out_b, "out_b", dev, dtype, shape), _ptr(lse_b, "lse_b", dev, f32, rows),
+        _ptr(out, "out", dev, dtype, shape), _ptr(lse, "lse", dev, f32, rows),
+        _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_merge_states", rc)
     return out, lse
 
 
