@@ -42,12 +42,6 @@ __device__ inline int paged_owner(const PagedIoArgs& a, int t)
     return below < a.num_seqs ? below : -1;
 }
 
-__device__ inline int paged_io_page(const PagedIoArgs& a, int s, int t)
-{
-    const int p = a.block_table[(long)s * a.max_pages + (t >> a.page_shift)];
-    return (uint32_t)p < (uint32_t)a.num_pages ? p : -1;
-}
-
 // Eight consecutive elements of a row.
 template <typename T>
 struct Row8 {
@@ -114,101 +108,147 @@ __device__ inline uint2 quantise8(const Row8<T>& r, int& byte)
     return make_uint2(w[0], w[1]);
 }
 
-// One wave per token and tensor, its H_kv D elements in steps of 512.
-// grid (max(tokens, sequences / 64), 2).
-template <int D, typename T, bool QUANT>
-__global__ __launch_bounds__(64) void paged_append_kernel(PagedIoArgs a)
+// Where rows r0 .. r0 + N - 1 of the batch lie in the pool: page and row in it.
+// page is -1 for a row without a place, -2 for one that exists but has no key
+// (read).  A lane looks up a row, so that N rows take the round trips of one;
+// the results are scalars.  `before`: lens counts the keys before the rows
+// (append), else all keys (read).
+template <int N>
+struct PagedPlace {
+    int page[N], slot[N];
+};
+
+template <int N>
+__device__ inline void paged_place(const PagedIoArgs& a, int r0, bool before, PagedPlace<N>& p)
 {
-    const int t = blockIdx.x, lane = threadIdx.x;
+    const int r = r0 + min(paged_lane(), N - 1);
+    int page = -1, slot = 0;
+    int s = r0 < a.num_tokens ? paged_owner(a, r0) : -1;
+    if (s >= 0 && r < a.num_tokens) {
+        int first = a.cu[s], end = a.cu[s + 1], len = a.lens[s];
+        while (r >= end) {  // the row of a later sequence
+            if (++s >= a.num_seqs) break;
+            first = end;
+            end = a.cu[s + 1];
+            len = a.lens[s];
+        }
+        if (s < a.num_seqs && r >= first && first >= 0) {
+            int key = r - first;
+            bool ok;
+            if (before) {
+                ok = len >= 0 && len <= a.max_len - (min(end, a.num_tokens) - first);
+                key += len;
+            } else {
+                ok = key < min(len, a.max_len);
+                page = -2;
+            }
+            if (ok) {
+                const int e = a.block_table[(long)s * a.max_pages + (key >> a.page_shift)];
+                page = (uint32_t)e < (uint32_t)a.num_pages ? e : page;
+                slot = key & ((1 << a.page_shift) - 1);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p.page[i] = __builtin_amdgcn_readlane(page, i);
+        p.slot[i] = __builtin_amdgcn_readlane(slot, i);
+    }
+}
+
+// A wave takes N consecutive tokens of one tensor, eight elements a lane.
+// grid (max(tokens / (4 N), sequences / 64), 2): few tokens a token per wave, for
+// the latency; many four, with one look-up and all their loads under way.
+template <int D, typename T, bool QUANT, int N>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedIoArgs a)
+{
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool is_v = blockIdx.y != 0;
-    const int elems = a.H_kv * D;
-    const T* src = static_cast<const T*>(is_v ? a.v_rows : a.k_rows) + (long)t * elems;
-    Row8<T> row;
-    const bool token = t < a.num_tokens;  // work-groups beyond serve the counts of many sequences
-    if (token && 8 * lane < elems) row.load(src + 8 * lane);  // under the look-ups
-    // the counts after the append, by the first work-groups
-    if (!is_v && t < (a.num_seqs + 63) / 64) {
-        for (int s = 64 * t + lane; s < min(a.num_seqs, 64 * t + 64); s += 64) {
+    const int elems = a.H_kv * D, r0 = (blockIdx.x * 4 + w) * N;
+    const T* src = static_cast<const T*>(is_v ? a.v_rows : a.k_rows) + (long)r0 * elems;
+    Row8<T> row[N];
+    auto load = [&](int e) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (r0 + i < a.num_tokens && e < elems) row[i].load(src + (long)i * elems + e);
+    };
+    load(8 * lane);  // under the look-ups
+    // the counts after the append, 64 sequences to a work-group
+    if (!is_v && w == 0) {
+        const int s = 64 * blockIdx.x + lane;
+        if (s < a.num_seqs) {
             const int n = a.lens[s], m = min(max(a.cu[s + 1], 0), a.num_tokens) - min(max(a.cu[s], 0), a.num_tokens);
             a.lens_out[s] = n >= 0 && m > 0 && n <= a.max_len - m ? n + m : n;
         }
     }
-    if (!token) return;
-    const int s = paged_owner(a, t);
-    if (s < 0) return;
-    const int n = a.lens[s], t0 = a.cu[s], m = min(a.cu[s + 1], a.num_tokens) - t0;
-    if (t0 < 0 || t < t0 || n < 0 || n > a.max_len - m) return;
-    const int key = n + t - t0;
-    const int page = paged_io_page(a, s, key);
-    if (page < 0) return;
-    const int slot = key & ((1 << a.page_shift) - 1);
-    const long at = (((long)page << a.page_shift) + slot) * elems;
-    unsigned char* dst = static_cast<unsigned char*>(is_v ? a.v_pages : a.k_pages) + at * (QUANT ? 1 : (int)sizeof(T));
+    PagedPlace<N> p;
+    paged_place(a, r0, true, p);
+    unsigned char* pages = static_cast<unsigned char*>(is_v ? a.v_pages : a.k_pages);
+    uint8_t* scales = is_v ? a.v_scales : a.k_scales;
     for (int e = 8 * lane; e < elems; e += 512) {
-        if (e >= 512) row.load(src + e);
-        if constexpr (QUANT) {
-            int byte;
-            *reinterpret_cast<uint2*>(dst + e) = quantise8<D>(row, byte);
-            if (e % D == 0) {
-                uint8_t* sc = is_v ? a.v_scales : a.k_scales;
-                sc[(((long)page * a.H_kv + e / D) << a.page_shift) + slot] = (uint8_t)byte;
+        if (e >= 512) load(e);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (p.page[i] < 0) continue;
+            const long at = ((long)p.page[i] << a.page_shift) + p.slot[i];
+            unsigned char* dst = pages + (at * elems + e) * (QUANT ? 1 : (int)sizeof(T));
+            if constexpr (QUANT) {
+                int byte;
+                *reinterpret_cast<uint2*>(dst) = quantise8<D>(row[i], byte);
+                if (e % D == 0) scales[(((long)p.page[i] * a.H_kv + e / D) << a.page_shift) + p.slot[i]] = (uint8_t)byte;
+            } else {
+                row[i].store(dst);
             }
-        } else {
-            row.store(dst + e * (int)sizeof(T));
         }
     }
 }
 
-// A wave takes kReadRows consecutive rows of one tensor.  grid (rows / (4 kReadRows), 2).
-constexpr int kReadRows = 8;
-
-template <int D, typename T, bool QUANT>
+// A wave takes N consecutive rows of one tensor.  grid (rows / (4 N), 2).
+template <int D, typename T, bool QUANT, int N>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
 {
     const int lane = threadIdx.x & 63;
     const bool is_v = blockIdx.y != 0;
     const int elems = a.H_kv * D;
-    const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kReadRows;
-    const int r1 = min(r0 + kReadRows, a.num_tokens);
-    if (r0 >= r1) return;
+    const int r0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * N;
     const unsigned char* pages = static_cast<const unsigned char*>(is_v ? a.v_pages : a.k_pages);
     const uint8_t* scales = is_v ? a.v_scales : a.k_scales;
-    T* out = static_cast<T*>(const_cast<void*>(is_v ? a.v_rows : a.k_rows));
-    int s = paged_owner(a, r0);
-    if (s < 0) return;
-    int end = __builtin_amdgcn_readfirstlane(a.cu[s + 1]), first = __builtin_amdgcn_readfirstlane(a.cu[s]);
-    int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[s], 0), a.max_len));
-    for (int r = r0; r < r1; ++r) {
-        while (r >= end) {
-            if (++s >= a.num_seqs) return;
-            first = end;
-            end = __builtin_amdgcn_readfirstlane(a.cu[s + 1]);
-            len = __builtin_amdgcn_readfirstlane(min(max(a.lens[s], 0), a.max_len));
+    T* out = static_cast<T*>(const_cast<void*>(is_v ? a.v_rows : a.k_rows)) + (long)r0 * elems;
+    PagedPlace<N> p;
+    paged_place(a, r0, false, p);
+    for (int e = 8 * lane; e < elems; e += 512) {
+        Row8<T> row[N];
+        uint2 x[N];
+        uint32_t byte[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (p.page[i] < 0) continue;
+            const long at = ((long)p.page[i] << a.page_shift) + p.slot[i];
+            if constexpr (QUANT) {
+                x[i] = *reinterpret_cast<const uint2*>(pages + at * elems + e);
+                byte[i] = scales[(((long)p.page[i] * a.H_kv + e / D) << a.page_shift) + p.slot[i]];
+            } else {
+                row[i].load(pages + (at * elems + e) * (int)sizeof(T));
+            }
         }
-        const int key = r - first;
-        const int page = key >= 0 && key < len ? __builtin_amdgcn_readfirstlane(paged_io_page(a, s, key)) : -1;
-        const int slot = key & ((1 << a.page_shift) - 1);
-        const long at = (((long)max(page, 0) << a.page_shift) + slot) * elems;
-        for (int e = 8 * lane; e < elems; e += 512) {
-            Row8<T> row;
-            if (page < 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (p.page[i] == -1) continue;
+            if (p.page[i] < 0) {
                 const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                row.set(z);
+                row[i].set(z);
             } else if constexpr (QUANT) {
-                const uint2 x = *reinterpret_cast<const uint2*>(pages + at + e);
-                const float sc = __uint_as_float((uint32_t)scales[(((long)page * a.H_kv + e / D) << a.page_shift) + slot] << 23);
+                const float sc = paged_scale(byte[i], 0);
                 float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    const int word = (int)(i ? x.y : x.x);
+                for (int k = 0; k < 8; k += 4) {
+                    const int word = (int)(k ? x[i].y : x[i].x);
                     const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
-                    v[i] = lo.x * sc, v[i + 1] = lo.y * sc, v[i + 2] = hi.x * sc, v[i + 3] = hi.y * sc;
+                    v[k] = lo.x * sc, v[k + 1] = lo.y * sc, v[k + 2] = hi.x * sc, v[k + 3] = hi.y * sc;
                 }
-                row.set(v);
-            } else {
-                row.load(pages + (at + e) * (int)sizeof(T));
+                row[i].set(v);
             }
-            row.store(out + (long)r * elems + e);
+            row[i].store(out + (long)i * elems + e);
         }
     }
 }

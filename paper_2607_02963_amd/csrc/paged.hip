@@ -211,21 +211,25 @@ PagedIoArgs io_args(const pdec_paged_dims* d)
     return a;
 }
 
-template <int D, typename T, bool QUANT>
+// Tokens from which a wave of the append takes four.
+constexpr int kAppendMany = 2048;
+constexpr int kReadRows = 8;  // rows per wave of the read-back
+
+template <int D, typename T, bool QUANT, int N>
 void launch_append(const PagedIoArgs& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)std::max(a.num_tokens, (a.num_seqs + 63) / 64), 2);
-    hipLaunchKernelGGL((paged_append_kernel<D, T, QUANT>), grid, dim3(64), 0, s, a);
+    const dim3 grid((unsigned)std::max((a.num_tokens + 4 * N - 1) / (4 * N), (a.num_seqs + 63) / 64), 2);
+    hipLaunchKernelGGL((paged_append_kernel<D, T, QUANT, N>), grid, dim3(256), 0, s, a);
 }
 
 template <int D, typename T, bool QUANT>
 void launch_read(const PagedIoArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.num_tokens + 4 * kReadRows - 1) / (4 * kReadRows)), 2);
-    hipLaunchKernelGGL((paged_read_kernel<D, T, QUANT>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_read_kernel<D, T, QUANT, kReadRows>), grid, dim3(256), 0, s, a);
 }
 
-// f.template operator()<D, T, QUANT>() for the dims' types
+// f(head dim, an element of the rows' type, whether the cache is e4m3), as types
 template <typename F>
 void for_types(const pdec_paged_dims* d, F f)
 {
@@ -280,7 +284,10 @@ int pdec_paged_kv_append(const pdec_paged_dims* d, const void* k_new, const void
     a.lens = lens_in;
     a.lens_out = lens_out;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    for_types(d, [&](auto dim, auto t, auto q) { launch_append<dim(), decltype(t), q()>(a, s); });
+    for_types(d, [&](auto dim, auto t, auto q) { 
+        if (a.num_tokens < kAppendMany) launch_append<dim(), decltype(t), q(), 1>(a, s);
+        else launch_append<dim(), decltype(t), q(), 4>(a, s);
+    });
     return launched();
 }
 

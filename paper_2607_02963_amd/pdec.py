@@ -867,9 +867,9 @@ def merge_states(out_a, lse_a, out_b, lse_b, *, out=None, lse=None, stream=None)
     shape, dtype, f32 = out_a.shape, out_a.dtype, torch.float32
     rows = shape[:-1]
     if out is None:
-        out = _empty(stream, shape, dtype, out_a.device)
+        out = torch.empty_like(out_a) if stream is None else _empty(stream, shape, dtype, out_a.device)
     if lse is None:
-        lse = _empty(stream, rows, f32, out_a.device)
+        lse = torch.empty_like(lse_a) if stream is None else _empty(stream, rows, f32, out_a.device)
     rc = lib().pdec_merge_states(
         rows.numel(), shape[-1], code, _ptr(out_a, "out_a", dev, dtype, shape),
         _ptr(lse_a, "lse_a", dev, f32, rows), _ptr(out_b, "out_b", dev, dtype, shape), _ptr(lse_b, "lse_b", dev, f32, rows),
