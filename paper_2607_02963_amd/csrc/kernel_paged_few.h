@@ -53,6 +53,31 @@ __device__ inline u32x4_t widen8(uint32_t lo, uint32_t hi)
     return r;
 }
 
+// One wave-wide DMA of N KB, N instructions of 16 bytes per lane from one scalar base
+// to consecutive places in LDS.  An instruction's immediate offset counts for its LDS
+// address and for its memory address: off[i] has it taken out (i KB, which the i-th
+// KB of a tensor is at least away from its first, a KB being whole rows).
+template <int N>
+__device__ inline void dma_rows(uint64_t base, const uint32_t (&off)[N], uint32_t lds_base, uint64_t lanes)
+{
+    const uint64_t sb = sgpr_base(reinterpret_cast<const void*>(base)), ln = sgpr_base(reinterpret_cast<const void*>(lanes));
+    const uint32_t m = __builtin_amdgcn_readfirstlane(lds_base);
+    if constexpr (N == 1)
+        asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %3, %2\n\ts_mov_b64 exec, -1" :
+                     : "s"(m), "s"(ln), "s"(sb), "v"(off[0]) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                     "global_load_lds_dwordx4 %4, %2 offset:1024\n\ts_mov_b64 exec, -1" :
+                     : "s"(m), "s"(ln), "s"(sb), "v"(off[0]), "v"(off[1]) : "memory");
+    else {
+        static_assert(N == 4, "instructions of a half");
+        asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                     "global_load_lds_dwordx4 %4, %2 offset:1024\n\tglobal_load_lds_dwordx4 %5, %2 offset:2048\n\t"
+                     "global_load_lds_dwordx4 %6, %2 offset:3072\n\ts_mov_b64 exec, -1" :
+                     : "s"(m), "s"(ln), "s"(sb), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory");
+    }
+}
+
 template <int D, int NT, bool FP8, int NW>
 __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
 {
@@ -81,17 +106,17 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
     if (!paged_begin(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
 
     const float c = a.qscale;
-    const uint32_t strideB = (uint32_t)a.H_kv * ROWB;
+    const uint32_t strideB = (uint32_t)a.H_kv * ROWB, pageB = strideB << a.page_shift;  // bytes of a token, a page
     const uint32_t ring = lds_u32(lds) + w * RING, sc_ring = lds_u32(lds) + NW * RING + w * NS * 64;
-    // byte offset of the lane's chunk in piece i of half h of a tensor
+    // byte offset of the lane's chunk in instruction i of half h of a tensor, less 1024 i (dma_rows)
     uint32_t koffs[2][PPH], voffs[2][PPH];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < PPH; ++i) {
             const int k = i * KPI + lane / CPK, key = 16 * h + k;
-            koffs[h][i] = (uint32_t)k * strideB + 16 * ((lane % CPK) ^ few_kswz<D, FP8>(key));
-            voffs[h][i] = (uint32_t)k * strideB + 16 * ((lane % CPK) ^ few_vswz<D, FP8>(key));
+            koffs[h][i] = (uint32_t)k * strideB + 16 * ((lane % CPK) ^ few_kswz<D, FP8>(key)) - 1024 * i;
+            voffs[h][i] = (uint32_t)k * strideB + 16 * ((lane % CPK) ^ few_vswz<D, FP8>(key)) - 1024 * i;
         }
     // operand reads, relative to a slot
     uint32_t kread[FP8 ? KS / 2 : KS], vread[DT];
@@ -109,6 +134,7 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
     }
     typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
     typedef __attribute__((address_space(3))) const uint32_t lds_u32_t;
+    const uint64_t sc_lane = FP8 ? reinterpret_cast<uint64_t>(lane & 8 ? a.v_scales : a.k_scales) + 4 * (lane & 3) : 0;
 
     while (paged_next(a, run, part)) {
         if (w == 0 && lane == 0) paged_note(a, run, part);
@@ -126,7 +152,8 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
         auto pages = [&](int b) __attribute__((always_inline)) {
             Pages x;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) x.half[h] = paged_entry(table, min((first(b) + 16 * h) >> a.page_shift, a.max_pages - 1));
+            for (int h = 0; h < 2; ++h)
+                x.half[h] = h > 0 && a.page_shift > 4 ? x.half[0] : paged_entry(table, min((first(b) + 16 * h) >> a.page_shift, a.max_pages - 1));
             return x;
         };
         auto there = [&](const Pages& x, int h) __attribute__((always_inline)) { return (uint32_t)x.half[h] < (uint32_t)a.num_pages; };
@@ -135,26 +162,27 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
         auto issue = [&](int b, const Pages& x) __attribute__((always_inline)) {
             const uint64_t lanes = b < mine ? ~0ull : 1ull;
             const uint32_t dst = ring + (b % NS) * SLOT;
-            uint64_t ksc[2], vsc[2];
+            const int row = first(b) & ((1 << a.page_shift) - 1);  // of the first half
+            uint64_t at[2], sc[2];
+            const int page0 = there(x, 0) && b < mine ? x.half[0] : 0;
+            at[0] = (uint64_t)(uint32_t)page0 * pageB + (uint32_t)row * strideB;
+            if constexpr (FP8) sc[0] = (((uint64_t)(uint32_t)page0 * a.H_kv + part.head) << a.page_shift) + (uint32_t)row;
+            if (a.page_shift > 4) {  // both halves on one page
+                at[1] = at[0] + 16 * strideB;
+                if constexpr (FP8) sc[1] = sc[0] + 16;
+            } else {
+                const int page1 = there(x, 1) && b < mine ? x.half[1] : 0;
+                at[1] = (uint64_t)(uint32_t)page1 * pageB;
+                if constexpr (FP8) sc[1] = ((uint64_t)(uint32_t)page1 * a.H_kv + part.head) << a.page_shift;
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int page = there(x, h) && b < mine ? x.half[h] : 0;
-                const int row = (first(b) + 16 * h) & ((1 << a.page_shift) - 1);
-                const uint64_t at = (((uint64_t)(uint32_t)page << a.page_shift) + (uint32_t)row) * strideB;
-#pragma unroll
-                for (int i = 0; i < PPH; ++i) {
-                    dma_16B_page(kbase + at, koffs[h][i], dst + 1024 * (h * PPH + i), lanes);
-                    dma_16B_page(vbase + at, voffs[h][i], dst + TENSOR + 1024 * (h * PPH + i), lanes);
-                }
-                if constexpr (FP8) {
-                    const uint64_t sc = (((uint64_t)(uint32_t)page * a.H_kv + part.head) << a.page_shift) + (uint32_t)row;
-                    ksc[h] = sgpr_base(a.k_scales) + sc;
-                    vsc[h] = sgpr_base(a.v_scales) + sc;
-                }
+                dma_rows(kbase + at[h], koffs[h], dst + 1024 * h * PPH, lanes);
+                dma_rows(vbase + at[h], voffs[h], dst + TENSOR + 1024 * h * PPH, lanes);
             }
             if constexpr (FP8) {  // 16 bytes each of K's halves, then of V's, four lanes to a half
-                const uint64_t from = lane & 8 ? (lane & 4 ? vsc[1] : vsc[0]) : (lane & 4 ? ksc[1] : ksc[0]);
-                dma_4B_lanes(from + 4 * (lane & 3), sc_ring + (b % NS) * 64, lanes & 0xffffu);
+                const uint64_t from = (lane & 4 ? sc[1] : sc[0]) + sc_lane;
+                dma_4B_lanes(from, sc_ring + (b % NS) * 64, lanes & 0xffffu);
             }
         };
 
