@@ -16,6 +16,11 @@
 // Rows are permuted 16 bytes at a time in LDS so that the reads of one phase
 // meet different banks.
 //
+// HW kv heads to a work-group, its waves dealt to the heads in turn: two where a
+// head's row is 64 bytes (8-bit rows of 64), half a cache line, whose other half
+// would be fetched again for the other head at another time (290 MB at 8 heads:
+// 104 us against 77).
+//
 // 8-bit pages stay 8 bits in LDS, and their operands are widened in registers:
 // each is used by one wave only, so once each.  A lane's 16 bytes of a key row
 // are the operands of two steps (the contraction over d is taken in that order,
@@ -78,10 +83,11 @@ __device__ inline void dma_rows(uint64_t base, const uint32_t (&off)[N], uint32_
     }
 }
 
-template <int D, int NT, bool FP8, int NW>
+template <int D, int NT, bool FP8, int NW, int HW>
 __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
 {
     constexpr int RT = 16 * NT;
+    constexpr int NK = NW / HW;                  // waves that share a head's keys
     constexpr int RING = 131072 / NW;            // bytes of a wave's ring
     constexpr int ESZ = FP8 ? 1 : 2, ROWB = D * ESZ;
     constexpr int KB = 32;                       // keys per block
@@ -100,6 +106,7 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
     __shared__ float m_s[NW][16 * MT], l_s[NW][16 * MT];
 
     const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
+    const int wk = w / HW, wh = w % HW;  // the wave's blocks, and its head of the pair's
     const int lane = paged_lane(), l16 = lane & 15, lg = lane >> 4;
     PagedRun run;
     PagedPart part;
@@ -141,13 +148,14 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
         const PagedSeq sq = part.seq;
         const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);
         const int tiles = (nrows + 15) / 16;
-        const int nb = 2 * (part.u1 - part.u0), mine = nb > w ? (nb - w + NW - 1) / NW : 0;  // blocks: of the part, of the wave
+        const int nb = 2 * (part.u1 - part.u0), mine = nb > wk ? (nb - wk + NK - 1) / NK : 0;  // blocks: of the part, of the wave
         const int t0 = part.u0 * kUnit;
         const int32_t* table = a.block_table + (long)part.s * a.max_pages;
-        const uint64_t kbase = sgpr_base(a.k_pages) + (uint64_t)part.head * ROWB, vbase = sgpr_base(a.v_pages) + (uint64_t)part.head * ROWB;
+        const int head = part.head * HW + wh;
+        const uint64_t kbase = sgpr_base(a.k_pages) + (uint64_t)head * ROWB, vbase = sgpr_base(a.v_pages) + (uint64_t)head * ROWB;
 
         // the wave's block b: its first key, and its halves' pages
-        auto first = [&](int b) __attribute__((always_inline)) { return t0 + KB * (w + NW * b); };
+        auto first = [&](int b) __attribute__((always_inline)) { return t0 + KB * (wk + NK * b); };
         struct Pages { int half[2]; };
         auto pages = [&](int b) __attribute__((always_inline)) {
             Pages x;
@@ -166,14 +174,14 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
             uint64_t at[2], sc[2];
             const int page0 = there(x, 0) && b < mine ? x.half[0] : 0;
             at[0] = (uint64_t)(uint32_t)page0 * pageB + (uint32_t)row * strideB;
-            if constexpr (FP8) sc[0] = (((uint64_t)(uint32_t)page0 * a.H_kv + part.head) << a.page_shift) + (uint32_t)row;
+            if constexpr (FP8) sc[0] = (((uint64_t)(uint32_t)page0 * a.H_kv + head) << a.page_shift) + (uint32_t)row;
             if (a.page_shift > 4) {  // both halves on one page
                 at[1] = at[0] + 16 * strideB;
                 if constexpr (FP8) sc[1] = sc[0] + 16;
             } else {
                 const int page1 = there(x, 1) && b < mine ? x.half[1] : 0;
                 at[1] = (uint64_t)(uint32_t)page1 * pageB;
-                if constexpr (FP8) sc[1] = ((uint64_t)(uint32_t)page1 * a.H_kv + part.head) << a.page_shift;
+                if constexpr (FP8) sc[1] = ((uint64_t)(uint32_t)page1 * a.H_kv + head) << a.page_shift;
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -193,7 +201,7 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
         for (int nt = 0; nt < NT; ++nt) {
             const int r = 16 * nt + l16, rr = row0 + min(r, nrows - 1);
             seen[nt] = r < nrows ? paged_seen(a, sq, rr / a.G) : 0;
-            const uint16_t* q = static_cast<const uint16_t*>(a.q) + paged_qrow(a, sq, part.head, rr) * D;
+            const uint16_t* q = static_cast<const uint16_t*>(a.q) + paged_qrow(a, sq, head, rr) * D;
 #pragma unroll
             for (int t = 0; t < KS; ++t)
                 qf[nt][t] = *reinterpret_cast<const u32x4_t*>(q + (FP8 ? 64 * (t / 2) + 16 * lg + 8 * (t & 1) : 32 * t + 8 * lg));
@@ -372,27 +380,28 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
             }
             lds_barrier();
             const int rows = min(nrows - 16 * n0, 16 * MT);
-            for (int i = 64 * w + lane; i < rows * (D / 4); i += 64 * NW) {
-                const int r = i / (D / 4), d4 = i % (D / 4);
-                float M = m_s[0][r];
+            for (int i = 64 * w + lane; i < HW * rows * (D / 4); i += 64 * NW) {
+                const int r = i / (D / 4) % rows, d4 = i % (D / 4), hs = i / (D / 4) / rows;
+                float M = m_s[hs][r];
 #pragma unroll
-                for (int x = 1; x < NW; ++x) M = fmaxf(M, m_s[x][r]);
+                for (int x = 1; x < NK; ++x) M = fmaxf(M, m_s[HW * x + hs][r]);
                 float L = 0.f;
                 f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int x = 0; x < NW; ++x) {
-                    const float f = fast_exp2(m_s[x][r] - M);  // 0 for a wave that saw none of the row's keys
-                    L += f * l_s[x][r];
-                    acc += f * *reinterpret_cast<const f32x4_t*>(o_s + (x * 16 * MT + r) * OROW + 4 * d4);
+                for (int x = 0; x < NK; ++x) {
+                    const int y = HW * x + hs;
+                    const float f = fast_exp2(m_s[y][r] - M);  // 0 for a wave that saw none of the row's keys
+                    L += f * l_s[y][r];
+                    acc += f * *reinterpret_cast<const f32x4_t*>(o_s + (y * 16 * MT + r) * OROW + 4 * d4);
                 }
                 const int row = 16 * n0 + r;
                 if (!part.whole) {
-                    const long at = (long)part.slot * RT + row;
+                    const long at = ((long)part.slot * HW + hs) * RT + row;
                     *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 4 * d4) = acc;
                     if (d4 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(M, L);
                     continue;
                 }
-                const long qr = paged_qrow(a, sq, part.head, row0 + row);
+                const long qr = paged_qrow(a, sq, part.head * HW + hs, row0 + row);
                 const bool any = __float_as_uint(L) != 0;  // L is 0, positive or NaN
                 const float inv = any ? 1.f / L : 0.f;
                 acc *= inv;

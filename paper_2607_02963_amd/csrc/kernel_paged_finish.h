@@ -21,7 +21,7 @@ __global__ __launch_bounds__(64 * kPagedFinishWaves) void paged_finish_kernel(Pa
     constexpr int RPB = kPagedFinishWaves / W;  // rows per work-group
     __shared__ float part[W > 1 ? W : 1][D + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = blockIdx.y * RPB + wave / W, w = wave % W;
+    const int y = blockIdx.y * RPB + wave / W, hs = y % a.heads, r = y / a.heads, w = wave % W;
     const int J = a.num_seqs * a.groups;
     // pairs that do not exist have no note
     if (a.by_pair && paged_units(a, blockIdx.x % J) == 0) return;
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(64 * kPagedFinishWaves) void paged_finish_kernel(Pa
     const PagedSeq sq = paged_seq(a, s);
     if (r >= min(a.rows, sq.n * a.G - row0)) return;  // W > 1: the whole work-group, which has one row
     const int count = cut.y - cut.x + 1;
-    auto state = [&](int i) { return (long)(2 * (cut.x + i) + (i == 0 ? 1 : 0)) * a.rows + r; };
+    auto state = [&](int i) { return ((long)(2 * (cut.x + i) + (i == 0 ? 1 : 0)) * a.heads + hs) * a.rows + r; };
     constexpr int B = 8;  // states in flight
     float L = 0.f, acc[E], x[B][E];
     float2 ml[B];
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * kPagedFinishWaves) void paged_finish_kernel(Pa
             for (int e = 0; e < E; ++e) acc[e] += part[k][E * lane + e];
         }
     }
-    const long qr = paged_qrow(a, sq, cut.w, row0 + r);
+    const long qr = paged_qrow(a, sq, cut.w * a.heads + hs, row0 + r);
     const bool any = L > 0.f || L != L;
     const float inv = any ? 1.f / L : 0.f;
     if constexpr (sizeof(T) == 4) {

@@ -38,7 +38,8 @@ namespace {
 template <int D, typename T>
 void launch_finish(const PagedArgs& a, hipStream_t s)
 {
-    const int pairs = a.H_kv * a.num_seqs * a.groups, rows = (int)std::min<long>(a.rows, (long)a.max_chunk * a.G);
+    const int pairs = a.H_kv / a.heads * a.num_seqs * a.groups;
+    const int rows = a.heads * (int)std::min<long>(a.rows, (long)a.max_chunk * a.G);
     const unsigned x = (unsigned)(a.by_pair ? pairs : a.workers);
     const dim3 block(64 * kPagedFinishWaves);
     // eight states or more per pair, if all work-groups have work: a row's waves share them
@@ -112,7 +113,7 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int 
     a.groups = (int)((std::min<int64_t>(R, a.rows_to) + a.rows - 1) / a.rows);
     const int64_t units = (a.max_len + kUnit - 1) / kUnit;
     const int64_t real_groups = (int64_t)d->num_tokens * a.G / a.rows + d->num_seqs;  // at most, over the batch
-    const int64_t pairs = (int64_t)d->num_seqs * a.groups * a.H_kv;
+    const int64_t pairs = (int64_t)d->num_seqs * a.groups * (a.H_kv / a.heads);
     if (pairs > INT32_MAX / 2 || real_groups * a.H_kv * (units + pad + 1) > INT32_MAX / 2) return false;
     a.workers = workers;
     a.least = least;
@@ -122,8 +123,8 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int 
     a.blocks = a.whole ? (int)((pairs + 7) / 8 * 8) : workers;
     *bytes = 0;
     if (!a.whole)
-        *bytes = align256((size_t)workers * sizeof(int4)) + align256((size_t)2 * workers * a.rows * 2 * sizeof(float)) +
-                 (size_t)2 * workers * a.rows * d->head_dim * sizeof(float);
+        *bytes = align256((size_t)workers * sizeof(int4)) + align256((size_t)2 * workers * a.heads * a.rows * 2 * sizeof(float)) +
+                 (size_t)2 * workers * a.heads * a.rows * d->head_dim * sizeof(float);
     return true;
 }
 
@@ -133,7 +134,7 @@ void place(PagedArgs& a, char* ws)
     a.cut = reinterpret_cast<int4*>(ws);
     ws += align256((size_t)a.workers * sizeof(int4));
     a.part_ml = reinterpret_cast<float*>(ws);
-    ws += align256((size_t)2 * a.workers * a.rows * 2 * sizeof(float));
+    ws += align256((size_t)2 * a.workers * a.heads * a.rows * 2 * sizeof(float));
     a.part_o = reinterpret_cast<float*>(ws);
 }
 
@@ -158,6 +159,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     const int64_t R = (int64_t)a.max_chunk * a.G;
     a.rows_from = 0;
     a.rows_to = INT32_MAX;
+    a.heads = 1;
     p.few = p.many = a;
     p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > kFewRows;
     // one sequence is the many rows' whatever its chunk; of several, each goes by its own
@@ -173,7 +175,9 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     if (p.use_few) {
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
         const bool f32 = d->dtype == PDEC_DTYPE_F32;
-        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : 64;
+        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : most <= 48 && d->head_dim == 64 ? 48 : 64;
+        // a head's row of half a cache line: two heads to a work-group
+        if (!f32 && d->cache_dtype == PDEC_DTYPE_E4M3 && d->head_dim == 64 && a.H_kv % 2 == 0) p.few.heads = 2;
         if (!divide(d, p.few, f32 ? 512 : 256, 2, f32 ? 1 : 4, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;

@@ -40,13 +40,14 @@ struct PagedArgs {
     const int32_t* seq_lens;
     void* out;
     float* lse;       // may be null
-    float* part_o;    // [2 workers, rows, D]
-    float* part_ml;   // [2 workers, rows, 2]
+    float* part_o;    // [2 workers, heads, rows, D]
+    float* part_ml;   // [2 workers, heads, rows, 2]
     int4* cut;        // a cut pair's (first work-group, last, pair of its head, head); first = -1: not cut
     int num_seqs, num_tokens, H_q, H_kv, G;
     int page_shift, num_pages, max_pages, max_chunk, max_len, causal;
     float qscale;     // softmax scale * log2(e)
-    int rows;         // query rows per item
+    int rows;         // query rows per item and head
+    int heads;        // kv heads of a pair (kernel_paged_few.h), 1 elsewhere
     int groups;       // row groups per (kv head, sequence), at most
     int rows_from;    // this launch serves the sequences with rows_from <= R <= rows_to
     int rows_to;
@@ -82,7 +83,7 @@ __device__ inline int paged_seen(const PagedArgs& a, const PagedSeq& x, int i)
 // the pad first.  Uniform over the work-group.
 struct PagedRun {
     int w;          // its number
-    int head, s, group;  // the pair at hand: kv head, sequence, row group
+    int head, s, group;  // the pair at hand: kv head (or `heads` of them), sequence, row group
     PagedSeq seq;
     int u, units;   // next position in it, and its units
     int left;       // positions left of the run
@@ -121,13 +122,13 @@ __device__ inline int paged_units(const PagedArgs& a, int j)
 // lane of the work-group (the caller says which) notes for the finish pass what is cut.
 __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool note)
 {
-    const int J = a.num_seqs * a.groups, lane = paged_lane();
+    const int J = a.num_seqs * a.groups, lane = paged_lane(), sets = a.H_kv / a.heads;
     if (note && !a.whole && !a.by_pair) a.cut[w] = make_int4(-1, 0, 0, 0);  // unless a pair is cut below
     int j;
     r.w = w;
     r.u = 0;
     if (a.whole) {
-        if (w >= J * a.H_kv) return false;
+        if (w >= J * sets) return false;
         r.head = w / J;
         j = w - r.head * J;
         r.pos = 0;
@@ -152,10 +153,10 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
         int total = 0, n = cost(lane), incl = scan(n);
         total = __builtin_amdgcn_readlane(incl, 63);
         for (int j0 = 64; j0 < J; j0 += 64) total += __builtin_amdgcn_readlane(scan(cost(j0 + lane)), 63);
-        const int workers = min(a.workers, max(total * a.H_kv / a.least, 1));
+        const int workers = min(a.workers, max(total * sets / a.least, 1));
         if (w >= workers || total == 0) return false;
-        r.per = total * a.H_kv / workers;
-        r.more = total * a.H_kv - r.per * workers;
+        r.per = total * sets / workers;
+        r.more = total * sets - r.per * workers;
         r.pos = w * r.per + min(w, r.more);
         r.left = r.per + (w < r.more ? 1 : 0);
         r.head = r.pos / total;
@@ -191,7 +192,7 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
 // one inside the loop would make everything that leaves it a vector value.)
 __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
 {
-    const int pad = a.whole ? 0 : a.pad;
+    const int pad = a.whole ? 0 : a.pad, sets = a.H_kv / a.heads;
     while (r.left > 0) {
         while (r.u >= r.units + pad || r.units == 0) {  // positions are left, so another pair follows
             r.u = 0;
@@ -201,7 +202,7 @@ __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
                 r.group = 0;
                 if (++r.s >= a.num_seqs) {
                     r.s = 0;
-                    if (++r.head >= a.H_kv) return false;  // lengths that changed under the call
+                    if (++r.head >= sets) return false;  // lengths that changed under the call
                 }
                 r.seq = paged_seq(a, r.s);
                 r.units = paged_units_of(a, r.seq, 0);

@@ -17,21 +17,25 @@ void launch_rows(const PagedArgs& a, hipStream_t s)
     else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, int HW>
 void launch_few(const PagedArgs& a, hipStream_t s)
 {
+    // eight waves where the registers allow two on a SIMD
     const dim3 grid((unsigned)a.blocks);
-    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8, 8>), grid, dim3(512), 0, s, a);
-    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8, 8>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, 4>), grid, dim3(256), 0, s, a);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8, 8, HW>), grid, dim3(512), 0, s, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8, 8, HW>), grid, dim3(512), 0, s, a);
+    else if constexpr (D == 128) hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, 4, HW>), grid, dim3(256), 0, s, a);
+    else if (a.rows == 48) hipLaunchKernelGGL((paged_few_kernel<D, 3, FP8, 8, HW>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, 8, HW>), grid, dim3(512), 0, s, a);
 }
 
 }  // namespace
 
 void launch_paged_few(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
 {
-    if (head_dim == 128) fp8 ? launch_few<128, true>(a, s) : launch_few<128, false>(a, s);
-    else fp8 ? launch_few<64, true>(a, s) : launch_few<64, false>(a, s);
+    if (head_dim == 128) fp8 ? launch_few<128, true, 1>(a, s) : launch_few<128, false, 1>(a, s);
+    else if (!fp8) launch_few<64, false, 1>(a, s);
+    else a.heads == 2 ? launch_few<64, true, 2>(a, s) : launch_few<64, true, 1>(a, s);
 }
 
 void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
