@@ -17,9 +17,10 @@
 // meet different banks.
 //
 // HW kv heads to a work-group, its waves dealt to the heads in turn: two where a
-// head's row is 64 bytes (8-bit rows of 64), half a cache line, whose other half
-// would be fetched again for the other head at another time (290 MB at 8 heads:
-// 104 us against 77).
+// head's row is a cache line (128 bytes) or half of one, so that neighbouring rows
+// are asked for at about the same time.  32 tokens over 8 heads of 64: 104 against
+// 77 us over 8-bit pages (half a line, whose other half was fetched twice), 120
+// against 108 over bfloat16; over 4 heads of 128 in 8 bits 65.3 against 62.8.
 //
 // 8-bit pages stay 8 bits in LDS, and their operands are widened in registers:
 // each is used by one wave only, so once each.  A lane's 16 bytes of a key row

@@ -5,8 +5,8 @@
 // states, then the sum of 2^(m - M) times each state; the waves' sums meet in
 // LDS, in order.  What bounds it: a chain of two memory round trips, and the
 // states' bytes.  Where few pairs are cut into many states (one long axis) a
-// single wave would take them in turn: 64 states of 224 rows took 21.7 us with
-// W = 1.
+// single wave would take them in turn: 64 states of 896 rows took 21.7 us with
+// W = 1, and take 9.2 with W = 4.
 #pragma once
 
 #include "kernel_mfma.h"
@@ -14,11 +14,13 @@
 
 namespace pdec {
 
+constexpr int kPagedFinishRows = 4;  // rows per work-group with one wave per row
+
 template <int D, typename T, int W>
-__global__ __launch_bounds__(64 * kPagedFinishWaves) void paged_finish_kernel(PagedArgs a)
+__global__ __launch_bounds__(64 * (W > 1 ? W : kPagedFinishRows)) void paged_finish_kernel(PagedArgs a)
 {
     constexpr int E = D / 64;  // elements per lane
-    constexpr int RPB = kPagedFinishWaves / W;  // rows per work-group
+    constexpr int RPB = W > 1 ? 1 : kPagedFinishRows;  // rows per work-group
     __shared__ float part[W > 1 ? W : 1][D + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int y = blockIdx.y * RPB + wave / W, hs = y % a.heads, r = y / a.heads, w = wave % W;

@@ -41,10 +41,13 @@ void launch_finish(const PagedArgs& a, hipStream_t s)
     const int pairs = a.H_kv / a.heads * a.num_seqs * a.groups;
     const int rows = a.heads * (int)std::min<long>(a.rows, (long)a.max_chunk * a.G);
     const unsigned x = (unsigned)(a.by_pair ? pairs : a.workers);
-    const dim3 block(64 * kPagedFinishWaves);
-    // eight states or more per pair, if all work-groups have work: a row's waves share them
-    if (pairs <= a.workers / 8) hipLaunchKernelGGL((paged_finish_kernel<D, T, 4>), dim3(x, (unsigned)rows), block, 0, s, a);
-    else hipLaunchKernelGGL((paged_finish_kernel<D, T, 1>), dim3(x, (unsigned)((rows + kPagedFinishWaves - 1) / kPagedFinishWaves)), block, 0, s, a);
+    // States per pair, if all work-groups have work: a row's waves share them.  Sixteen
+    // waves a row where the rows leave compute units free (28 rows of 64 states: a call
+    // of 23.6 us to 21.9), four where there are many (896 rows: 9.2 us, sixteen 13.7).
+    const int states = a.workers / pairs;
+    if (states >= 32 && pairs * rows <= 256) hipLaunchKernelGGL((paged_finish_kernel<D, T, 16>), dim3(x, (unsigned)rows), dim3(1024), 0, s, a);
+    else if (states >= 8) hipLaunchKernelGGL((paged_finish_kernel<D, T, 4>), dim3(x, (unsigned)rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_finish_kernel<D, T, 1>), dim3(x, (unsigned)((rows + kPagedFinishRows - 1) / kPagedFinishRows)), dim3(64 * kPagedFinishRows), 0, s, a);
 }
 
 }  // namespace
@@ -176,8 +179,8 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
         const bool f32 = d->dtype == PDEC_DTYPE_F32;
         p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : most <= 48 && d->head_dim == 64 ? 48 : 64;
-        // a head's row of half a cache line: two heads to a work-group
-        if (!f32 && d->cache_dtype == PDEC_DTYPE_E4M3 && d->head_dim == 64 && a.H_kv % 2 == 0) p.few.heads = 2;
+        // heads' rows of a cache line or half of one: two heads to a work-group
+        if (!f32 && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;
         if (!divide(d, p.few, f32 ? 512 : 256, 2, f32 ? 1 : 4, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;

@@ -26,8 +26,6 @@
 
 namespace pdec {
 
-constexpr int kPagedFinishWaves = 4;  // waves per work-group of the finish pass
-
 // One launch's arguments.
 struct PagedArgs {
     const void* q;

@@ -33,9 +33,11 @@ void launch_few(const PagedArgs& a, hipStream_t s)
 
 void launch_paged_few(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
 {
-    if (head_dim == 128) fp8 ? launch_few<128, true, 1>(a, s) : launch_few<128, false, 1>(a, s);
-    else if (!fp8) launch_few<64, false, 1>(a, s);
-    else a.heads == 2 ? launch_few<64, true, 2>(a, s) : launch_few<64, true, 1>(a, s);
+    const bool two = a.heads == 2;
+    if (head_dim == 128 && !fp8) launch_few<128, false, 1>(a, s);
+    else if (head_dim == 128) two ? launch_few<128, true, 2>(a, s) : launch_few<128, true, 1>(a, s);
+    else if (fp8) two ? launch_few<64, true, 2>(a, s) : launch_few<64, true, 1>(a, s);
+    else two ? launch_few<64, false, 2>(a, s) : launch_few<64, false, 1>(a, s);
 }
 
 void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
