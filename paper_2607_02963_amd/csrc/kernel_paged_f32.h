@@ -59,7 +59,7 @@ __device__ inline f32x4_t paged_mfma4(float a, float b, f32x4_t c)
 }
 
 template <int D, int NT, typename TC>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedArgs a)
+__global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_kernel(PagedArgs a)
 {
     constexpr int NW = 4, RT = 16 * NT;
     constexpr int KPL = D / 4;   // elements of a key (query) row per lane
@@ -110,37 +110,54 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
         PagedRaw<TC, KPL> kx;
         PagedRaw<TC, DT> vx[4];
         uint32_t ks = 0, vs = 0;  // scales of keys 4 lg .. 4 lg + 3
-        // this wave's keys of unit u: 16 from key t, on one page; nothing is
-        // loaded where no row sees any of them
-        auto begins = [&](int u, int& t, int& page) {
-            t = u * kUnit + 16 * w;
-            page = u < part.u1 && t < most ? __builtin_amdgcn_readfirstlane(paged_page(a, part.s, t)) : -1;
-            return page >= 0;
+        // The wave's 16 keys of a unit are on one page.  Units none of whose keys a row
+        // sees, and keys without a page, are passed over.
+        const int32_t* table = a.block_table + (long)part.s * a.max_pages;
+        auto next = [&](int u, int& page) {
+            for (; u < part.u1; ++u) {
+                const int t = u * kUnit + 16 * w;
+                page = t < most ? paged_entry(table, min(t >> a.page_shift, a.max_pages - 1)) : -1;
+                if ((uint32_t)page < (uint32_t)a.num_pages) break;
+            }
+            return u;
         };
-        auto load = [&](int t, int page) {
-            const int slot = t & ((1 << a.page_shift) - 1);
-            const long base = (((long)page << a.page_shift) + slot) * rowb + (long)part.head * D * ESZ;
-            kx.load(static_cast<const unsigned char*>(a.k_pages) + base + l16 * rowb + KPL * lg * ESZ);
+        auto row_of = [&](int u, int page) { return ((long)page << a.page_shift) + ((u * kUnit + 16 * w) & ((1 << a.page_shift) - 1)); };
+        auto scale_at = [&](int u, int page) {
+            return (((long)page * a.H_kv + part.head) << a.page_shift) + ((u * kUnit + 16 * w) & ((1 << a.page_shift) - 1)) + 4 * lg;
+        };
+        auto load_k = [&](int u, int page) {
+            kx.load(static_cast<const unsigned char*>(a.k_pages) + (row_of(u, page) + l16) * rowb + ((long)part.head * D + KPL * lg) * ESZ);
+            if constexpr (SCALED) ks = *reinterpret_cast<const uint32_t*>(a.k_scales + scale_at(u, page));
+        };
+        auto load_v = [&](int u, int page) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                vx[i].load(static_cast<const unsigned char*>(a.v_pages) + base + (4 * lg + i) * rowb + DT * l16 * ESZ);
-            if constexpr (SCALED) {
-                const long sc = (((long)page * a.H_kv + part.head) << a.page_shift) + slot + 4 * lg;
-                ks = *reinterpret_cast<const uint32_t*>(a.k_scales + sc);
-                vs = *reinterpret_cast<const uint32_t*>(a.v_scales + sc);
-            }
+                vx[i].load(static_cast<const unsigned char*>(a.v_pages) + (row_of(u, page) + 4 * lg + i) * rowb + ((long)part.head * D + DT * l16) * ESZ);
+            if constexpr (SCALED) vs = *reinterpret_cast<const uint32_t*>(a.v_scales + scale_at(u, page));
         };
-        for (int u = part.u0; u < part.u1; ++u) {
-            int t, page;
-            if (!begins(u, t, page)) continue;
-            load(t, page);
-            f32x4_t s[NT];
+        int page = -1, u = next(part.u0, page);
+        if (u < part.u1) {
+            load_k(u, page);
+            load_v(u, page);
+        }
+        while (u < part.u1) {
+            const int t = u * kUnit + 16 * w;
+            const uint32_t ksc = ks;
+            f32x4_t s[NT], s1[NT];  // two sums where there is one tile: the products of a sum wait for each other
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < NT; ++nt) s[nt] = s1[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < KPL; ++j)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) s[nt] = paged_mfma4(kx.get(j), qv[nt][j], s[nt]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (NT == 1 && (j & 1)) s1[nt] = paged_mfma4(kx.get(j), qv[nt][j], s1[nt]);
+                    else s[nt] = paged_mfma4(kx.get(j), qv[nt][j], s[nt]);
+                }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+                if (NT == 1) s[nt] += s1[nt];
+            u = next(u + 1, page);
+            if (u < part.u1) load_k(u, page);  // under this unit's softmax and P V
             float p[NT][4], mx[NT], vf[4][DT];
             const bool all_see = t + 16 <= least;
             bool need = false;
@@ -148,7 +165,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = SCALED ? s[nt][i] * paged_scale(ks, i) : s[nt][i];
+                    const float x = SCALED ? s[nt][i] * paged_scale(ksc, i) : s[nt][i];
                     p[nt][i] = t + 4 * lg + i < seen[nt] ? x : kNegInf;
                 }
                 mx[nt] = fmaxf(fmaxf(p[nt][0], p[nt][1]), fmaxf(p[nt][2], p[nt][3]));
@@ -187,6 +204,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
                     if (!all_see) odd |= strange(vf[i][dt]);
                 }
             }
+            // 8-bit values have been widened into other registers: the next ones come
+            // under the products, float32 ones under the next scores
+            if (SCALED && u < part.u1) load_v(u, page);
             auto products = [&]() {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -224,6 +244,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void paged_f32_kernel(PagedAr
                         }
                     }
             }
+            if (!SCALED && u < part.u1) load_v(u, page);
         }
 
         // ---- merge of the four waves; lane: row l % 16 of tile nt, d = D/4 (l / 16) + DT j + dt ----
