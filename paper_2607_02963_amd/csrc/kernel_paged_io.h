@@ -2,9 +2,9 @@
 // attention results.
 //
 // All three move memory: a row in, a row out, a few operations per element.
-// 16-byte accesses; the sequence of a row is found once per wave by counting
-// the offsets at or below it (64 at a time, one memory round trip for up to 64
-// sequences, where a binary search would take one per halving).
+// 16-byte accesses; the sequence of a row is found once per wave by counting the
+// offsets at or below it, 64 places at a time: one memory round trip for up to 64
+// sequences, two for up to 4096.
 #pragma once
 
 #include "kernel_mfma.h"
@@ -27,18 +27,19 @@ struct PagedIoArgs {
     int page_shift, num_pages, max_pages, max_len;
 };
 
-// Sequence of row t (uniform over the wave): the last s with cu[s] <= t among
-// those with rows, or -1 for a row behind the last sequence's.
+// Sequence of row t (uniform over the wave): as many whole sequences lie before it as
+// ends cu[s + 1] at or below t; -1 for a row behind the last sequence's.
 __device__ inline int paged_owner(const PagedIoArgs& a, int t)
 {
     const int lane = paged_lane();
-    int below = 0;  // ends cu[s + 1] at or below t: as many whole sequences lie before it
-    for (int s0 = 0; s0 < a.num_seqs; s0 += 64) {
-        const int s = s0 + lane;
-        const uint64_t b = __ballot(s < a.num_seqs && a.cu[s + 1] <= t);
-        below += __builtin_popcountll(b);
-        if (~b) break;
+    int lo = 0, n = a.num_seqs;  // the number is in [lo, lo + n]
+    while (n > 64) {
+        const int step = (n + 63) / 64, i = lo + (lane + 1) * step;
+        const int c = __builtin_popcountll(__ballot(i <= lo + n && a.cu[min(i, a.num_seqs)] <= t));
+        lo += c * step;
+        n = min(step, n - c * step);
     }
+    const int below = lo + __builtin_popcountll(__ballot(lane < n && a.cu[min(lo + lane + 1, a.num_seqs)] <= t));
     return below < a.num_seqs ? below : -1;
 }
 

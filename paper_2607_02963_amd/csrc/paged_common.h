@@ -139,18 +139,33 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             }
             return x;
         };
-        // a lane's pair: its sequence, and its price
+        // A lane's pair, or where there are many its sequence with all its groups: most of
+        // a mixed batch's sequences have one group of as many as the longest chunk's bound
+        // allows.  (200 sequences, one of 2048 new tokens: 335 us by pairs, 231 by
+        // sequences; 6 chunks in 168 pairs: 455 and 465.)
+        const bool by_seq = J > 512;
+        const int items = by_seq ? a.num_seqs : J;
         PagedSeq x = {0, 0, 0};
         auto cost = [&](int k) {
-            if (k >= J) return 0;
-            const int s = k / a.groups;
-            x = paged_seq(a, s);
-            const int n = paged_units_of(a, x, k - s * a.groups);
-            return n > 0 ? n + a.pad : 0;
+            if (k >= items) return 0;
+            if (!by_seq) {
+                const int s = k / a.groups;
+                x = paged_seq(a, s);
+                const int n = paged_units_of(a, x, k - s * a.groups);
+                return n > 0 ? n + a.pad : 0;
+            }
+            x = paged_seq(a, k);
+            int n = 0;
+            for (int g = 0; g < a.groups; ++g) {
+                const int u = paged_units_of(a, x, g);
+                if (u == 0) break;
+                n += u + a.pad;
+            }
+            return n;
         };
         int total = 0, n = cost(lane), incl = scan(n);
         total = __builtin_amdgcn_readlane(incl, 63);
-        for (int j0 = 64; j0 < J; j0 += 64) total += __builtin_amdgcn_readlane(scan(cost(j0 + lane)), 63);
+        for (int j0 = 64; j0 < items; j0 += 64) total += __builtin_amdgcn_readlane(scan(cost(j0 + lane)), 63);
         const int workers = min(a.workers, max(total * sets / a.least, 1));
         if (w >= workers || total == 0) return false;
         r.per = total * sets / workers;
@@ -159,24 +174,43 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
         r.left = r.per + (w < r.more ? 1 : 0);
         r.head = r.pos / total;
         int rest = r.pos - r.head * total, j0 = 0;
-        if (J > 64) incl = scan(n = cost(lane));
+        if (items > 64) incl = scan(n = cost(lane));
         while (true) {
             const int all = __builtin_amdgcn_readlane(incl, 63);  // scalar, as everything that leaves the loop
             if (rest < all) break;
             rest -= all;
             j0 += 64;
+            if (j0 >= items) return false;  // lengths that changed under the call
             incl = scan(n = cost(j0 + lane));
         }
-        const int at = __builtin_ctzll(__ballot(incl > rest));
-        j = j0 + at;
-        r.u = rest - __builtin_amdgcn_readlane(incl - n, at);
-        r.s = j / a.groups;
-        r.group = j - r.s * a.groups;
+        int at = __builtin_ctzll(__ballot(incl > rest));
+        rest -= __builtin_amdgcn_readlane(incl - n, at);
         r.seq.t0 = __builtin_amdgcn_readlane(x.t0, at);
         r.seq.n = __builtin_amdgcn_readlane(x.n, at);
         r.seq.L = __builtin_amdgcn_readlane(x.L, at);
-        r.units = __builtin_amdgcn_readlane(n, at) - a.pad;
-        return true;
+        if (!by_seq) {
+            j = j0 + at;
+            r.s = j / a.groups;
+            r.group = j - r.s * a.groups;
+            r.u = rest;
+            r.units = __builtin_amdgcn_readlane(n, at) - a.pad;
+            return true;
+        }
+        r.s = j0 + at;
+        for (int g0 = 0; g0 < a.groups; g0 += 64) {  // a lane per group
+            const int u = g0 + lane < a.groups ? paged_units_of(a, r.seq, g0 + lane) : 0, c = u > 0 ? u + a.pad : 0;
+            const int upto = scan(c), all = __builtin_amdgcn_readlane(upto, 63);
+            if (rest >= all) {
+                rest -= all;
+                continue;
+            }
+            at = __builtin_ctzll(__ballot(upto > rest));
+            r.group = g0 + at;
+            r.u = rest - __builtin_amdgcn_readlane(upto - c, at);
+            r.units = __builtin_amdgcn_readlane(u, at);
+            return true;
+        }
+        return false;
     }
     r.s = j / a.groups;
     r.group = j - r.s * a.groups;
@@ -186,8 +220,9 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
     return r.units > 0;
 }
 
-// The next part of the run; false at its end.  (No branch here is by the lane:
-// one inside the loop would make everything that leaves it a vector value.)
+// The next part of the run; false at its end.  (All that leaves the loop is scalar
+// and no store is by the lane: one inside the loop would make everything that
+// leaves it a vector value.)
 __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
 {
     const int pad = a.whole ? 0 : a.pad, sets = a.H_kv / a.heads;
@@ -196,7 +231,7 @@ __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
             r.u = 0;
             ++r.group;
             if (r.group >= a.groups || (r.units = paged_units_of(a, r.seq, r.group)) == 0) {
-                // the next sequence's first group
+                // the next sequence's first group; behind one that has none, 64 sequences at a time
                 r.group = 0;
                 if (++r.s >= a.num_seqs) {
                     r.s = 0;
@@ -204,6 +239,11 @@ __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
                 }
                 r.seq = paged_seq(a, r.s);
                 r.units = paged_units_of(a, r.seq, 0);
+                if (r.units == 0) {
+                    const int k = r.s + paged_lane();
+                    const uint64_t b = __ballot(k < a.num_seqs && paged_units_of(a, paged_seq(a, min(k, a.num_seqs - 1)), 0) > 0);
+                    r.s += b ? __builtin_ctzll(b) - 1 : 63;  // the one before it
+                }
             }
         }
         const int take = min(r.left, r.units + pad - r.u);

@@ -95,6 +95,33 @@ def test_append_counts_of_more_sequences_than_tokens():
     assert where == [[int(s), int(lens[s])] for s in np.nonzero(np.diff(cu))[0]]
 
 
+@pytest.mark.parametrize("S", [65, 500, 5000])
+def test_append_and_read_of_many_sequences(S):
+    """Every token finds its sequence among many, some without tokens."""
+    rng = np.random.default_rng(S)
+    n = rng.integers(0, 4, S)
+    n[:3], n[-2:] = 0, 0
+    cu = np.concatenate([[0], np.cumsum(n)])
+    T = int(cu[-1])
+    before = rng.integers(0, 12, S)
+    k = torch.zeros((S, 16, 1, 64), device="cuda")
+    v = torch.zeros_like(k)
+    new = torch.arange(1, T + 1, dtype=torch.float32).view(T, 1, 1).expand(T, 1, 64).contiguous().cuda()
+    table, lens = i32(rng.permutation(S)[:, None]), torch.zeros(S, dtype=torch.int32, device="cuda")
+    pdec.paged_kv_append(new, -new, k, v, table, i32(cu), i32(before), lens)
+    assert lens.tolist() == (before + n).tolist()
+    want = torch.zeros(S, 16)
+    tab = table[:, 0].tolist()
+    for s in range(S):
+        for i in range(n[s]):
+            want[tab[s], before[s] + i] = cu[s] + i + 1
+    assert torch.equal(k[:, :, 0, 7].cpu(), want) and torch.equal(v[:, :, 0, 63].cpu(), -want)
+    rows = np.concatenate([[0], np.cumsum(before + n)])
+    kd, vd = pdec.paged_kv_read(k, v, table, lens, i32(rows), num_rows=int(rows[-1]))
+    flat = np.concatenate([want[tab[s], :before[s] + n[s]].numpy() for s in range(S)])
+    assert np.array_equal(kd[:, 0, 3].cpu().numpy(), flat) and np.array_equal(vd[:, 0, 3].cpu().numpy(), -flat)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_quantisation_of_hard_rows(dtype, D):

@@ -72,6 +72,21 @@ def test_many_sequences(dtype, cache):
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("S,where", [(70, (0, 69)), (200, (3, 150)), (300, (299,)), (400, ())])
+def test_a_few_chunks_among_many_single_tokens(dtype, cache, S, where):
+    """Chunks of up to 600 tokens at a few places of a batch of single tokens and of sequences without any."""
+    rng = np.random.default_rng(S)
+    n = [int(rng.integers(0, 2)) for _ in range(S)]
+    lens = [int(rng.integers(max(a, 1), 60)) for a in n]
+    for k, s in enumerate(where):
+        n[s], lens[s] = (600, 37)[k % 2], (600, 900)[k % 2]
+    c = Paged(n, lens, 14, 2, 64, 16, dtype, cache, seed=S)
+    for kw in ({}, {"max_chunk": max(n), "max_len": max(lens)}):
+        out, lse = c.attn(**kw)
+        compare(dtype, out, lse, c.reference(), f"{dtype}/{cache} {kw}")
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("causal", [True, False])
 def test_absent_pages_and_rows_that_see_nothing(dtype, cache, causal):
     """Pages missing at the start, in the middle, everywhere; more new tokens than keys."""
