@@ -547,8 +547,8 @@ int pdec_attn_prefill_backward(const pdec_dims* dims, const void* q, const void*
  * PDEC_DEBUG=1 the calls check them (pdec_check_paged_lengths), synchronising.
  */
 typedef struct pdec_paged_dims {
-    int32_t num_seqs;     /* S >= 1                                                              */
-    int32_t num_tokens;   /* rows of q/out/lse (of k_new/v_new), >= 1                            */
+    int32_t num_seqs;     /* S, 1..2^27                                                          */
+    int32_t num_tokens;   /* rows of q/out/lse (of k_new/v_new), 1..2^27                         */
     int32_t num_q_heads;  /* H_q, a multiple of num_kv_heads                                     */
     int32_t num_kv_heads; /* H_kv                                                                */
     int32_t head_dim;     /* D: 64 or 128                                                        */

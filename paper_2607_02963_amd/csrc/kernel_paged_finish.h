@@ -28,7 +28,8 @@ __global__ __launch_bounds__(64 * (W > 1 ? W : kPagedFinishRows)) void paged_fin
     // pairs that do not exist have no note
     if (a.by_pair && paged_units(a, blockIdx.x % J) == 0) return;
     const int4 cut = a.cut[blockIdx.x];
-    if (cut.x < 0) return;
+    // not cut; or (lengths outside the contract) a note that nobody wrote
+    if (cut.x < 0 || cut.y < cut.x || cut.y >= a.workers || (uint32_t)cut.z >= (uint32_t)J || (uint32_t)cut.w >= (uint32_t)(a.H_kv / a.heads)) return;
     const int s = cut.z / a.groups, row0 = (cut.z - s * a.groups) * a.rows;
     const PagedSeq sq = paged_seq(a, s);
     if (r >= min(a.rows, sq.n * a.G - row0)) return;  // W > 1: the whole work-group, which has one row

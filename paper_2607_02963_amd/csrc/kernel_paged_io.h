@@ -127,11 +127,26 @@ __device__ inline void paged_place(const PagedIoArgs& a, int r0, bool before, Pa
     int s = r0 < a.num_tokens ? paged_owner(a, r0) : -1;
     if (s >= 0 && r < a.num_tokens) {
         int first = a.cu[s], end = a.cu[s + 1], len = a.lens[s];
-        while (r >= end) {  // the row of a later sequence
-            if (++s >= a.num_seqs) break;
-            first = end;
-            end = a.cu[s + 1];
-            len = a.lens[s];
+        if (r >= end) {  // a later sequence's: the first that ends behind r, mostly the next
+            int hi = a.num_seqs;
+            for (int step = 1; ++s < hi; step *= 2) {
+                const int at = min(s + step - 1, hi - 1);
+                if (a.cu[at + 1] > r) {
+                    hi = at;
+                    break;
+                }
+                s = at;
+            }
+            while (s < hi) {
+                const int mid = s + (hi - s) / 2;
+                if (a.cu[mid + 1] > r) hi = mid;
+                else s = mid + 1;
+            }
+            if (s < a.num_seqs) {
+                first = a.cu[s];
+                end = a.cu[s + 1];
+                len = a.lens[s];
+            }
         }
         if (s < a.num_seqs && r >= first && first >= 0) {
             int key = r - first;

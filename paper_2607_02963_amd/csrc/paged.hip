@@ -5,7 +5,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <vector>
+#include <memory>
+#include <new>
 
 #include "pdec.h"
 
@@ -67,6 +68,9 @@ using namespace pdec;
 
 bool aligned(const void* p, uintptr_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Rows of a call, and sequences: the launches' threads stay within 32 bits.
+constexpr int kMostRows = 1 << 27;
+
 int check_dims(const pdec_paged_dims* d)
 {
     if (!d) return PDEC_ERR_INVALID_ARG;
@@ -80,6 +84,7 @@ int check_dims(const pdec_paged_dims* d)
     if (d->head_dim != 64 && d->head_dim != 128) return PDEC_ERR_UNSUPPORTED;
     if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
         return PDEC_ERR_UNSUPPORTED;
+    if (d->num_tokens > kMostRows || d->num_seqs > kMostRows) return PDEC_ERR_UNSUPPORTED;
     const int64_t most = (int64_t)d->max_pages * d->page_size;
     if (most > ((int64_t)1 << 30)) return PDEC_ERR_UNSUPPORTED;
     if (d->max_len > most) return PDEC_ERR_INVALID_ARG;
@@ -124,6 +129,7 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int 
     a.whole = units <= kWholeUnits ? 1 : 0;
     a.by_pair = pairs <= workers ? 1 : 0;
     a.blocks = a.whole ? (int)((pairs + 7) / 8 * 8) : workers;
+    if ((int64_t)a.blocks * 512 > UINT32_MAX) return false;  // threads of the launch
     *bytes = 0;
     if (!a.whole)
         *bytes = align256((size_t)workers * sizeof(int4)) + align256((size_t)2 * workers * a.heads * a.rows * 2 * sizeof(float)) +
@@ -196,13 +202,14 @@ bool cache_pointers(const pdec_paged_dims* d, const void* k, const void* v, cons
 // PDEC_DEBUG=1: the lengths of a call, copied and checked (synchronises).
 int debug_check(const pdec_paged_dims* d, const int32_t* cu, const int32_t* lens, int attn, void* stream)
 {
-    std::vector<int32_t> c((size_t)d->num_seqs + 1), l((size_t)d->num_seqs);
+    const size_t S = (size_t)d->num_seqs;
+    const std::unique_ptr<int32_t[]> c(new (std::nothrow) int32_t[2 * S + 1]);  // no exception leaves a C entry
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (hipMemcpyAsync(c.data(), cu, c.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
-        hipMemcpyAsync(l.data(), lens, l.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+    if (!c || hipMemcpyAsync(c.get(), cu, (S + 1) * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+        hipMemcpyAsync(c.get() + S + 1, lens, S * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
         hipStreamSynchronize(s) != hipSuccess)
         return PDEC_ERR_HIP;
-    return pdec_check_paged_lengths(d, c.data(), l.data(), attn);
+    return pdec_check_paged_lengths(d, c.get(), c.get() + S + 1, attn);
 }
 
 PagedIoArgs io_args(const pdec_paged_dims* d)
@@ -397,8 +404,8 @@ int pdec_merge_states(int64_t num_rows, int32_t head_dim, int32_t dtype, const v
         return PDEC_ERR_INVALID_ARG;
     if (dtype != PDEC_DTYPE_F32 && dtype != PDEC_DTYPE_BF16) return PDEC_ERR_UNSUPPORTED;
     if (head_dim != 64 && head_dim != 128) return PDEC_ERR_UNSUPPORTED;
-    const int64_t blocks = (num_rows * (head_dim / 8) + 255) / 256;
-    if (num_rows > ((int64_t)1 << 40) || blocks > INT32_MAX) return PDEC_ERR_UNSUPPORTED;
+    const int64_t blocks = (std::min<int64_t>(num_rows, (int64_t)1 << 33) * (head_dim / 8) + 255) / 256;
+    if (num_rows > ((int64_t)1 << 32) || blocks * 256 > UINT32_MAX) return PDEC_ERR_UNSUPPORTED;  // threads of the launch
     const dim3 grid((unsigned)blocks), block(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool f32 = dtype == PDEC_DTYPE_F32;

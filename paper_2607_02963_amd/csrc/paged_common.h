@@ -271,7 +271,7 @@ __device__ inline void paged_note(const PagedArgs& a, const PagedRun& r, const P
     if (a.whole || p.u0 > 0) return;
     const int j = p.s * a.groups + p.group;
     const int at = p.end - 1, first = r.more * (r.per + 1);  // the work-group of the pair's last position
-    const int last = at < first ? at / (r.per + 1) : r.more + (at - first) / r.per;
+    const int last = min(at < first ? at / (r.per + 1) : r.more + (at - first) / r.per, a.workers - 1);
     const int4 cut = make_int4(p.whole ? -1 : r.w, last, j, p.head);
     if (a.by_pair) a.cut[p.head * a.num_seqs * a.groups + j] = cut;
     else if (!p.whole) a.cut[r.w] = cut;

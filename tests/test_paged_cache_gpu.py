@@ -29,6 +29,8 @@ CASES = [  # n, keys before, H_kv, D, page
     ([300], [17], 8, 64, 128),
     ([70, 130], [1, 30], 3, 128, 32),
     ([0, 2], [5, 1023], 24, 64, 1024),
+    ([1030, 0, 1, 2, 0, 0, 1015], [7, 3, 63, 127, 0, 9, 0], 4, 128, 64),  # four tokens to a wave
+    ([3, 2100], [900, 5], 10, 64, 16),
 ]
 
 
@@ -80,6 +82,31 @@ def test_append_leaves_what_does_not_fit_and_drops_rows_without_a_page():
     lens_out.zero_()
     pdec.paged_kv_append(new, new, k, v, table, i32([0, 5, 7, 11, 14]), i32([0, 0, 0, 0]), lens_out, max_len=4)
     assert lens_out.tolist() == [0, 2, 4, 3]
+
+
+def test_cache_calls_of_a_batch_padded_with_empty_sequences():
+    """3000 sequences, tokens in the first, one in the middle and the last, rows behind them all."""
+    S, T = 3000, 2600
+    n, lens = np.zeros(S, int), np.zeros(S, int)
+    n[0], n[1700], n[-1] = 1501, 402, 600
+    lens[1700] = 11
+    cu, cols = np.concatenate([[0], np.cumsum(n)]), 100
+    table = np.full((S, cols), -1)
+    pages = iter(np.random.default_rng(3).permutation(400))
+    for s in (0, 1700, S - 1):
+        table[s, :-(-(n[s] + lens[s]) // 16)] = [next(pages) for _ in range(-(-(n[s] + lens[s]) // 16))]
+    k = torch.zeros((400, 16, 1, 64), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    new = new_rows(T, 1, 64, "bf16", 5).cuda()
+    after = torch.zeros(S, dtype=torch.int32, device="cuda")
+    pdec.paged_kv_append(new, -new, k, v, i32(table), i32(cu), i32(lens), after)
+    assert after.tolist() == (lens + n).tolist()
+    rows = np.concatenate([[0], np.cumsum(lens + n)])
+    out = [torch.full((T + 20, 1, 64), 3.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    pdec.paged_kv_read(k, v, i32(table), after, i32(rows), k_out=out[0], v_out=out[1])
+    want = torch.cat([new[:1501], torch.zeros_like(new[:11]), new[1501:2503]])
+    assert torch.equal(out[0][:2514], want) and torch.equal(out[1][:2514], torch.where(want == 0, want, -want))
+    assert (out[0][2514:] == 3).all() and (out[1][2514:] == 3).all()
 
 
 def test_append_counts_of_more_sequences_than_tokens():

@@ -166,6 +166,72 @@ def test_calls_agree_bit_for_bit_whatever_the_workspace_holds(dtype, cache):
     assert none is None and torch.equal(bits(o1), bits(o4))
 
 
+@pytest.mark.parametrize("n,H_q,H_kv,D,dtype,cache,few,many", [
+    (3, 8, 2, 64, "bf16", "bf16", 16, 0), (3, 12, 3, 64, "bf16", "bf16", 16, 0), (4, 14, 2, 64, "bf16", "e4m3", 32, 0),
+    (4, 7, 1, 64, "bf16", "e4m3", 32, 0), (11, 8, 2, 64, "bf16", "bf16", 48, 0), (11, 12, 3, 64, "bf16", "e4m3", 48, 0),
+    (11, 8, 2, 128, "bf16", "bf16", 64, 0), (9, 14, 2, 128, "bf16", "e4m3", 64, 0), (9, 21, 3, 128, "bf16", "e4m3", 64, 0),
+    (16, 12, 3, 64, "bf16", "bf16", 64, 0), (16, 8, 2, 64, "bf16", "e4m3", 64, 0), (2, 14, 2, 128, "bf16", "e4m3", 16, 0),
+    (4, 21, 3, 128, "bf16", "bf16", 32, 0), (17, 12, 3, 128, "bf16", "bf16", 64, 128), (31, 8, 2, 64, "bf16", "e4m3", 64, 128),
+    (33, 12, 3, 64, "bf16", "bf16", 64, 256), (70, 14, 2, 128, "bf16", "e4m3", 64, 256),
+    (2, 8, 2, 64, "f32", "f32", 16, 0), (40, 8, 2, 128, "f32", "e4m3", 32, 0)])
+@pytest.mark.parametrize("lens", [[200], [2900], [250, 70, 130], [900, 2900, 70], [100] * 20])
+def test_every_kernel_of_the_plan(n, H_q, H_kv, D, dtype, cache, few, many, lens):
+    """The rows per item that a chunk gets, whole pairs and cut ones, one state or many to a pair."""
+    ns = [n] + [1 + (5 * i) % n for i in range(1, len(lens))]
+    c = Paged(ns, lens, H_q, H_kv, D, 32, dtype, cache, seed=n).put()
+    dims = pdec.paged_dims_of(c.dev["q"], c.dev["k_pages"], c.dev["block_table"], max_chunk=n, max_len=max(lens))
+    plan = pdec.query_paged_plan(dims)
+    assert (plan["rows_few"], plan["rows_many"]) == (few if not many or len(lens) > 1 else 0, many)
+    assert plan["merge_pass"] == (max(lens) > 256)
+    out, lse = c.attn(max_chunk=n, max_len=max(lens))
+    compare(dtype, out, lse, c.reference(), f"{lens}")
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("page", [64, 256])
+def test_holes_under_many_rows(dtype, cache, page):
+    """Pages of whole stages absent at the front, inside and at the end, under chunks with rows in every tile."""
+    n, lens = [40, 300, 9], [2000, 1700, 1500]
+    absent = {(0, 0), (1, 0), (1, 1), (1, 3), (1, 1600 // page), (2, 0), (2, 2)}
+    c = Paged(n, lens, 14, 2, 128, page, dtype, cache, seed=21, absent=absent)
+    for causal in (True, False):
+        out, lse = c.attn(causal=causal)
+        compare(dtype, out, lse, c.reference(causal), f"{dtype}/{cache} {page} {causal}")
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_two_calls_at_once(dtype, cache):
+    """Calls under way on two streams, each with a workspace of its own, have the bits that each has alone."""
+    cs = [Paged([1, 70], [1500, 2600], 14, 2, 128, 64, dtype, cache, seed=22).put(),
+          Paged([5] * 6, [800, 90, 2100, 5, 64, 700], 14, 2, 128, 64, dtype, cache, seed=23).put()]
+    want = [[x.clone() for x in c.attn()] for c in cs]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in cs], []
+    for _ in range(5):
+        for c, st in zip(cs, streams):
+            got.append((c, c.attn(stream=st)))
+    torch.cuda.synchronize()
+    for c, g in got:
+        for x, y in zip(want[cs.index(c)], g):
+            assert torch.equal(bits(x), bits(y))
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_lengths_outside_the_contract_stay_inside_the_arrays(dtype, cache):
+    """Negative, decreasing and too large lengths; sequences 0 and 4 are right, and so are their rows; rows that
+    nobody has stay."""
+    c = Paged([3, 2, 2, 2, 70], [300, 40, 40, 40, 400], 14, 2, 64, 16, dtype, cache, seed=24, pad=4).put()
+    want, ref = [x.clone() for x in c.attn()], c.reference()
+    good = list(range(3)) + list(range(9, 79))
+    cu, lens = [0, 3, 5, 4, 9, 79], [300, -7, 2 ** 31 - 1, 10 ** 6, 400]
+    c.dev["cu_tokens"], c.dev["seq_lens"] = c.i32(cu), c.i32(lens)
+    out, lse = torch.full_like(want[0], 7.0), torch.full_like(want[1], 7.0)
+    c.attn(out=out, lse=lse)
+    # other lengths divide the work elsewhere, so sums associate otherwise: within the bounds, not the same bits
+    compare(dtype, out[good], lse[good], [x[good] for x in ref], "rows of the right sequences")
+    assert (out[79:] == 7).all() and (lse[79:] == 7).all()
+
+
 def test_a_pool_beyond_32_bit_offsets():
     """Pages behind 4 GiB of a pool: 70000 pages of 64 KiB."""
     P, page, H_kv, D = 70000, 64, 4, 128

@@ -24,7 +24,7 @@ BAD = [dict(num_seqs=0), dict(num_tokens=0), dict(H_q=27), dict(H_q=0), dict(H_k
        dict(num_pages=0), dict(max_pages=0), dict(max_pages=1 << 25), dict(max_chunk=-1), dict(max_len=-1),
        dict(max_len=128 * 64 + 1), dict(dtype_code=E4M3), dict(dtype_code=7), dict(cache_code=F32),
        dict(dtype_code=F32), dict(causal=2), dict(causal=-1), dict(scale=float("nan")), dict(scale=float("inf")),
-       dict(H_kv=1 << 16, H_q=1 << 16)]
+       dict(H_kv=1 << 16, H_q=1 << 16), dict(num_tokens=(1 << 27) + 1), dict(num_seqs=(1 << 27) + 1)]
 
 
 @pytest.mark.parametrize("kw", BAD, ids=str)
@@ -86,8 +86,17 @@ def test_merge_refusals():
     L = pdec.lib()
     names = ["out_a", "lse_a", "out_b", "lse_b", "out", "lse"]
     _each_pointer(lambda a: L.pdec_merge_states(10, 128, BF16, *a, None), names, {"lse"})
-    for n, D, t in ((0, 128, BF16), (-1, 128, BF16), (10, 96, BF16), (10, 128, E4M3), (10, 128, 9), (1 << 41, 128, BF16)):
+    for n, D, t in ((0, 128, BF16), (-1, 128, BF16), (10, 96, BF16), (10, 128, E4M3), (10, 128, 9), (1 << 41, 128, BF16),
+                    ((1 << 28) + 1, 128, BF16), ((1 << 29) + 1, 64, F32), ((1 << 63) - 1, 128, F32)):
         assert L.pdec_merge_states(n, D, t, *FAKE[:6], None) in (pdec.PDEC_ERR_INVALID_ARG, pdec.PDEC_ERR_UNSUPPORTED)
+
+
+@pytest.mark.parametrize("kw", [dict(num_seqs=1 << 25, max_len=64, max_chunk=1), dict(num_seqs=1 << 27, max_chunk=1),
+                                dict(num_tokens=1 << 27, max_pages=1 << 20), dict(num_seqs=1 << 20, num_tokens=1 << 20)])
+def test_more_work_than_a_launch_counts_is_refused(kw):
+    d = dims(**kw)
+    assert pdec.paged_workspace_size(d) == 0
+    assert pdec.lib().pdec_paged_attn(ctypes.byref(d), *FAKE[:11], 1 << 40, None) == pdec.PDEC_ERR_UNSUPPORTED
 
 
 def test_length_check():
