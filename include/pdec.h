@@ -609,8 +609,8 @@ size_t pdec_paged_workspace_size(const pdec_paged_dims* dims);
 /* The kernels a pdec_paged_attn call uses, for tests and measurement. */
 typedef struct pdec_paged_plan {
     int32_t rows_few;   /* rows (new tokens x H_q / H_kv) per work item of the kernel for      */
-                        /* sequences of few rows; 0: not launched                              */
-    int32_t rows_many;  /* the same of the kernel for many rows; 0: not launched               */
+                        /* sequences of few rows, 16, 32, 48 or 64; 0: not launched            */
+    int32_t rows_many;  /* the same of the kernel for many rows, 128 or 256; 0: not launched   */
     int32_t workers;    /* work-groups that share the keys of each of the two                  */
     int32_t merge_pass; /* 1 if partial states are merged by a pass of their own               */
 } pdec_paged_plan;

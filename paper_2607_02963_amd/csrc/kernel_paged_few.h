@@ -2,13 +2,22 @@
 // drafted tokens, short chunks), bfloat16, on v_mfma_f32_16x16x32_bf16.
 //
 // What bounds it: the bytes of the pages.  A key meets 16 NT rows at most, so
-// nothing is shared between waves: each of a work-group's four waves takes every
-// fourth 32-key block of the part through a ring of its own in LDS (32 KB,
-// filled by global_load_lds_dwordx4), with a softmax state of its own, and never
-// waits for another wave until the four states are joined at the part's end.
-// A block's 16-key halves are each on one page: a scalar base and fixed lane
-// offsets per half, the pages of the block after the ring's read one block ahead.
-// 128 KB in flight per compute unit is more than the latency of the memory asks.
+// nothing is shared between waves: each of a work-group's eight waves takes every
+// eighth 32-key block of the part (of its head's waves' blocks) through a ring of
+// its own in LDS (16 KB, filled by global_load_lds_dwordx4), with a softmax state
+// of its own, and never waits for another wave until the states are joined at the
+// part's end.  A block's 16-key halves are each on one page: a scalar base and
+// fixed lane offsets per half, the pages of the block after the ring's read one
+// block ahead.  128 KB in flight per compute unit is more than the latency of the
+// memory asks; two waves to a SIMD hide each other's products and exponentials.
+// One token of each of 32 sequences over 8-bit pages (291 MB): 62 us, 4.7 TB/s with
+// the finish pass; one over 32768 bfloat16 keys (67 MB) 21.6 us, 3.1 TB/s, of which
+// the passes' starts and ends are about 8.
+//
+// Up to 32 rows at D = 128 and 64 at D = 64: above, 64 rows' accumulators leave a
+// SIMD one wave at D = 128, and the kernel for many rows, which shares its keys over
+// its waves, is as fast or faster from there (13 sequences of 35 rows of 128 47.7
+// against 39.9 us, of 56 rows 53.8 against 41.7; 64 rows of 64 48.4 against 51.7).
 //
 // Per block, products and layouts as in the decode step (kernel_mfma.h):
 //   S^T  = K  Q^T    A = 16 keys x 32 d from LDS, B = Q^T (registers)
@@ -79,14 +88,17 @@ __device__ inline void dma_rows(uint64_t base, const uint32_t (&off)[N], uint32_
         static_assert(N == 4, "instructions of a half");
         asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
                      "global_load_lds_dwordx4 %4, %2 offset:1024\n\tglobal_load_lds_dwordx4 %5, %2 offset:2048\n\t"
-                     "global_load_lds_dwordx4 %6, %2 offset:3072\n\ts_mov_b64 exec, -1" :
+                     "global_load_lds_dwordx4 %6, %2 offset:0xc00\n\ts_mov_b64 exec, -1" :
                      : "s"(m), "s"(ln), "s"(sb), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory");
     }
 }
 
-template <int D, int NT, bool FP8, int NW, int HW>
-__global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
+constexpr int kFewWaves = 8;  // of a work-group
+
+template <int D, int NT, bool FP8, int HW>
+__global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedArgs a)
 {
+    constexpr int NW = kFewWaves;
     constexpr int RT = 16 * NT;
     constexpr int NK = NW / HW;                  // waves that share a head's keys
     constexpr int RING = 131072 / NW;            // bytes of a wave's ring
@@ -100,11 +112,10 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
     constexpr int PB = 4 * PPH + (FP8 ? 1 : 0);  // and per block, its scales with them
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
-    constexpr int MT = NT < 2 || NW == 8 ? 1 : 2;  // tiles merged at a time
     static_assert((NS - 1) * PB < 64, "the wait counts them");
-    static_assert(NW * 16 * MT * OROW * 4 <= NW * RING, "merge buffer");
+    static_assert(16 * OROW * 4 <= RING, "merge buffer");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + (FP8 ? NW * NS * 64 : 0)];
-    __shared__ float m_s[NW][16 * MT], l_s[NW][16 * MT];
+    __shared__ float m_s[NW][16], l_s[NW][16];
 
     const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
     const int wk = w / HW, wh = w % HW;  // the wave's blocks, and its head of the pair's
@@ -358,29 +369,25 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
             now = pages(min(b + 1, mine - 1));
         }
 
-        // ---- the four waves' states joined; lane: row l % 16 of tile nt, d = 16 dt + 4 (l / 16) + i ----
+        // ---- the waves' states joined, tile by tile; lane: row l % 16 of tile nt, d = 16 dt + 4 (l / 16) + i ----
         wait_vmcnt<0>();  // no DMA into the ring outlives the part
         float* const o_s = reinterpret_cast<float*>(lds);
 #pragma unroll
-        for (int n0 = 0; n0 < NT; n0 += MT) {
-            if (n0 >= tiles) break;
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt >= tiles) break;
             lds_barrier();  // the ring, or the tiles before, have been read
-#pragma unroll
-            for (int k = 0; k < MT; ++k) {
-                const int nt = n0 + k, r = 16 * k + l16;
-                float l = lsum[nt];
-                l += __shfl_xor(l, 16);
-                l += __shfl_xor(l, 32);
-                if (lg == 0) {
-                    m_s[w][r] = m_ref[nt];
-                    l_s[w][r] = l;
-                }
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-                    *reinterpret_cast<f32x4_t*>(o_s + (w * 16 * MT + r) * OROW + 16 * dt + 4 * lg) = o[nt][dt];
+            float l = lsum[nt];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (lg == 0) {
+                m_s[w][l16] = m_ref[nt];
+                l_s[w][l16] = l;
             }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                *reinterpret_cast<f32x4_t*>(o_s + (w * 16 + l16) * OROW + 16 * dt + 4 * lg) = o[nt][dt];
             lds_barrier();
-            const int rows = min(nrows - 16 * n0, 16 * MT);
+            const int rows = min(nrows - 16 * nt, 16);
             for (int i = 64 * w + lane; i < HW * rows * (D / 4); i += 64 * NW) {
                 const int r = i / (D / 4) % rows, d4 = i % (D / 4), hs = i / (D / 4) / rows;
                 float M = m_s[hs][r];
@@ -393,9 +400,9 @@ __global__ __launch_bounds__(64 * NW) void paged_few_kernel(PagedArgs a)
                     const int y = HW * x + hs;
                     const float f = fast_exp2(m_s[y][r] - M);  // 0 for a wave that saw none of the row's keys
                     L += f * l_s[y][r];
-                    acc += f * *reinterpret_cast<const f32x4_t*>(o_s + (y * 16 * MT + r) * OROW + 4 * d4);
+                    acc += f * *reinterpret_cast<const f32x4_t*>(o_s + (y * 16 + r) * OROW + 4 * d4);
                 }
-                const int row = 16 * n0 + r;
+                const int row = 16 * nt + r;
                 if (!part.whole) {
                     const long at = ((long)part.slot * HW + hs) * RT + row;
                     *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 4 * d4) = acc;

@@ -97,8 +97,9 @@ int chunk_bound(const pdec_paged_dims* d) { return d->max_chunk > 0 ? std::min(d
 int len_bound(const pdec_paged_dims* d) { return d->max_len > 0 ? d->max_len : d->max_pages * d->page_size; }
 int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
-// Sequences of at most so many rows per kv head are the few-row kernel's.
-constexpr int kFewRows = 64;
+// Sequences of at most so many rows per kv head are the few-row kernel's: up to two
+// 16-row tiles at D = 128, four at D = 64.
+int few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
 
 struct AttnPlan {
     PagedArgs few{}, many{};
@@ -170,22 +171,29 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     a.rows_to = INT32_MAX;
     a.heads = 1;
     p.few = p.many = a;
-    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > kFewRows;
-    // one sequence is the many rows' whatever its chunk; of several, each goes by its own
-    p.use_few = !p.use_many || d->num_seqs > 1;
+    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d->head_dim);
+    // One sequence is the many rows' whatever its chunk, and so are all where none has
+    // more rows than a 128-row item: a second kernel and its finish pass cost more than
+    // the rows left empty (24 sequences of 300 to 4000 keys, one of 16 new tokens and the
+    // others of one 35.1 us, with both kernels 49.7; 1 to 16 tokens 42.9 and 61.1).  Over
+    // 256-row items each goes by its own.
+    p.use_few = !p.use_many || (d->num_seqs > 1 && R > 128);
     if (p.use_many) {
+        // two 32-row tiles in each wave: a key read from LDS meets twice the rows
         p.many.rows = R <= 128 ? 128 : 256;
         if (p.use_few) {
-            p.many.rows_from = kFewRows + 1;
-            p.few.rows_to = kFewRows;
+            p.many.rows_from = few_rows(d->head_dim) + 1;
+            p.few.rows_to = few_rows(d->head_dim);
         }
+        // a work-group per compute unit; a start's price was swept (six chunks of 301 to 1023
+        // tokens, 8-bit and bfloat16: 3 526 and 480 us, 6 456 and 418, 9 464 and 421, 14 471 and 424)
         if (!divide(d, p.many, 256, 4, 6, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     if (p.use_few) {
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
         const bool f32 = d->dtype == PDEC_DTYPE_F32;
-        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : most <= 48 && d->head_dim == 64 ? 48 : 64;
-        // heads' rows of a cache line or half of one: two heads to a work-group
+        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : most <= 48 ? 48 : 64;
+        // heads' rows of a cache line or half of one: two heads to a work-group (kernel_paged_few.h)
         if (!f32 && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;
         if (!divide(d, p.few, f32 ? 512 : 256, 2, f32 ? 1 : 4, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
@@ -225,9 +233,10 @@ PagedIoArgs io_args(const pdec_paged_dims* d)
     return a;
 }
 
-// Tokens from which a wave of the append takes four.
+// Tokens from which a wave of the append takes four: 16384 tokens of 4 heads of 128 took
+// 15.3 us by one and take 12.0; up to 4096 both take the call's own 8.9.
 constexpr int kAppendMany = 2048;
-constexpr int kReadRows = 8;  // rows per wave of the read-back
+constexpr int kReadRows = 8;  // rows per wave of the read-back: 4 and 16 are slower
 
 template <int D, typename T, bool QUANT, int N>
 void launch_append(const PagedIoArgs& a, hipStream_t s)

@@ -20,13 +20,13 @@ void launch_rows(const PagedArgs& a, hipStream_t s)
 template <int D, bool FP8, int HW>
 void launch_few(const PagedArgs& a, hipStream_t s)
 {
-    // eight waves where the registers allow two on a SIMD
-    const dim3 grid((unsigned)a.blocks);
-    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8, 8, HW>), grid, dim3(512), 0, s, a);
-    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8, 8, HW>), grid, dim3(512), 0, s, a);
-    else if constexpr (D == 128) hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, 4, HW>), grid, dim3(256), 0, s, a);
-    else if (a.rows == 48) hipLaunchKernelGGL((paged_few_kernel<D, 3, FP8, 8, HW>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, 8, HW>), grid, dim3(512), 0, s, a);
+    const dim3 grid((unsigned)a.blocks), block(64 * kFewWaves);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few_kernel<D, 1, FP8, HW>), grid, block, 0, s, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((paged_few_kernel<D, 2, FP8, HW>), grid, block, 0, s, a);
+    else if constexpr (D == 64) {
+        if (a.rows == 48) hipLaunchKernelGGL((paged_few_kernel<D, 3, FP8, HW>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((paged_few_kernel<D, 4, FP8, HW>), grid, block, 0, s, a);
+    }
 }
 
 }  // namespace

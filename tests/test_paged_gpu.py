@@ -169,10 +169,10 @@ def test_calls_agree_bit_for_bit_whatever_the_workspace_holds(dtype, cache):
 @pytest.mark.parametrize("n,H_q,H_kv,D,dtype,cache,few,many", [
     (3, 8, 2, 64, "bf16", "bf16", 16, 0), (3, 12, 3, 64, "bf16", "bf16", 16, 0), (4, 14, 2, 64, "bf16", "e4m3", 32, 0),
     (4, 7, 1, 64, "bf16", "e4m3", 32, 0), (11, 8, 2, 64, "bf16", "bf16", 48, 0), (11, 12, 3, 64, "bf16", "e4m3", 48, 0),
-    (11, 8, 2, 128, "bf16", "bf16", 64, 0), (9, 14, 2, 128, "bf16", "e4m3", 64, 0), (9, 21, 3, 128, "bf16", "e4m3", 64, 0),
+    (11, 8, 2, 128, "bf16", "bf16", 0, 128), (9, 14, 2, 128, "bf16", "e4m3", 0, 128), (9, 21, 3, 128, "bf16", "e4m3", 0, 128),
     (16, 12, 3, 64, "bf16", "bf16", 64, 0), (16, 8, 2, 64, "bf16", "e4m3", 64, 0), (2, 14, 2, 128, "bf16", "e4m3", 16, 0),
-    (4, 21, 3, 128, "bf16", "bf16", 32, 0), (17, 12, 3, 128, "bf16", "bf16", 64, 128), (31, 8, 2, 64, "bf16", "e4m3", 64, 128),
-    (33, 12, 3, 64, "bf16", "bf16", 64, 256), (70, 14, 2, 128, "bf16", "e4m3", 64, 256),
+    (4, 21, 3, 128, "bf16", "bf16", 32, 0), (17, 12, 3, 128, "bf16", "bf16", 0, 128), (31, 8, 2, 64, "bf16", "e4m3", 0, 128),
+    (33, 12, 3, 64, "bf16", "bf16", 64, 256), (70, 14, 2, 128, "bf16", "e4m3", 32, 256),
     (2, 8, 2, 64, "f32", "f32", 16, 0), (40, 8, 2, 128, "f32", "e4m3", 32, 0)])
 @pytest.mark.parametrize("lens", [[200], [2900], [250, 70, 130], [900, 2900, 70], [100] * 20])
 def test_every_kernel_of_the_plan(n, H_q, H_kv, D, dtype, cache, few, many, lens):
