@@ -13,7 +13,9 @@
 // value's scale the value: powers of two, so neither rounds.
 //
 // What bounds it: for few rows the memory round trips and then the bytes of the
-// pages, for many the float32 products (145 TFLOP/s on this part).
+// pages (one token of 28 heads over 32768 keys 39 us; the next unit's keys and
+// values are under way while this one is worked on, 44 us without), for many the
+// float32 products (133 TFLOP/s in a large library product).
 #pragma once
 
 #include "kernel_mfma.h"

@@ -236,7 +236,7 @@ PagedIoArgs io_args(const pdec_paged_dims* d)
 // Tokens from which a wave of the append takes four: 16384 tokens of 4 heads of 128 took
 // 15.3 us by one and take 12.0; up to 4096 both take the call's own 8.9.
 constexpr int kAppendMany = 2048;
-constexpr int kReadRows = 8;  // rows per wave of the read-back: 4 and 16 are slower
+constexpr int kReadRows = 4;  // rows per wave of the read-back (32768 rows: 24.2 us, by 8 26.8, by 16 25.7)
 
 template <int D, typename T, bool QUANT, int N>
 void launch_append(const PagedIoArgs& a, hipStream_t s)

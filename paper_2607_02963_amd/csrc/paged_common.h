@@ -141,9 +141,11 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
         };
         // A lane's pair, or where there are many its sequence with all its groups: most of
         // a mixed batch's sequences have one group of as many as the longest chunk's bound
-        // allows.  (200 sequences, one of 2048 new tokens: 335 us by pairs, 231 by
-        // sequences; 6 chunks in 168 pairs: 455 and 465.)
-        const bool by_seq = J > 512;
+        // allows (200 sequences, one of 2048 new tokens: 335 us by pairs, 228 by sequences;
+        // 64, one of 1024: 128 and 107).  Few sequences of many groups each would keep a
+        // lane counting (one chunk of 32768 tokens, 896 groups: 7.67 and 7.80 ms; 64 chunks
+        // of 14 groups 544 and 561 us).
+        const bool by_seq = J > 1024 && a.num_seqs > 16;
         const int items = by_seq ? a.num_seqs : J;
         PagedSeq x = {0, 0, 0};
         auto cost = [&](int k) {
