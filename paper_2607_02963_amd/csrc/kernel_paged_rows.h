@@ -26,8 +26,8 @@
 //
 // What bounds it: the matrix cores, with the softmax beside them, as for whole
 // branches: 2048 tokens over 32768 keys, 28 heads of 128 over 4 (932 GFLOP) take
-// 950 us, 980 TFLOP/s of the 1241 that a large library product reaches; six chunks
-// of 301 to 1023 tokens over 8-bit pages 457 us, 788 TFLOP/s, the difference being
+// 920 us, 1010 TFLOP/s of the 1241 that a large library product reaches; six chunks
+// of 301 to 1023 tokens over 8-bit pages 431 us, 835 TFLOP/s, the difference being
 // the widening and the pairs' starts and ends.  lse is exact to float32 here, so
 // the row sums are of the unrounded P, on the vector units.
 #pragma once

@@ -48,7 +48,10 @@ void launch_finish(const PagedArgs& a, hipStream_t s)
     const int states = a.workers / pairs;
     if (states >= 32 && pairs * rows <= 256) hipLaunchKernelGGL((paged_finish_kernel<D, T, 16>), dim3(x, (unsigned)rows), dim3(1024), 0, s, a);
     else if (states >= 8) hipLaunchKernelGGL((paged_finish_kernel<D, T, 4>), dim3(x, (unsigned)rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_finish_kernel<D, T, 1>), dim3(x, (unsigned)((rows + kPagedFinishRows - 1) / kPagedFinishRows)), dim3(64 * kPagedFinishRows), 0, s, a);
+    else {
+        constexpr int RPB = FinishCfg<D, 1>::RPB;
+        hipLaunchKernelGGL((paged_finish_kernel<D, T, 1>), dim3(x, (unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, s, a);
+    }
 }
 
 }  // namespace
