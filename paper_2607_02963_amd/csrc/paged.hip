@@ -203,6 +203,9 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     return PDEC_OK;
 }
 
+// What a caller is asked for, also where nothing is cut and nothing is stored.
+size_t workspace_of(const AttnPlan& p) { return std::max<size_t>(align256(p.few_bytes) + p.many_bytes, 16); }
+
 // What the three cache calls share of their pointers' checks.
 bool cache_pointers(const pdec_paged_dims* d, const void* k, const void* v, const uint8_t* ks, const uint8_t* vs)
 {
@@ -345,7 +348,7 @@ int pdec_paged_kv_read(const pdec_paged_dims* d, const void* k_pages, const void
 size_t pdec_paged_workspace_size(const pdec_paged_dims* d)
 {
     AttnPlan p;
-    return plan_attn(d, p) == PDEC_OK ? std::max<size_t>(align256(p.few_bytes) + p.many_bytes, 16) : 0;
+    return plan_attn(d, p) == PDEC_OK ? workspace_of(p) : 0;
 }
 
 int pdec_query_paged_plan(const pdec_paged_dims* d, pdec_paged_plan* plan)
@@ -373,7 +376,7 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
         !aligned(cu_tokens, 4) || !aligned(seq_lens, 4) || !aligned(workspace, 16) ||
         !cache_pointers(d, k_pages, v_pages, k_scales, v_scales))
         return PDEC_ERR_INVALID_ARG;
-    if (workspace_bytes < align256(p.few_bytes) + p.many_bytes) return PDEC_ERR_WORKSPACE;
+    if (workspace_bytes < workspace_of(p)) return PDEC_ERR_WORKSPACE;
     if (debug_mode() && (rc = debug_check(d, cu_tokens, seq_lens, 1, stream)) != PDEC_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     for (PagedArgs* a : {&p.few, &p.many}) {
