@@ -670,11 +670,17 @@ def _cache_code(pages: torch.Tensor) -> int:
 
 
 @functools.lru_cache(maxsize=256)
-def _paged_dims(num_tokens, H_q, pool, table, dtype_code, cache_code, max_chunk, max_len, causal, scale) -> PagedDims:
+def _kept_dims(num_tokens, H_q, pool, table, dtype_code, cache_code, max_chunk, max_len, causal, scale) -> PagedDims:
     """The dims of a call by its sizes (a serving loop makes the same few over and over); not to be written to."""
     P, page, H_kv, D = pool
     return make_paged_dims(table[0], num_tokens, H_q, H_kv, D, page, P, table[1], dtype_code, cache_code,
                            max_chunk=max_chunk, max_len=max_len, causal=causal, scale=scale)
+
+
+def _paged_dims(num_tokens, H_q, pool, table, dtype_code, cache_code, max_chunk, max_len, causal, scale) -> PagedDims:
+    """``_kept_dims`` by the values that the bounds and the scale have now (they may be tensors or arrays of one element,
+    which stand for themselves as keys, whatever is written to them)."""
+    return _kept_dims(num_tokens, H_q, pool, table, dtype_code, cache_code, int(max_chunk), int(max_len), causal, float(scale))
 
 
 def paged_dims_of(q, k_pages, block_table, *, causal=True, max_chunk=None, max_len=None, scale=0.0) -> PagedDims:
