@@ -660,9 +660,12 @@ def aggregate(g, x, cu_seg, salient, mode, *, scores=None, q=None, k=None, lse=N
 
 def make_paged_dims(num_seqs, num_tokens, H_q, H_kv, D, page_size, num_pages, max_pages, dtype_code, cache_code, *,
                     max_chunk=0, max_len=0, causal=1, scale=0.0) -> PagedDims:
-    return PagedDims(int(num_seqs), int(num_tokens), int(H_q), int(H_kv), int(D), int(page_size), int(num_pages),
-                     int(max_pages), int(max_chunk), int(max_len), int(dtype_code), int(cache_code), int(causal),
-                     float(scale))
+    sizes = [int(x) for x in (num_seqs, num_tokens, H_q, H_kv, D, page_size, num_pages, max_pages, max_chunk, max_len,
+                              dtype_code, cache_code, causal)]
+    for x in sizes:  # ctypes would take the low 32 bits: another bound
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{x} is beyond 32 bits")
+    return PagedDims(*sizes, float(scale))
 
 
 def _cache_code(pages: torch.Tensor) -> int:

@@ -23,3 +23,12 @@ def test_a_bound_that_is_written_to(make):
     d = dims(chunk, length, scale)
     assert (d.max_chunk, d.max_len, d.softmax_scale) == (8, 1500, 0.5)
     assert dims(8, 1500, 0.5) is d  # the same sizes have the same dims, made once
+
+
+@pytest.mark.parametrize("kw", [dict(max_len=2 ** 32 + 100), dict(max_chunk=2 ** 32), dict(max_len=-2 ** 32 + 1)], ids=str)
+def test_a_bound_beyond_32_bits_is_refused(kw):
+    """Its low 32 bits would be another bound, below the lengths it was meant for."""
+    with pytest.raises(ValueError):
+        dims(**kw)
+    with pytest.raises(ValueError):
+        pdec.make_paged_dims(2, 32, 28, 4, 128, 64, 100, 50, pdec.PDEC_DTYPE_BF16, pdec.PDEC_DTYPE_BF16, **kw)
