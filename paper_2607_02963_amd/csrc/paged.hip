@@ -125,8 +125,10 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int 
     a.groups = (int)((std::min<int64_t>(R, a.rows_to) + a.rows - 1) / a.rows);
     const int64_t units = (a.max_len + kUnit - 1) / kUnit;
     const int64_t real_groups = (int64_t)d->num_tokens * a.G / a.rows + d->num_seqs;  // at most, over the batch
+    // (the number of groups passes 2^50 for sizes that no tensor has: no product with it)
+    if (real_groups > INT32_MAX / 2 / a.H_kv / (units + pad + 1)) return false;
     const int64_t pairs = (int64_t)d->num_seqs * a.groups * (a.H_kv / a.heads);
-    if (pairs > INT32_MAX / 2 || real_groups * a.H_kv * (units + pad + 1) > INT32_MAX / 2) return false;
+    if (pairs > INT32_MAX / 2) return false;
     a.workers = workers;
     a.least = least;
     a.pad = pad;
