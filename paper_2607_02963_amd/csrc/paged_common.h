@@ -131,11 +131,14 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
         j = w - r.head * J;
         r.pos = 0;
     } else {
-        auto scan = [&](int x) {  // inclusive, over the lanes
+        // Inclusive, over the lanes.  Sums saturate: a head's positions and those of all
+        // heads fit 30 bits by the host's bounds on the sizes, but offsets outside the
+        // contract (each of many sequences with all of the tokens) pass 32 bits.
+        auto scan = [&](uint32_t x) {
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
-                const int y = __shfl_up(x, off);
-                if (lane >= off) x += y;
+                const uint32_t y = __shfl_up(x, off);
+                if (lane >= off) x = __builtin_elementwise_add_sat(x, y);
             }
             return x;
         };
@@ -165,9 +168,12 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             }
             return n;
         };
-        int total = 0, n = cost(lane), incl = scan(n);
-        total = __builtin_amdgcn_readlane(incl, 63);
-        for (int j0 = 64; j0 < items; j0 += 64) total += __builtin_amdgcn_readlane(scan(cost(j0 + lane)), 63);
+        auto last = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); };
+        int n = cost(lane);
+        uint32_t incl = scan(n), sum = last(incl);
+        for (int j0 = 64; j0 < items; j0 += 64) sum = __builtin_elementwise_add_sat(sum, last(scan(cost(j0 + lane))));
+        if ((uint64_t)sum * (uint32_t)sets > INT32_MAX / 2) return false;  // lengths outside the contract
+        const int total = (int)sum;
         const int workers = min(a.workers, max(total * sets / a.least, 1));
         if (w >= workers || total == 0) return false;
         r.per = total * sets / workers;
@@ -178,15 +184,15 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
         int rest = r.pos - r.head * total, j0 = 0;
         if (items > 64) incl = scan(n = cost(lane));
         while (true) {
-            const int all = __builtin_amdgcn_readlane(incl, 63);  // scalar, as everything that leaves the loop
-            if (rest < all) break;
-            rest -= all;
+            const uint32_t all = last(incl);  // scalar, as everything that leaves the loop
+            if ((uint32_t)rest < all) break;
+            rest -= (int)all;
             j0 += 64;
             if (j0 >= items) return false;  // lengths that changed under the call
             incl = scan(n = cost(j0 + lane));
         }
-        int at = __builtin_ctzll(__ballot(incl > rest));
-        rest -= __builtin_amdgcn_readlane(incl - n, at);
+        int at = __builtin_ctzll(__ballot(incl > (uint32_t)rest));
+        rest -= __builtin_amdgcn_readlane((int)incl - n, at);
         r.seq.t0 = __builtin_amdgcn_readlane(x.t0, at);
         r.seq.n = __builtin_amdgcn_readlane(x.n, at);
         r.seq.L = __builtin_amdgcn_readlane(x.L, at);
@@ -201,7 +207,7 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
         r.s = j0 + at;
         for (int g0 = 0; g0 < a.groups; g0 += 64) {  // a lane per group
             const int u = g0 + lane < a.groups ? paged_units_of(a, r.seq, g0 + lane) : 0, c = u > 0 ? u + a.pad : 0;
-            const int upto = scan(c), all = __builtin_amdgcn_readlane(upto, 63);
+            const int upto = (int)scan(c), all = __builtin_amdgcn_readlane(upto, 63);
             if (rest >= all) {
                 rest -= all;
                 continue;
