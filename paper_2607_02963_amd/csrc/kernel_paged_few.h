@@ -312,7 +312,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedArgs a)
                     }
                     float mx = p[0];
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, p[i]);
+                    for (int i = 1; i < 8; ++i) mx = paged_top(mx, p[i]);
                     if (__any(mx * c > m_ref[nt] + 8.f)) {  // rare after a row's first keys
                         const float mt = max_over_groups(mx) * c;
                         const bool up = mt > m_ref[nt] + 8.f;
@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedArgs a)
                 const int r = i / (D / 4) % rows, d4 = i % (D / 4), hs = i / (D / 4) / rows;
                 float M = m_s[hs][r];
 #pragma unroll
-                for (int x = 1; x < NK; ++x) M = fmaxf(M, m_s[HW * x + hs][r]);
+                for (int x = 1; x < NK; ++x) M = paged_top(M, m_s[HW * x + hs][r]);
                 float L = 0.f;
                 f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

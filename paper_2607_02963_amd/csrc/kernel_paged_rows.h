@@ -37,6 +37,11 @@
 
 namespace pdec {
 
+// The larger of two scores, NaN if one is.  A NaN raises no row's reference, and its
+// probability is NaN whatever that is.  (v_maximum3_f32: fmaxf would quiet each operand
+// with a v_max(x, x) first.)
+__device__ inline float paged_top(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // The halves of a bf16 pair that are infinite or NaN, as a mask: an exponent of
 // all ones carries into its half's top bit.
 __device__ inline uint32_t strange_bf16x2(uint32_t w)
@@ -329,12 +334,12 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         // max of element pair i (0 .. 8 NT - 1) into mx
         auto max_step = [&](float (&mx)[NT], const bf32x16_t (&s)[NT], int i) __attribute__((always_inline)) {
             const int nt = i / 8, k = 2 * (i % 8);
-            mx[nt] = k == 0 ? fmaxf(s[nt][0], s[nt][1]) : fmaxf(fmaxf(mx[nt], s[nt][k]), s[nt][k + 1]);
+            mx[nt] = k == 0 ? paged_top(s[nt][0], s[nt][1]) : paged_top(paged_top(mx[nt], s[nt][k]), s[nt][k + 1]);
         };
         // a row's reference max moves only when its block max exceeds it by more than 8
         auto rescale_tile = [&](float mx, int nt) __attribute__((always_inline)) {
             const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-            const float mt = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1])) * c;
+            const float mt = paged_top(__uint_as_float(b[0]), __uint_as_float(b[1])) * c;
             const bool up = mt > m_ref[nt] + 8.f;
             const float alpha = up ? fast_exp2(m_ref[nt] - mt) : 1.f;
             m_ref[nt] = up ? mt : m_ref[nt];

@@ -1,6 +1,7 @@
-// Launches of the bfloat16 kernels of the attention over paged caches, compiled
-// as the other matrix-core kernels are (see the build script): the IEEE mode bit
-// clear and without NaN semantics.
+// Launches of the bfloat16 kernels of the attention over paged caches, a
+// translation unit of their own for the compilation's time.  Compiled with NaN
+// semantics, unlike the dense matrix-core kernels (see the build script): hidden
+// rows hold anything, and a visible NaN is the result of the rows that see it.
 #include <hip/hip_runtime.h>
 
 #include "kernel_paged_few.h"
