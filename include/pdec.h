@@ -538,7 +538,7 @@ int pdec_attn_prefill_backward(const pdec_dims* dims, const void* q, const void*
  * A call serves a ragged batch of num_seqs sequences.  The new tokens of
  * sequence s are rows [cu_tokens[s], cu_tokens[s+1]) of q, out, lse, k_new and
  * v_new; a sequence may have none.  Rows of these behind the last sequence's
- * (a padded batch) are neither read nor written.
+ * (a padded batch) have no effect and are not written.  Outputs overlap no input.
  *   cu_tokens   [num_seqs + 1] int32, device, from 0, non-decreasing, at most num_tokens
  *   block_table [num_seqs, max_pages] int32, device
  *   seq_lens    [num_seqs] int32, device: keys of the sequence, its new tokens included
@@ -555,7 +555,8 @@ typedef struct pdec_paged_dims {
     int32_t page_size;    /* tokens per page: a power of two, 16..1024                           */
     int32_t num_pages;    /* pages of the pool, >= 1                                             */
     int32_t max_pages;    /* columns of block_table, >= 1; max_pages * page_size <= 2^30         */
-    int32_t max_chunk;    /* upper bound on one sequence's new tokens; 0 means num_tokens        */
+    int32_t max_chunk;    /* upper bound on one sequence's new tokens; 0 means num_tokens.  It   */
+                          /* chooses the attention's kernels: 1 for a batch of single tokens     */
     int32_t max_len;      /* upper bound on any sequence's keys; 0 means max_pages * page_size   */
     int32_t dtype;        /* PDEC_DTYPE_F32 or PDEC_DTYPE_BF16: q, out, k_new, v_new, dense rows */
     int32_t cache_dtype;  /* dtype, or PDEC_DTYPE_E4M3                                           */
@@ -581,7 +582,8 @@ typedef struct pdec_paged_dims {
  * its value, or 2^(k-10).  Infinities and NaNs become NaN, magnitudes above
  * 448 * 2^119 become that.
  * Pages that receive rows must not be shared by two sequences of the call.
- * num_q_heads, max_chunk, causal and softmax_scale are ignored.
+ * num_q_heads, max_chunk, causal and softmax_scale change nothing, but have to be
+ * valid as for the attention (num_q_heads = num_kv_heads and zeros do).
  * Asynchronous on `stream`.  Returns a pdec_status.
  */
 int pdec_paged_kv_append(const pdec_paged_dims* dims, const void* k_new, const void* v_new, const int32_t* cu_tokens,
@@ -590,13 +592,15 @@ int pdec_paged_kv_append(const pdec_paged_dims* dims, const void* k_new, const v
 
 /*
  * The first cu_rows[s+1] - cu_rows[s] keys and values of every sequence as
- * dense rows, in dims->dtype (exact: an e4m3 value times a power of two):
+ * dense rows, in dims->dtype (an e4m3 value times a power of two: exact in
+ * float32, and in bfloat16 from 2^-126 on or if the rows came from bfloat16; else
+ * rounded to bfloat16's subnormals):
  * row cu_rows[s] + t of k_out / v_out receives key t of s.  Rows t at or
  * beyond seq_lens[s], and rows of absent pages, receive 0.
  *   cu_rows [S + 1] int32, device, as cu_tokens, at most num_tokens;
  *   k_out, v_out [num_tokens, H_kv, D] device, 16-byte aligned.  Rows behind
  *   the last sequence's are left as they were.
- * num_q_heads, max_chunk, causal and softmax_scale are ignored.
+ * num_q_heads, max_chunk, causal and softmax_scale: as for the append.
  * Asynchronous on `stream`.  Returns a pdec_status.
  */
 int pdec_paged_kv_read(const pdec_paged_dims* dims, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
@@ -632,7 +636,9 @@ int pdec_query_paged_plan(const pdec_paged_dims* dims, pdec_paged_plan* plan);
  *   aligned, contents ignored.
  * Softmax statistics and sums are float32; for bfloat16 the probabilities meet
  * the values in bfloat16, as in the step calls, while lse and the normaliser
- * are sums of the unrounded ones.  Repeated calls agree bit for bit.
+ * are sums of the unrounded ones.  Sums of values are divided at the end: where
+ * they pass float32's range (2^8 times the sum of |v| over a row's keys does),
+ * the result is infinite or NaN.  Repeated calls agree bit for bit.
  * Asynchronous on `stream`.  Returns a pdec_status.
  */
 int pdec_paged_attn(const pdec_paged_dims* dims, const void* q, const void* k_pages, const void* v_pages,

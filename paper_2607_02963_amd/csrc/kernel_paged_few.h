@@ -8,16 +8,20 @@
 // of its own, and never waits for another wave until the states are joined at the
 // part's end.  A block's 16-key halves are each on one page: a scalar base and
 // fixed lane offsets per half, the pages of the block after the ring's read one
-// block ahead.  128 KB in flight per compute unit is more than the latency of the
-// memory asks; two waves to a SIMD hide each other's products and exponentials.
-// One token of each of 32 sequences over 8-bit pages (291 MB): 62 us, 4.7 TB/s with
-// the finish pass; one over 32768 bfloat16 keys (67 MB) 21.6 us, 3.1 TB/s, of which
-// the passes' starts and ends are about 8.
+// block ahead.  A ring holds two blocks (four of 8-bit rows of 64), but one of
+// bfloat16 rows of 128: there a wave asks for its next block behind this one's
+// products and has nothing under way meanwhile, and only the other wave of its SIMD
+// covers for it.  One token of each of 32 sequences over 8-bit pages (291 MB): 62 us,
+// 4.7 TB/s with the finish pass; one over 32768 bfloat16 keys (67 MB) 20.4 us,
+// 3.3 TB/s: two blocks to a wave, half of the wave cycles waiting, and the passes'
+// starts and ends about 8.
 //
 // Up to 32 rows at D = 128 and 64 at D = 64: above, 64 rows' accumulators leave a
 // SIMD one wave at D = 128, and the kernel for many rows, which shares its keys over
 // its waves, is as fast or faster from there (13 sequences of 35 rows of 128 47.7
 // against 39.9 us, of 56 rows 53.8 against 41.7; 64 rows of 64 48.4 against 51.7).
+// Not over 8-bit pages where memory bounds the call: 32 sequences of 35 rows took
+// 112 us in a form for 64 rows, and take 120 in the kernel for many rows.
 //
 // Per block, products and layouts as in the decode step (kernel_mfma.h):
 //   S^T  = K  Q^T    A = 16 keys x 32 d from LDS, B = Q^T (registers)
@@ -329,7 +333,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedArgs a)
                         // (a hidden key's scale may be anything, 0 times infinity among it)
                         if constexpr (FP8) vp[i] = full || p[i] > 0.f ? p[i] * paged_scale(vs[i >> 2], i & 3) : p[i];
                     }
-                    // the row sums take P unrounded, the product rounded to bf16
+                    // the row sums take P unrounded; the product's operands are bf16, so P is
+                    // rounded by half a step (2^-8) of each term, as out is.  A value's power of
+                    // two takes no bits
                     lsum[nt] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
                     const bf16x8_t pf = as_bf16x8(u32x4_t{pack_bf16x2(vp[0], vp[1]), pack_bf16x2(vp[2], vp[3]),
                                                           pack_bf16x2(vp[4], vp[5]), pack_bf16x2(vp[6], vp[7])});

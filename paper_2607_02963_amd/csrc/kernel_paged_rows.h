@@ -356,7 +356,8 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 for (int nt = 0; nt < NT; ++nt) rescale_tile(mx[nt], nt);
             }
         };
-        // P of element pair i (0 .. 8 NT - 1), rounded to bf16 for the product; the row sums take it unrounded
+        // P of element pair i (0 .. 8 NT - 1), rounded to bf16, the product's operand type, by half
+        // a step (2^-8) of each term, as out is; the row sums take it unrounded
         auto prob_step = [&](u32x4_t (&pk)[NT][2], const bf32x16_t (&s)[NT], int i) __attribute__((always_inline)) {
             const int nt = i / 8, k = i % 8;
             const float p0 = fast_exp2(fmaf(s[nt][2 * k], c, -m_ref[nt])), p1 = fast_exp2(fmaf(s[nt][2 * k + 1], c, -m_ref[nt]));

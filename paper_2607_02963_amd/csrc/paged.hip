@@ -101,7 +101,7 @@ int len_bound(const pdec_paged_dims* d) { return d->max_len > 0 ? d->max_len : d
 int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
 
 // Sequences of at most so many rows per kv head are the few-row kernel's: up to two
-// 16-row tiles at D = 128, four at D = 64.
+// 16-row tiles at D = 128, four at D = 64 (both sides measured: kernel_paged_few.h).
 int few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
 
 struct AttnPlan {
@@ -113,7 +113,10 @@ struct AttnPlan {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Where no pair has more units than this nothing is cut, a work-group takes a pair
-// and there is no finish pass: one token over 250 keys 10.9 us, cut 13.8.
+// and there is no finish pass.  Whole and cut, one token over 60 to 250 bfloat16 keys
+// 11 and 15 us, 32 tokens over 8-bit pages 12 and 15, 8 chunks of 60 18-25 and 25-33.
+// Above, few pairs of a long axis want cutting (one float32 token over 1000 keys 14 us,
+// whole 22); 400 keys are as well or better whole (14 and 11 us, 36 and 28).
 constexpr int kWholeUnits = 4;
 
 // The division of one launch's work over `workers` work-groups (paged_common.h),
