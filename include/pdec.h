@@ -69,7 +69,8 @@ typedef enum {
 typedef enum {
     PDEC_DTYPE_F32 = 0,
     PDEC_DTYPE_BF16 = 1,
-    PDEC_DTYPE_E4M3 = 2 /* 8-bit cache rows (paged caches only): OCP e4m3 with one scale per token and kv head */
+    PDEC_DTYPE_E4M3 = 2, /* 8-bit cache rows (paged caches only): OCP e4m3 with one scale per token and kv head */
+    PDEC_DTYPE_E2M1 = 3 /* 4-bit cache rows (paged caches only): OCP e2m1 with one scale per 32 elements */
 } pdec_dtype;
 
 /* Sizes of one call.  All fields are host values. */
@@ -535,6 +536,14 @@ int pdec_attn_prefill_backward(const pdec_dims* dims, const void* q, const void*
  *   k_scales, v_scales [num_pages, H_kv, page_size] uint8, value = e4m3 * 2^(byte - 127).
  * The append writes bytes 1..246; a byte of 0 counts as a scale of 0.
  *
+ * Or in 4 bits (PDEC_DTYPE_E2M1), e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) with
+ * one power of two per 32 elements of a row, a head's tokens one after another:
+ *   k_pages, v_pages [num_pages, H_kv, page_size, D / 2] uint8, element 2 i of a row in
+ *   the low half of its byte i, element 2 i + 1 in the high half;
+ *   k_scales, v_scales [num_pages, H_kv, page_size, D / 32] uint8, 16-byte aligned,
+ *   value = e2m1 * 2^(byte - 127); 255 with 32 zeros makes the 32 elements NaN.
+ * The append writes bytes 1..252 and 255.
+ *
  * A call serves a ragged batch of num_seqs sequences.  The new tokens of
  * sequence s are rows [cu_tokens[s], cu_tokens[s+1]) of q, out, lse, k_new and
  * v_new; a sequence may have none.  Rows of these behind the last sequence's
@@ -559,7 +568,7 @@ typedef struct pdec_paged_dims {
                           /* chooses the attention's kernels: 1 for a batch of single tokens     */
     int32_t max_len;      /* upper bound on any sequence's keys; 0 means max_pages * page_size   */
     int32_t dtype;        /* PDEC_DTYPE_F32 or PDEC_DTYPE_BF16: q, out, k_new, v_new, dense rows */
-    int32_t cache_dtype;  /* dtype, or PDEC_DTYPE_E4M3                                           */
+    int32_t cache_dtype;  /* dtype, PDEC_DTYPE_E4M3 or PDEC_DTYPE_E2M1                           */
     int32_t causal;       /* attention: 1: new token i of n sees keys t <= len - n + i; 0: all   */
                           /* new tokens see all len keys (the event streams' queries against a   */
                           /* shared prefix; queries against another sequence's states)           */
@@ -574,13 +583,17 @@ typedef struct pdec_paged_dims {
  * with lens_out[s] = lens_in[s].
  *   k_new, v_new [num_tokens, H_kv, D] device, 16-byte aligned;
  *   lens_in, lens_out [S] int32, device, different arrays;
- *   k_scales, v_scales: e4m3 cache only, else NULL.
+ *   k_scales, v_scales: 8- and 4-bit caches only, else NULL.
  * A row x of D elements goes to an e4m3 cache as e4m3(x / 2^k), to nearest
  * even, k the least integer in [-126, 119] with max |x| / 2^k <= 448 over the
  * finite elements (0 if they are all 0), and the byte k + 127.  Dividing by a
  * power of two is exact, so each element is rounded once: by at most 2^-4 of
  * its value, or 2^(k-10).  Infinities and NaNs become NaN, magnitudes above
  * 448 * 2^119 become that.
+ * 32 elements x go to an e2m1 cache as e2m1(x / 2^k), to nearest even, k the least
+ * integer in [-126, 125] with max |x| / 2^k <= 6 (0 if they are all 0), and the byte
+ * k + 127: each element is rounded once, by at most 2^-2 of its value, or 2^(k-2).
+ * Magnitudes above 6 * 2^125 become that; an infinity or NaN makes the 32 NaN.
  * Pages that receive rows must not be shared by two sequences of the call.
  * num_q_heads, max_chunk, causal and softmax_scale change nothing, but have to be
  * valid as for the attention (num_q_heads = num_kv_heads and zeros do).
@@ -594,7 +607,7 @@ int pdec_paged_kv_append(const pdec_paged_dims* dims, const void* k_new, const v
  * The first cu_rows[s+1] - cu_rows[s] keys and values of every sequence as
  * dense rows, in dims->dtype (an e4m3 value times a power of two: exact in
  * float32, and in bfloat16 from 2^-126 on or if the rows came from bfloat16; else
- * rounded to bfloat16's subnormals):
+ * rounded to bfloat16's subnormals; an e2m1 value: exact in both):
  * row cu_rows[s] + t of k_out / v_out receives key t of s.  Rows t at or
  * beyond seq_lens[s], and rows of absent pages, receive 0.
  *   cu_rows [S + 1] int32, device, as cu_tokens, at most num_tokens;
@@ -630,7 +643,8 @@ int pdec_query_paged_plan(const pdec_paged_dims* dims, pdec_paged_plan* plan);
  * (causal) or t < len (not causal) on pages that are present;
  *   out = sum_t p_t v_t, p_t = exp(scale <q, k_t> - lse), lse the log-sum-exp;
  * a query that sees nothing gets 0 and -inf.  Hidden keys and values, whatever
- * they hold (infinities and NaNs too), do not reach a query's result.
+ * they hold (infinities and NaNs too), do not reach a query's result.  (Nor, in a
+ * 4-bit cache, does a NaN value whose probability is below float32's range.)
  *   q, out [num_tokens, H_q, D], lse [num_tokens, H_q] float32 or NULL;
  *   workspace >= pdec_paged_workspace_size(dims) bytes, device, 16-byte
  *   aligned, contents ignored.

@@ -1,0 +1,343 @@
+// Attention over 4-bit paged caches, few query rows per kv head, bfloat16 queries, on
+// v_mfma_f32_16x16x32_bf16.
+//
+// The division of the work is that of the other caches' few-row kernel
+// (kernel_paged_few.h): eight waves, each with a ring of its own in LDS, a softmax state
+// of its own, joined at the part's end.  A wave's block is 64 keys, four quarters of 16,
+// each on one page; a quarter of K or V is one DMA instruction, the scales of a block's
+// keys and values one more.
+//
+// Products and layouts, for 64 keys t + 16 q + j of quarters q:
+//   S^T  = K  Q^T    four tiles of 16 keys; tile kt holds the keys 16 q + 4 kt + i, so
+//                    that a lane's 16 scores are the keys of one quarter, in order
+//   O^T += V^T P^T   two steps of 32 keys: ds_read_b64_tr_b4 gives a lane 16 keys of one
+//                    d, the first eight for one step, the others for the second
+// A lane's 16 bytes of a key row (8 at D = 64) have one scale, which the widening
+// v_cvt_scalef32_pk_bf16_fp4 takes with it.  A lane's 16 values have a scale each, so
+// that those multiply the probabilities, once for each block of 32 d, before they are
+// rounded: a power of two takes no bits.
+#pragma once
+
+#include "kernel_paged_few.h"
+#include "paged_e2m1.h"
+
+namespace pdec {
+
+// 16-byte chunk permutations of the rows in LDS: chunk ch of key k sits at ch ^ swizzle(k).
+template <int D>
+__device__ inline int few4_kswz(int key) { return D == 128 ? ((key >> 4) & 3) : ((key >> 4) & 1); }
+template <int D>
+__device__ inline int few4_vswz(int key) { return D == 128 ? ((key >> 2) & 3) : ((key >> 3) & 1); }
+
+// One wave-wide DMA of 16 bytes per lane from the lanes' own addresses.
+__device__ inline void dma_16B_lanes(uint64_t addr, uint32_t lds_base, uint64_t lanes)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1" :
+                 : "s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(addr), "s"(sgpr_base(reinterpret_cast<const void*>(lanes)))
+                 : "memory");
+}
+
+// x y, 0 if one is 0, whatever the other (v_mul_legacy_f32, which has no builtin; as
+// inline assembly the compiler would not keep it apart from a v_exp_f32 before it).
+__device__ float mul_zero(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+
+template <int D, int NT>
+__global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
+{
+    constexpr int NW = kFewWaves;
+    constexpr int RT = 16 * NT;
+    constexpr int RING = 131072 / NW;            // bytes of a wave's ring
+    constexpr int ROWB = D / 2;
+    constexpr int KB = kUnit;                    // keys per block
+    constexpr int TENSOR = KB * ROWB, SLOT = 2 * TENSOR;
+    constexpr int NS = RING / SLOT;              // ring slots of a wave
+    constexpr int CPK = ROWB / 16;               // 16-byte chunks per key
+    constexpr int QB = 16 * ROWB;                // bytes of a quarter, one DMA instruction
+    constexpr int SPK = D / kE2m1Block;          // scales per key
+    constexpr int SC = 2 * KB * SPK;             // bytes of a block's scales
+    constexpr int PB = 9;                        // instructions per block: K's and V's quarters, the scales
+    constexpr int KS = D / 32, DT = D / 16;
+    constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
+    constexpr uint64_t QLANES = QB == 1024 ? ~0ull : (1ull << (QB / 16)) - 1;
+    constexpr uint64_t SLANES = (1ull << (SC / 16)) - 1;
+    static_assert(KB == 64 && QB <= 1024 && (NS - 1) * PB < 64, "a block's instructions, and the wait that counts them");
+    static_assert(16 * OROW * 4 <= RING, "merge buffer");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + NW * NS * SC];
+    __shared__ float m_s[NW][16], l_s[NW][16];
+
+    const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
+    const int lane = paged_lane(), l16 = lane & 15, lg = lane >> 4;
+    PagedRun run;
+    PagedPart part;
+    if (!paged_begin(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
+
+    const float c = a.qscale;
+    const uint32_t ring = lds_u32(lds) + w * RING, sc_ring = lds_u32(lds) + NW * RING + w * NS * SC;
+    // byte offset of the lane's chunk in a quarter
+    uint32_t koffs[4], voffs;
+    {
+        const int k = lane / CPK & 15;  // (at D = 64 the upper lanes take no part)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) koffs[q] = (uint32_t)k * ROWB + 16 * ((lane % CPK) ^ few4_kswz<D>(16 * q + k));
+        voffs = (uint32_t)k * ROWB + 16 * ((lane % CPK) ^ few4_vswz<D>(k));
+    }
+    // operand reads, relative to a slot: key 16 (l16 / 4) + l16 % 4 + 4 kt of K, the lane's elements;
+    // key 16 lg + l16 of V, eight bytes of tile dt
+    uint32_t kread, vread[DT];
+    const int kkey = 16 * (l16 >> 2) + (l16 & 3), vkey = 16 * lg + l16;
+    if constexpr (D == 128) kread = kkey * ROWB + 16 * (lg ^ few4_kswz<D>(kkey));
+    else kread = kkey * ROWB + 16 * ((lg >> 1) ^ few4_kswz<D>(kkey)) + 8 * (lg & 1);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) vread[dt] = TENSOR + vkey * ROWB + 16 * ((dt >> 1) ^ few4_vswz<D>(l16)) + 8 * (dt & 1);
+    const uint32_t ksread = kkey * SPK + (D == 128 ? lg : lg >> 1), vsread = KB * SPK + 16 * lg * SPK;
+    typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
+    typedef __attribute__((address_space(3))) const u32x2_t lds_u32x2_t;
+    typedef __attribute__((address_space(3))) const uint8_t lds_u8_t;
+    typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+    typedef __attribute__((address_space(3))) i32x2_t lds_i32x2_t;
+    // the scales: lanes 0 .. 4 SPK - 1 K's, SPK to a quarter, then V's
+    const int sq_lane = lane / SPK & 3;
+    const uint64_t sc_lane = reinterpret_cast<uint64_t>(lane & (4 * SPK) ? a.v_scales : a.k_scales) + 16 * (lane % SPK);
+
+    while (paged_next(a, run, part)) {
+        if (w == 0 && lane == 0) paged_note(a, run, part);
+        const PagedSeq sq = part.seq;
+        const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);
+        const int tiles = (nrows + 15) / 16;
+        const int nb = part.u1 - part.u0, mine = nb > w ? (nb - w + NW - 1) / NW : 0;  // blocks: of the part, of the wave
+        const int t0 = part.u0 * kUnit;
+        const int32_t* table = a.block_table + (long)part.s * a.max_pages;
+        const int head = part.head;
+        const uint64_t kbase = sgpr_base(a.k_pages), vbase = sgpr_base(a.v_pages);
+
+        // the wave's block b: its first key, and its quarters' pages
+        auto first = [&](int b) __attribute__((always_inline)) { return t0 + KB * (w + NW * b); };
+        struct Pages { int q[4]; };
+        auto pages = [&](int b) __attribute__((always_inline)) {
+            Pages x;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                x.q[q] = q > 0 && a.page_shift > 5 ? x.q[0] : paged_entry(table, min((first(b) + 16 * q) >> a.page_shift, a.max_pages - 1));
+            return x;
+        };
+        auto there = [&](int page) __attribute__((always_inline)) { return (uint32_t)page < (uint32_t)a.num_pages; };
+        // blocks past the last are pieces of one lane, so that every wait counts the same
+        // (ring.h); an absent page is read as page 0, and its keys masked
+        auto issue = [&](int b, const Pages& x) __attribute__((always_inline)) {
+            const uint64_t real = b < mine ? ~0ull : 1ull;
+            const uint32_t dst = ring + (b % NS) * SLOT;
+            uint64_t row[4];  // the quarters' rows of the pool
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int page = there(x.q[q]) && b < mine ? x.q[q] : 0;
+                row[q] = (((uint64_t)(uint32_t)page * a.H_kv + head) << a.page_shift) + (uint32_t)((first(b) + 16 * q) & ((1 << a.page_shift) - 1));
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t off[2][1] = {{koffs[q]}, {voffs}};
+                dma_rows(kbase + row[q] * ROWB, off[0], dst + QB * q, real & QLANES);
+                dma_rows(vbase + row[q] * ROWB, off[1], dst + TENSOR + QB * q, real & QLANES);
+            }
+            const uint64_t lo = sq_lane & 1 ? row[1] : row[0], hi = sq_lane & 1 ? row[3] : row[2];
+            dma_16B_lanes(sc_lane + (sq_lane & 2 ? hi : lo) * SPK, sc_ring + (b % NS) * SC, real & SLANES);
+        };
+
+        // ---- this lane's rows: 16 nt + l % 16; those past the last see nothing ----
+        int seen[NT];
+        u32x4_t qf[NT][KS];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = 16 * nt + l16, rr = row0 + min(r, nrows - 1);
+            seen[nt] = r < nrows ? paged_seen(a, sq, rr / a.G) : 0;
+            const uint16_t* q = static_cast<const uint16_t*>(a.q) + paged_qrow(a, sq, head, rr) * D;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) qf[nt][i] = *reinterpret_cast<const u32x4_t*>(q + 8 * KS * lg + 8 * i);
+        }
+        // keys that every row sees (rows past the last are masked or not, their results are not stored)
+        const int least = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, row0 / a.G));
+        const int most = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, (row0 + nrows - 1) / a.G));
+#pragma unroll
+        for (int b = 0; b < NS; ++b)
+            if (mine > 0) issue(b, pages(min(b, mine - 1)));
+        Pages ahead = pages(min(NS, max(mine - 1, 0)));
+        Pages now = pages(0);
+
+        f32x4_t o[NT][DT];
+        float m_ref[NT], lsum[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m_ref[nt] = kMinRef;
+            lsum[nt] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        // the query loads and the DMA complete in no order relative to each other
+        wait_vmcnt<0>();
+
+        for (int b = 0; b < mine; ++b) {
+            wave_wait_vmcnt<(NS - 1) * PB>();  // block b has landed
+            const uint32_t slot = ring + (b % NS) * SLOT, scs = sc_ring + (b % NS) * SC;
+            const int t = first(b);
+            const bool have[4] = {there(now.q[0]), there(now.q[1]), there(now.q[2]), there(now.q[3])};
+            if ((have[0] | have[1] | have[2] | have[3]) && t < most) {
+                const bool all = have[0] & have[1] & have[2] & have[3];
+                const bool full = t + KB <= least && all;
+                const bool mine_there = lg & 2 ? (lg & 1 ? have[3] : have[2]) : (lg & 1 ? have[1] : have[0]);
+                // one tile, or all: rows past the last see nothing, or their results are not stored
+                auto block = [&](auto count) __attribute__((always_inline)) {
+                    constexpr int N = count;
+                    float p[N][16];  // scores, then probabilities, of keys t + 16 lg + j
+                    {
+                        f32x4_t s[N][4];
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt) {
+                            if (N > 1) __builtin_amdgcn_sched_barrier(0);  // registers: one tile's operands at a time
+                            const float ks = e2m1_scale(*(lds_u8_t*)(uintptr_t)(scs + ksread + 4 * kt * SPK));
+                            uint32_t x[KS];
+                            if constexpr (D == 128) {
+                                const u32x4_t y = *(lds_u32x4_t*)(uintptr_t)(slot + kread + 4 * kt * ROWB);
+#pragma unroll
+                                for (int i = 0; i < KS; ++i) x[i] = y[i];
+                            } else {
+                                const u32x2_t y = *(lds_u32x2_t*)(uintptr_t)(slot + kread + 4 * kt * ROWB);
+#pragma unroll
+                                for (int i = 0; i < KS; ++i) x[i] = y[i];
+                            }
+#pragma unroll
+                            for (int nt = 0; nt < N; ++nt) s[nt][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int i = 0; i < KS; ++i) {
+                                const bf16x8_t kf = as_bf16x8(e2m1_bf16(x[i], ks));
+#pragma unroll
+                                for (int nt = 0; nt < N; ++nt)
+                                    s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[nt][i]), s[nt][kt]);
+                            }
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < N; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) p[nt][j] = s[nt][j >> 2][j & 3];
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < N; ++nt) {
+                        if (!full) {
+                            const int lim = mine_there ? seen[nt] - t - 16 * lg : 0;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) p[nt][j] = j >= lim ? kNegInf : p[nt][j];
+                        }
+                        float mx = p[nt][0];
+#pragma unroll
+                        for (int j = 1; j < 16; ++j) mx = paged_top(mx, p[nt][j]);
+                        if (__any(mx * c > m_ref[nt] + 8.f)) {  // rare after a row's first keys
+                            const float mt = max_over_groups(mx) * c;
+                            const bool up = mt > m_ref[nt] + 8.f;
+                            const float alpha = up ? fast_exp2(m_ref[nt] - mt) : 1.f;
+                            m_ref[nt] = up ? mt : m_ref[nt];
+                            lsum[nt] *= alpha;
+#pragma unroll
+                            for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
+                        }
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            p[nt][j] = fast_exp2(fmaf(p[nt][j], c, -m_ref[nt]));  // 0 for a hidden key
+                            sum[j & 3] += p[nt][j];
+                        }
+                        // the row sums take P unrounded; the product's operands are bf16, so P is
+                        // rounded by half a step (2^-8) of each term, as out is
+                        lsum[nt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    }
+                    uint32_t vs[4 * SPK];  // the scales of the lane's 16 values
+#pragma unroll
+                    for (int i = 0; i < SPK; ++i) {
+                        const u32x4_t x = *(lds_u32x4_t*)(uintptr_t)(scs + vsread + 16 * i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vs[4 * i + e] = x[e];
+                    }
+                    // a hidden value's scale may be NaN: its probability of 0 stays 0
+#pragma unroll
+                    for (int blk = 0; blk < SPK; ++blk) {
+                        if (N > 1) __builtin_amdgcn_sched_barrier(0);
+                        u32x4_t pf[N][2];
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const float s0 = SPK == 4 ? paged_scale(vs[j], blk) : paged_scale(vs[j / 2], blk);
+                            const float s1 = SPK == 4 ? paged_scale(vs[j + 1], blk) : paged_scale(vs[j / 2], 2 + blk);
+#pragma unroll
+                            for (int nt = 0; nt < N; ++nt)
+                                pf[nt][j >> 3][(j >> 1) & 3] = pack_bf16x2(mul_zero(p[nt][j], s0), mul_zero(p[nt][j + 1], s1));
+                        }
+#pragma unroll
+                        for (int dt = 2 * blk; dt < 2 * blk + 2; ++dt) {
+                            const i32x2_t x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2_t*)(uintptr_t)(slot + vread[dt]));
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const bf16x8_t vf = as_bf16x8(e2m1_bf16((uint32_t)(h ? x.y : x.x), 1.f));
+#pragma unroll
+                                for (int nt = 0; nt < N; ++nt) o[nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt][h]), o[nt][dt]);
+                            }
+                        }
+                    }
+                };
+                if (NT > 1 && tiles > 1) block(std::integral_constant<int, NT>{});
+                else block(std::integral_constant<int, 1>{});
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+            issue(b + NS, ahead);
+            ahead = pages(min(b + NS + 1, mine - 1));
+            now = pages(min(b + 1, mine - 1));
+        }
+
+        // ---- the waves' states joined, tile by tile; lane: row l % 16 of tile nt, d = 16 dt + 4 (l / 16) + i ----
+        wait_vmcnt<0>();  // no DMA into the ring outlives the part
+        float* const o_s = reinterpret_cast<float*>(lds);
+        constexpr int OW = 16 * OROW;  // a wave's rows, in floats
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt >= tiles) break;
+            lds_barrier();  // the ring, or the tiles before, have been read
+            float l = lsum[nt];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (lg == 0) {
+                m_s[w][l16] = m_ref[nt];
+                l_s[w][l16] = l;
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4_t*>(o_s + w * OW + l16 * OROW + 16 * dt + 4 * lg) = o[nt][dt];
+            lds_barrier();
+            const int rows = min(nrows - 16 * nt, 16);
+            for (int i = 64 * w + lane; i < rows * (D / 4); i += 64 * NW) {
+                const int r = i / (D / 4), d4 = i % (D / 4);
+                float M = m_s[0][r];
+#pragma unroll
+                for (int x = 1; x < NW; ++x) M = paged_top(M, m_s[x][r]);
+                float L = 0.f;
+                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < NW; ++x) {
+                    const float f = fast_exp2(m_s[x][r] - M);  // 0 for a wave that saw none of the row's keys
+                    L += f * l_s[x][r];
+                    acc += f * *reinterpret_cast<const f32x4_t*>(o_s + x * OW + r * OROW + 4 * d4);
+                }
+                const int row = 16 * nt + r;
+                if (!part.whole) {
+                    const long at = (long)part.slot * RT + row;
+                    *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 4 * d4) = acc;
+                    if (d4 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(M, L);
+                    continue;
+                }
+                const long qr = paged_qrow(a, sq, head, row0 + row);
+                const bool any = __float_as_uint(L) != 0;  // L is 0, positive or NaN
+                const float inv = any ? 1.f / L : 0.f;
+                acc *= inv;
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + qr * D + 4 * d4) =
+                    make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+                if (d4 == 0 && a.lse) a.lse[qr] = any ? kLn2 * (M + __log2f(L)) : kNegInf;
+            }
+        }
+        lds_barrier();  // the states have been read: the next part's DMA may come
+    }
+}
+
+}  // namespace pdec

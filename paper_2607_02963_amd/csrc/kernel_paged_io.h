@@ -12,8 +12,7 @@
 // joined rows of 128 float32 (27 MB) 7.5 us, 3.6 TB/s.
 #pragma once
 
-#include "kernel_mfma.h"
-#include "paged_common.h"
+#include "paged_e2m1.h"
 
 namespace pdec {
 
@@ -177,10 +176,13 @@ __device__ inline void paged_place(const PagedIoArgs& a, int r0, bool before, Pa
     }
 }
 
+// How a cache holds its rows.
+enum PagedForm { kPlainRows, kE4m3Rows, kE2m1Rows };
+
 // A wave takes N consecutive tokens of one tensor, eight elements a lane.
 // grid (max(tokens / (4 N), sequences / 64), 2): few tokens a token per wave, for
 // the latency; many four, with one look-up and all their loads under way.
-template <int D, typename T, bool QUANT, int N>
+template <int D, typename T, PagedForm FORM, int N>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedIoArgs a)
 {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -211,9 +213,19 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedIoArgs a)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (p.page[i] < 0) continue;
+            if constexpr (FORM == kE2m1Rows) {
+                const long at = e2m1_row(p.page[i], e / D, a.H_kv, a.page_shift, p.slot[i]);
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = row[i].get(j);
+                int byte;
+                *reinterpret_cast<uint32_t*>(pages + at * (D / 2) + e % D / 2) = quantise4(x, byte);
+                if (e % kE2m1Block == 0) scales[at * (D / kE2m1Block) + e % D / kE2m1Block] = (uint8_t)byte;
+                continue;
+            }
             const long at = ((long)p.page[i] << a.page_shift) + p.slot[i];
-            unsigned char* dst = pages + (at * elems + e) * (QUANT ? 1 : (int)sizeof(T));
-            if constexpr (QUANT) {
+            unsigned char* dst = pages + (at * elems + e) * (FORM == kE4m3Rows ? 1 : (int)sizeof(T));
+            if constexpr (FORM == kE4m3Rows) {
                 int byte;
                 *reinterpret_cast<uint2*>(dst) = quantise8<D>(row[i], byte);
                 if (e % D == 0) scales[(((long)p.page[i] * a.H_kv + e / D) << a.page_shift) + p.slot[i]] = (uint8_t)byte;
@@ -225,7 +237,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedIoArgs a)
 }
 
 // A wave takes N consecutive rows of one tensor.  grid (rows / (4 N), 2).
-template <int D, typename T, bool QUANT, int N>
+template <int D, typename T, PagedForm FORM, int N>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -244,8 +256,14 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (p.page[i] < 0) continue;
+            if constexpr (FORM == kE2m1Rows) {
+                const long at = e2m1_row(p.page[i], e / D, a.H_kv, a.page_shift, p.slot[i]);
+                x[i].x = *reinterpret_cast<const uint32_t*>(pages + at * (D / 2) + e % D / 2);
+                byte[i] = scales[at * (D / kE2m1Block) + e % D / kE2m1Block];
+                continue;
+            }
             const long at = ((long)p.page[i] << a.page_shift) + p.slot[i];
-            if constexpr (QUANT) {
+            if constexpr (FORM == kE4m3Rows) {
                 x[i] = *reinterpret_cast<const uint2*>(pages + at * elems + e);
                 byte[i] = scales[(((long)p.page[i] * a.H_kv + e / D) << a.page_shift) + p.slot[i]];
             } else {
@@ -258,7 +276,11 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
             if (p.page[i] < 0) {
                 const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                 row[i].set(z);
-            } else if constexpr (QUANT) {
+            } else if constexpr (FORM == kE2m1Rows) {
+                float v[8];
+                e2m1_f32(x[i].x, e2m1_scale(byte[i]), v);
+                row[i].set(v);
+            } else if constexpr (FORM == kE4m3Rows) {
                 const float sc = paged_scale(byte[i], 0);
                 float v[8];
 #pragma unroll

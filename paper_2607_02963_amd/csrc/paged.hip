@@ -28,10 +28,12 @@ void launch_f32_rows(const PagedArgs& a, hipStream_t s)
 
 }  // namespace
 
-void launch_paged_f32(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
+void launch_paged_f32(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
 {
-    if (head_dim == 128) fp8 ? launch_f32_rows<128, fp8_t>(a, s) : launch_f32_rows<128, float>(a, s);
-    else fp8 ? launch_f32_rows<64, fp8_t>(a, s) : launch_f32_rows<64, float>(a, s);
+    auto rows = [&](auto cache) { head_dim == 128 ? launch_f32_rows<128, decltype(cache)>(a, s) : launch_f32_rows<64, decltype(cache)>(a, s); };
+    if (cache_dtype == PDEC_DTYPE_E2M1) rows(fp4_t{});
+    else if (cache_dtype == PDEC_DTYPE_E4M3) rows(fp8_t{});
+    else rows(float{});
 }
 
 namespace {
@@ -83,7 +85,8 @@ int check_dims(const pdec_paged_dims* d)
         return PDEC_ERR_INVALID_ARG;
     if (std::isnan(d->softmax_scale) || std::isinf(d->softmax_scale)) return PDEC_ERR_INVALID_ARG;
     if (d->dtype != PDEC_DTYPE_F32 && d->dtype != PDEC_DTYPE_BF16) return PDEC_ERR_UNSUPPORTED;
-    if (d->cache_dtype != d->dtype && d->cache_dtype != PDEC_DTYPE_E4M3) return PDEC_ERR_UNSUPPORTED;
+    if (d->cache_dtype != d->dtype && d->cache_dtype != PDEC_DTYPE_E4M3 && d->cache_dtype != PDEC_DTYPE_E2M1)
+        return PDEC_ERR_UNSUPPORTED;
     if (d->head_dim != 64 && d->head_dim != 128) return PDEC_ERR_UNSUPPORTED;
     if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
         return PDEC_ERR_UNSUPPORTED;
@@ -179,7 +182,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     a.rows_to = INT32_MAX;
     a.heads = 1;
     p.few = p.many = a;
-    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d->head_dim);
+    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d->head_dim) && d->cache_dtype != PDEC_DTYPE_E2M1;
     // One sequence is the many rows' whatever its chunk, and so are all where none has
     // more rows than a 128-row item: a second kernel and its finish pass cost more than
     // the rows left empty (24 sequences of 300 to 4000 keys, one of 16 new tokens and the
@@ -200,9 +203,10 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     if (p.use_few) {
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
         const bool f32 = d->dtype == PDEC_DTYPE_F32;
-        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : most <= 48 ? 48 : 64;
+        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 || d->head_dim == 128 ? 32 : most <= 48 ? 48 : 64;
         // heads' rows of a cache line or half of one: two heads to a work-group (kernel_paged_few.h)
-        if (!f32 && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;
+        if (!f32 && d->cache_dtype != PDEC_DTYPE_E2M1 && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0)
+            p.few.heads = 2;
         if (!divide(d, p.few, f32 ? 512 : 256, 2, f32 ? 1 : 4, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;
@@ -215,6 +219,7 @@ size_t workspace_of(const AttnPlan& p) { return std::max<size_t>(align256(p.few_
 bool cache_pointers(const pdec_paged_dims* d, const void* k, const void* v, const uint8_t* ks, const uint8_t* vs)
 {
     if (!aligned(k, 16) || !aligned(v, 16)) return false;
+    if (d->cache_dtype == PDEC_DTYPE_E2M1) return aligned(ks, 16) && aligned(vs, 16);
     return d->cache_dtype != PDEC_DTYPE_E4M3 || (aligned(ks, 4) && aligned(vs, 4));
 }
 
@@ -249,29 +254,30 @@ PagedIoArgs io_args(const pdec_paged_dims* d)
 constexpr int kAppendMany = 2048;
 constexpr int kReadRows = 4;  // rows per wave of the read-back (32768 rows: 24.2 us, by 8 26.8, by 16 25.7)
 
-template <int D, typename T, bool QUANT, int N>
+template <int D, typename T, PagedForm FORM, int N>
 void launch_append(const PagedIoArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)std::max((a.num_tokens + 4 * N - 1) / (4 * N), (a.num_seqs + 63) / 64), 2);
-    hipLaunchKernelGGL((paged_append_kernel<D, T, QUANT, N>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_append_kernel<D, T, FORM, N>), grid, dim3(256), 0, s, a);
 }
 
-template <int D, typename T, bool QUANT>
+template <int D, typename T, PagedForm FORM>
 void launch_read(const PagedIoArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.num_tokens + 4 * kReadRows - 1) / (4 * kReadRows)), 2);
-    hipLaunchKernelGGL((paged_read_kernel<D, T, QUANT, kReadRows>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_read_kernel<D, T, FORM, kReadRows>), grid, dim3(256), 0, s, a);
 }
 
-// f(head dim, an element of the rows' type, whether the cache is e4m3), as types
+// f(head dim, an element of the rows' type, the cache's form), as types
 template <typename F>
 void for_types(const pdec_paged_dims* d, F f)
 {
-    const bool q = d->cache_dtype == PDEC_DTYPE_E4M3, f32 = d->dtype == PDEC_DTYPE_F32;
-    auto types = [&](auto dim) {
-        if (f32) q ? f(dim, float{}, std::true_type{}) : f(dim, float{}, std::false_type{});
-        else q ? f(dim, uint16_t{}, std::true_type{}) : f(dim, uint16_t{}, std::false_type{});
+    auto forms = [&](auto dim, auto t) {
+        if (d->cache_dtype == PDEC_DTYPE_E2M1) f(dim, t, std::integral_constant<PagedForm, kE2m1Rows>{});
+        else if (d->cache_dtype == PDEC_DTYPE_E4M3) f(dim, t, std::integral_constant<PagedForm, kE4m3Rows>{});
+        else f(dim, t, std::integral_constant<PagedForm, kPlainRows>{});
     };
+    auto types = [&](auto dim) { d->dtype == PDEC_DTYPE_F32 ? forms(dim, float{}) : forms(dim, uint16_t{}); };
     if (d->head_dim == 128) types(std::integral_constant<int, 128>{});
     else types(std::integral_constant<int, 64>{});
 }
@@ -403,14 +409,13 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
     };
     if (p.use_many) {
         place(p.many, ws + align256(p.few_bytes));
-        launch_paged_rows(p.many, d->head_dim, d->cache_dtype == PDEC_DTYPE_E4M3, s);
+        launch_paged_rows(p.many, d->head_dim, d->cache_dtype, s);
         if ((rc = launched()) != PDEC_OK || (rc = finish(p.many)) != PDEC_OK) return rc;
     }
     if (p.use_few) {
         place(p.few, ws);
-        const bool fp8 = d->cache_dtype == PDEC_DTYPE_E4M3;
-        if (d->dtype == PDEC_DTYPE_F32) launch_paged_f32(p.few, d->head_dim, fp8, s);
-        else launch_paged_few(p.few, d->head_dim, fp8, s);
+        if (d->dtype == PDEC_DTYPE_F32) launch_paged_f32(p.few, d->head_dim, d->cache_dtype, s);
+        else launch_paged_few(p.few, d->head_dim, d->cache_dtype, s);
         if ((rc = launched()) != PDEC_OK || (rc = finish(p.few)) != PDEC_OK) return rc;
     }
     return PDEC_OK;

@@ -5,7 +5,9 @@
 #include <hip/hip_runtime.h>
 
 #include "kernel_paged_few.h"
+#include "kernel_paged_few4.h"
 #include "kernel_paged_rows.h"
+#include "pdec.h"
 
 namespace pdec {
 
@@ -30,19 +32,36 @@ void launch_few(const PagedArgs& a, hipStream_t s)
     }
 }
 
+template <int D>
+void launch_few4(const PagedArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)a.blocks), block(64 * kFewWaves);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few4_kernel<D, 1>), grid, block, 0, s, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((paged_few4_kernel<D, 2>), grid, block, 0, s, a);
+    else if constexpr (D == 64) {
+        if (a.rows == 48) hipLaunchKernelGGL((paged_few4_kernel<D, 3>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((paged_few4_kernel<D, 4>), grid, block, 0, s, a);
+    }
+}
+
 }  // namespace
 
-void launch_paged_few(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
+void launch_paged_few(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
 {
-    const bool two = a.heads == 2;
+    if (cache_dtype == PDEC_DTYPE_E2M1) {
+        head_dim == 128 ? launch_few4<128>(a, s) : launch_few4<64>(a, s);
+        return;
+    }
+    const bool two = a.heads == 2, fp8 = cache_dtype == PDEC_DTYPE_E4M3;
     if (head_dim == 128 && !fp8) launch_few<128, false, 1>(a, s);
     else if (head_dim == 128) two ? launch_few<128, true, 2>(a, s) : launch_few<128, true, 1>(a, s);
     else if (fp8) two ? launch_few<64, true, 2>(a, s) : launch_few<64, true, 1>(a, s);
     else two ? launch_few<64, false, 2>(a, s) : launch_few<64, false, 1>(a, s);
 }
 
-void launch_paged_rows(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
+void launch_paged_rows(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
 {
+    const bool fp8 = cache_dtype == PDEC_DTYPE_E4M3;
     if (head_dim == 128) fp8 ? launch_rows<128, true>(a, s) : launch_rows<128, false>(a, s);
     else fp8 ? launch_rows<64, true>(a, s) : launch_rows<64, false>(a, s);
 }

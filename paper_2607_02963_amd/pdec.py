@@ -27,6 +27,7 @@ NOALLOC_SCRATCH_BYTES = 32 << 20
 PDEC_DTYPE_F32 = 0
 PDEC_DTYPE_BF16 = 1
 PDEC_DTYPE_E4M3 = 2
+PDEC_DTYPE_E2M1 = 3
 
 PATH_AUTO, PATH_VALU, PATH_MFMA, PATH_MFMA32 = 0, 1, 2, 3
 
@@ -669,6 +670,8 @@ def make_paged_dims(num_seqs, num_tokens, H_q, H_kv, D, page_size, num_pages, ma
 
 
 def _cache_code(pages: torch.Tensor) -> int:
+    if pages.dtype is torch.uint8:  # two e2m1 values a byte
+        return PDEC_DTYPE_E2M1
     return PDEC_DTYPE_E4M3 if pages.dtype == torch.float8_e4m3fn else _dtype_code(pages)
 
 
@@ -688,7 +691,7 @@ def _paged_dims(num_tokens, H_q, pool, table, dtype_code, cache_code, max_chunk,
 
 def paged_dims_of(q, k_pages, block_table, *, causal=True, max_chunk=None, max_len=None, scale=0.0) -> PagedDims:
     """The dims of a ``paged_attn`` call on these tensors, for ``paged_workspace_size`` and ``query_paged_plan``."""
-    P, page, H_kv, D = k_pages.shape
+    P, page, H_kv, D = _paged_sizes(k_pages, "k_pages", block_table)[0]
     return make_paged_dims(block_table.shape[0], q.shape[0], q.shape[1], H_kv, D, page, P, block_table.shape[1],
                            _dtype_code(q), _cache_code(k_pages), max_chunk=max_chunk or 0, max_len=max_len or 0,
                            causal=bool(causal), scale=scale)
@@ -737,10 +740,15 @@ def _ptr(t, name, dev, dtype, shape):
 
 
 def _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, shape):
-    """Addresses (k, v, k scales, v scales) of a paged cache."""
+    """Addresses (k, v, k scales, v scales) of a paged cache; shape is (pages, tokens of one, heads, head dim)."""
+    if k_pages.dtype is torch.uint8:
+        (P, page, H_kv, D), u8 = shape, torch.uint8
+        rows, sc = (P, H_kv, page, D // 2), (P, H_kv, page, D // 32)
+        return (_ptr(k_pages, "k_pages", dev, u8, rows), _ptr(v_pages, "v_pages", dev, u8, rows),
+                _ptr(k_scales, "k_scales", dev, u8, sc), _ptr(v_scales, "v_scales", dev, u8, sc))
     if k_pages.dtype is not torch.float8_e4m3fn:
         if k_scales is not None or v_scales is not None:
-            raise ValueError("only an e4m3 cache has scales")
+            raise ValueError("only an e4m3 or a 4-bit cache has scales")
         return _ptr(k_pages, "k_pages", dev, dtype, shape), _ptr(v_pages, "v_pages", dev, dtype, shape), None, None
     sc = (shape[0], shape[2], shape[1])
     return (_ptr(k_pages, "k_pages", dev, torch.float8_e4m3fn, shape), _ptr(v_pages, "v_pages", dev, torch.float8_e4m3fn, shape),
@@ -748,11 +756,14 @@ def _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, shape):
 
 
 def _paged_sizes(pages, name, block_table):
-    """Shape of a pool of pages (a tuple of four) and of its block table."""
+    """Sizes of a pool (pages, tokens of one, heads, head dim) and of its block table."""
     if not isinstance(pages, torch.Tensor) or pages.dim() != 4:
         raise ValueError(f"{name} must be a [num_pages, page_size, H_kv, D] tensor")
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be a [num_seqs, max_pages] tensor")
+    if pages.dtype is torch.uint8:  # 4 bits: [num_pages, H_kv, page_size, D / 2]
+        P, H_kv, page, half = pages.shape
+        return (P, page, H_kv, 2 * half), tuple(block_table.shape)
     return tuple(pages.shape), tuple(block_table.shape)
 
 
@@ -770,7 +781,8 @@ def paged_kv_append(k_new, v_new, k_pages, v_pages, block_table, cu_tokens, lens
     """Append the new tokens' keys and values to their sequences' pages (``pdec_paged_kv_append``).
 
     k_new/v_new [T,H_kv,D] float32 or bf16; k_pages/v_pages [P,page,H_kv,D] of the same dtype, or
-    ``torch.float8_e4m3fn`` with k_scales/v_scales uint8 [P,H_kv,page]; block_table int32 [S,max_pages];
+    ``torch.float8_e4m3fn`` with k_scales/v_scales uint8 [P,H_kv,page], or 4 bits: uint8 [P,H_kv,page,D/2] (two
+    values a byte, the even element low) with k_scales/v_scales uint8 [P,H_kv,page,D/32]; block_table int32 [S,max_pages];
     cu_tokens int32 [S+1]; lens_in int32 [S] (keys before), lens_out int32 [S] (another tensor: keys after).
     """
     dev, code = _device_of(k_new, "k_new")
@@ -793,7 +805,7 @@ def paged_kv_read(k_pages, v_pages, block_table, seq_lens, cu_rows, *, k_out=Non
     """Pages as dense rows (``pdec_paged_kv_read``); returns (k_out, v_out) [R,H_kv,D].
 
     Row cu_rows[s] + t receives key t of sequence s, 0 at or beyond seq_lens[s].  Give k_out and v_out, or
-    ``num_rows`` (and ``dtype``, by default bf16 for an e4m3 cache).  Other arguments as for ``paged_kv_append``.
+    ``num_rows`` (and ``dtype``, by default bf16 for an 8- or 4-bit cache).  Other arguments as for ``paged_kv_append``.
     """
     dev, _ = _device_of(k_pages, "k_pages", rows=False)
     pool, table = _paged_sizes(k_pages, "k_pages", block_table)
@@ -804,7 +816,7 @@ def paged_kv_read(k_pages, v_pages, block_table, seq_lens, cu_rows, *, k_out=Non
         if num_rows is None:
             raise ValueError("num_rows is required without k_out and v_out")
         if dtype is None:
-            dtype = torch.bfloat16 if k_pages.dtype == torch.float8_e4m3fn else k_pages.dtype
+            dtype = torch.bfloat16 if k_pages.dtype in (torch.float8_e4m3fn, torch.uint8) else k_pages.dtype
         k_out, v_out = (_empty(stream, (num_rows,) + pool[2:], dtype, k_pages.device) for _ in "kv")
     dtype, shape = k_out.dtype, (k_out.shape[0],) + pool[2:]
     dims = _paged_dims(shape[0], pool[2], pool, table, _dtype_code(k_out), _cache_code(k_pages), 0, max_len or 0, 1, 0.0)
