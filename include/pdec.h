@@ -685,6 +685,138 @@ int pdec_check_paged_lengths(const pdec_paged_dims* dims, const int32_t* cu, con
 int pdec_merge_states(int64_t num_rows, int32_t head_dim, int32_t dtype, const void* out_a, const float* lse_a,
                       const void* out_b, const float* lse_b, void* out, float* lse, void* stream);
 
+/*
+ * ---- Block tables ----
+ *
+ * The tables that the paged calls read, made on the device from the lengths of a
+ * step's requests: which pages of the pool the new tokens get, and where the tokens
+ * of each sequence start in the batch.  The pool's free pages are a stack, entries
+ * [0, count) of an array.
+ */
+typedef struct pdec_table_dims {
+    int32_t num_seqs;   /* S, 1..2^27                                                     */
+    int32_t num_tokens; /* reserve: tokens that the batch has room for, 1..2^27           */
+    int32_t page_size;  /* tokens per page: a power of two, 16..1024                      */
+    int32_t num_pages;  /* pages of the pool, and entries of free_pages, >= 1             */
+    int32_t max_pages;  /* columns of block_table, >= 1; max_pages * page_size <= 2^30    */
+    int32_t max_len;    /* most keys of a sequence; 0 means max_pages * page_size.  Only  */
+                        /* the entries of so many keys are looked at                      */
+} pdec_table_dims;
+
+/* Bytes of workspace the two calls need (0 for invalid dims).  Host only. */
+size_t pdec_table_workspace_size(const pdec_table_dims* dims);
+
+/*
+ * Gives the new tokens of every sequence their places.  Sequence s has seq_lens[s]
+ * keys and asks for new_tokens[s] more; of the entries of its row of block_table
+ * that those keys need, the ones outside [0, num_pages) lack a page.  Sequences are
+ * served in order while the pages that they lack, summed up, are in the free list
+ * and their new tokens fit in num_tokens; the first that does not fit, and all behind
+ * it, get nothing.  A request that cannot be (a negative length or count, more than
+ * max_len keys) is passed over: it counts as one for no tokens.
+ *   block_table [S, max_pages]      the served sequences' lacking entries are written:
+ *                                   in order of s, then of the entry, from the end of
+ *                                   the free list downwards; nothing else is;
+ *   free_pages [num_pages]          read; free_in [1] its count before, free_out [1]
+ *                                   after (another array);
+ *   cu_tokens [S + 1]               written: the served sequences' tokens, as the paged
+ *                                   calls take them; a sequence that is not served has none;
+ *   positions [num_tokens] int32    written, or NULL: token t's number in its sequence,
+ *                                   seq_lens[s] upwards;
+ *   slots [num_tokens] int64        written, or NULL: the token's row of the pool,
+ *                                   page * page_size + its row in the page.
+ * Positions and slots behind the last token are left as they were.  All arrays are
+ * int32 in device memory but slots; workspace: >= pdec_table_workspace_size(dims)
+ * bytes, device, 16-byte aligned, contents ignored.  A page must be in the free list
+ * and the tables once at most; pages outside [0, num_pages) count as lacking
+ * afterwards.  Asynchronous on `stream`.  Returns a pdec_status.
+ */
+int pdec_paged_reserve(const pdec_table_dims* dims, const int32_t* new_tokens, const int32_t* seq_lens,
+                       int32_t* block_table, const int32_t* free_pages, const int32_t* free_in, int32_t* free_out,
+                       int32_t* cu_tokens, int32_t* positions, int64_t* slots, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/*
+ * Gives back the pages that a sequence does not keep: with keep_from[s] (NULL: 0) and
+ * keep_len[s], those of its row that hold no key of [keep_from, keep_len).  A sequence
+ * that has ended keeps nothing (keep_len 0), one whose drafted tokens are refused its
+ * accepted length, one with a sliding window its last keys.  The entries become -1, the
+ * pages go to the end of the free list in the opposite order of the reservation (from
+ * the last sequence's last entry), so that a reservation of the same keys takes them
+ * again.  Arrays as above (free_pages is written).  Asynchronous on `stream`.
+ * Returns a pdec_status.
+ */
+int pdec_paged_release(const pdec_table_dims* dims, const int32_t* keep_from, const int32_t* keep_len,
+                       int32_t* block_table, int32_t* free_pages, const int32_t* free_in, int32_t* free_out,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Rotary positions ----
+ *
+ * Of a head's first R = rotary_dim elements pair i, the elements i and i + R/2, or 2i
+ * and 2i + 1 (interleaved), turns by pos * f_i:
+ *   y_a = m (x_a cos - x_b sin),  y_b = m (x_b cos + x_a sin);
+ * elements R .. D-1 stay.  f_i = theta^(-2i/R), for positions beyond the trained ones
+ *   PDEC_ROPE_LINEAR    f_i / factor;
+ *   PDEC_ROPE_NTK       with theta * factor^(R/(R-2)) in theta's place: the last pair's
+ *                       is divided by factor, the first pair's stays;
+ *   PDEC_ROPE_BY_PARTS  u_i f_i + (1 - u_i) f_i / factor, u_i = (turns_i - slow_turns) /
+ *                       (fast_turns - slow_turns) within [0, 1], turns_i = original_len
+ *                       f_i / 2 pi the pair's turns over the trained length;
+ *   PDEC_ROPE_TABLE     freqs[i], from device memory.
+ * Angles are formed in double.  float32 rows turn in double and are rounded once,
+ * bfloat16 rows in float32.
+ */
+enum { PDEC_ROPE_PLAIN = 0, PDEC_ROPE_LINEAR = 1, PDEC_ROPE_NTK = 2, PDEC_ROPE_BY_PARTS = 3, PDEC_ROPE_TABLE = 4 };
+
+typedef struct pdec_rope_spec {
+    int32_t head_dim;     /* D: 64 or 128                                               */
+    int32_t rotary_dim;   /* R: a multiple of 16, at most D; 0 means D                  */
+    int32_t interleaved;  /* 0: i with i + R/2; 1: 2i with 2i + 1                       */
+    int32_t scaling;      /* PDEC_ROPE_*                                                */
+    double theta;         /* > 0; not looked at with a table                            */
+    double factor;        /* > 0; linear, ntk and by parts                              */
+    double original_len;  /* > 0; by parts                                              */
+    double slow_turns;    /* by parts: pairs of so few turns are divided by the factor, */
+    double fast_turns;    /* pairs of so many not at all; slow_turns < fast_turns       */
+    double magnitude;     /* m; 0 means 1                                               */
+    const double* freqs;  /* table: [R/2], device, 8-byte aligned                       */
+} pdec_rope_spec;
+
+/*
+ * Queries and keys turned by their tokens' positions; with backward = 1 by the
+ * transposed matrix, m times the turn by -pos f_i: given the gradient of a loss with
+ * respect to the turned rows, the gradient with respect to the plain ones.
+ *   positions [num_tokens] int32, device;
+ *   q [num_tokens, num_q_heads, D], k [num_tokens, num_k_heads, D] of dtype (float32 or
+ *   bfloat16), and q_out, k_out the same, device, 16-byte aligned.  A token's heads lie
+ *   one after another, the next token's *_stride elements on (a multiple of 16 bytes, at
+ *   least heads * D): rows of one packed projection, for instance.  q_out may be q and
+ *   k_out k, with the same stride; else outputs overlap no input.  num_k_heads may be 0.
+ * Asynchronous on `stream` (one launch).  Returns a pdec_status.
+ */
+int pdec_rope(const pdec_rope_spec* spec, int64_t num_tokens, int32_t num_q_heads, int32_t num_k_heads, int32_t dtype,
+              int32_t backward, const int32_t* positions, const void* q, int64_t q_stride, void* q_out,
+              int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, void* stream);
+
+/*
+ * pdec_paged_kv_append with the rotary positions of the new tokens: what pdec_rope and
+ * then the append would leave, bit for bit, in one launch.  Key t of sequence s stands
+ * at position pos_base[s] + t (pos_base NULL: t).  dims and the arrays as for the append,
+ * num_q_heads the queries', head_dim the spec's.
+ *   q [num_tokens, H_q, D], k_new, v_new [num_tokens, H_kv, D], q_out [num_tokens, H_q, D]
+ *   device, 16-byte aligned; strides as for pdec_rope.  q_out may be q, with the same
+ *   stride.  Queries of a sequence that is left as it was turn all the same; rows behind
+ *   the last sequence's are not written;
+ *   pos_base [S] int32, device, or NULL.
+ * Asynchronous on `stream` (one launch).  Returns a pdec_status.
+ */
+int pdec_paged_rope_kv_append(const pdec_paged_dims* dims, const pdec_rope_spec* spec, const void* q, int64_t q_stride,
+                              void* q_out, int64_t q_out_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                              int64_t v_stride, const int32_t* pos_base, const int32_t* cu_tokens,
+                              const int32_t* block_table, const int32_t* lens_in, int32_t* lens_out, void* k_pages,
+                              void* v_pages, uint8_t* k_scales, uint8_t* v_scales, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

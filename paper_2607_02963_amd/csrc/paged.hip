@@ -5,14 +5,13 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <memory>
-#include <new>
 
 #include "pdec.h"
 
 #include "kernel_paged_f32.h"
 #include "kernel_paged_finish.h"
 #include "kernel_paged_io.h"
+#include "paged_host.h"
 
 namespace pdec {
 
@@ -71,38 +70,7 @@ namespace {
 
 using namespace pdec;
 
-bool aligned(const void* p, uintptr_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// Rows of a call, and sequences: the launches' threads stay within 32 bits.
-constexpr int kMostRows = 1 << 27;
-
-int check_dims(const pdec_paged_dims* d)
-{
-    if (!d) return PDEC_ERR_INVALID_ARG;
-    if (d->num_seqs < 1 || d->num_tokens < 1 || d->num_q_heads < 1 || d->num_kv_heads < 1 ||
-        d->num_q_heads % d->num_kv_heads != 0 || d->num_pages < 1 || d->max_pages < 1 || d->max_chunk < 0 ||
-        d->max_len < 0 || d->causal < 0 || d->causal > 1 || d->page_size < 1)
-        return PDEC_ERR_INVALID_ARG;
-    if (std::isnan(d->softmax_scale) || std::isinf(d->softmax_scale)) return PDEC_ERR_INVALID_ARG;
-    if (d->dtype != PDEC_DTYPE_F32 && d->dtype != PDEC_DTYPE_BF16) return PDEC_ERR_UNSUPPORTED;
-    if (d->cache_dtype != d->dtype && d->cache_dtype != PDEC_DTYPE_E4M3 && d->cache_dtype != PDEC_DTYPE_E2M1)
-        return PDEC_ERR_UNSUPPORTED;
-    if (d->head_dim != 64 && d->head_dim != 128) return PDEC_ERR_UNSUPPORTED;
-    if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0)
-        return PDEC_ERR_UNSUPPORTED;
-    if (d->num_tokens > kMostRows || d->num_seqs > kMostRows) return PDEC_ERR_UNSUPPORTED;
-    const int64_t most = (int64_t)d->max_pages * d->page_size;
-    if (most > ((int64_t)1 << 30)) return PDEC_ERR_UNSUPPORTED;
-    if (d->max_len > most) return PDEC_ERR_INVALID_ARG;
-    // a token's keys, and a page, within 32-bit offsets (a pool may be larger)
-    if ((int64_t)d->num_kv_heads * d->head_dim * d->page_size * 4 > INT32_MAX) return PDEC_ERR_UNSUPPORTED;
-    return PDEC_OK;
-}
-
 int chunk_bound(const pdec_paged_dims* d) { return d->max_chunk > 0 ? std::min(d->max_chunk, d->num_tokens) : d->num_tokens; }
-int len_bound(const pdec_paged_dims* d) { return d->max_len > 0 ? d->max_len : d->max_pages * d->page_size; }
-int shift_of(int page_size) { return __builtin_ctz((unsigned)page_size); }
-
 // Sequences of at most so many rows per kv head are the few-row kernel's: up to two
 // 16-row tiles at D = 128, four at D = 64 (both sides measured: kernel_paged_few.h).
 int few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
@@ -215,40 +183,6 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
 // What a caller is asked for, also where nothing is cut and nothing is stored.
 size_t workspace_of(const AttnPlan& p) { return std::max<size_t>(align256(p.few_bytes) + p.many_bytes, 16); }
 
-// What the three cache calls share of their pointers' checks.
-bool cache_pointers(const pdec_paged_dims* d, const void* k, const void* v, const uint8_t* ks, const uint8_t* vs)
-{
-    if (!aligned(k, 16) || !aligned(v, 16)) return false;
-    if (d->cache_dtype == PDEC_DTYPE_E2M1) return aligned(ks, 16) && aligned(vs, 16);
-    return d->cache_dtype != PDEC_DTYPE_E4M3 || (aligned(ks, 4) && aligned(vs, 4));
-}
-
-// PDEC_DEBUG=1: the lengths of a call, copied and checked (synchronises).
-int debug_check(const pdec_paged_dims* d, const int32_t* cu, const int32_t* lens, int attn, void* stream)
-{
-    const size_t S = (size_t)d->num_seqs;
-    const std::unique_ptr<int32_t[]> c(new (std::nothrow) int32_t[2 * S + 1]);  // no exception leaves a C entry
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    if (!c || hipMemcpyAsync(c.get(), cu, (S + 1) * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
-        hipMemcpyAsync(c.get() + S + 1, lens, S * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
-        hipStreamSynchronize(s) != hipSuccess)
-        return PDEC_ERR_HIP;
-    return pdec_check_paged_lengths(d, c.get(), c.get() + S + 1, attn);
-}
-
-PagedIoArgs io_args(const pdec_paged_dims* d)
-{
-    PagedIoArgs a{};
-    a.num_seqs = d->num_seqs;
-    a.num_tokens = d->num_tokens;
-    a.H_kv = d->num_kv_heads;
-    a.page_shift = shift_of(d->page_size);
-    a.num_pages = d->num_pages;
-    a.max_pages = d->max_pages;
-    a.max_len = len_bound(d);
-    return a;
-}
-
 // Tokens from which a wave of the append takes four: 16384 tokens of 4 heads of 128 took
 // 15.3 us by one and take 12.0; up to 4096 both take the call's own 8.9.
 constexpr int kAppendMany = 2048;
@@ -267,22 +201,6 @@ void launch_read(const PagedIoArgs& a, hipStream_t s)
     const dim3 grid((unsigned)((a.num_tokens + 4 * kReadRows - 1) / (4 * kReadRows)), 2);
     hipLaunchKernelGGL((paged_read_kernel<D, T, FORM, kReadRows>), grid, dim3(256), 0, s, a);
 }
-
-// f(head dim, an element of the rows' type, the cache's form), as types
-template <typename F>
-void for_types(const pdec_paged_dims* d, F f)
-{
-    auto forms = [&](auto dim, auto t) {
-        if (d->cache_dtype == PDEC_DTYPE_E2M1) f(dim, t, std::integral_constant<PagedForm, kE2m1Rows>{});
-        else if (d->cache_dtype == PDEC_DTYPE_E4M3) f(dim, t, std::integral_constant<PagedForm, kE4m3Rows>{});
-        else f(dim, t, std::integral_constant<PagedForm, kPlainRows>{});
-    };
-    auto types = [&](auto dim) { d->dtype == PDEC_DTYPE_F32 ? forms(dim, float{}) : forms(dim, uint16_t{}); };
-    if (d->head_dim == 128) types(std::integral_constant<int, 128>{});
-    else types(std::integral_constant<int, 64>{});
-}
-
-int launched() { return hipGetLastError() == hipSuccess ? PDEC_OK : PDEC_ERR_HIP; }
 
 }  // namespace
 

@@ -37,7 +37,9 @@ EXPORTED = ("pdec_strerror", "pdec_workspace_size", "pdec_attn_step", "pdec_attn
             "pdec_aggregation_workspace_size", "pdec_aggregate", "pdec_backward_workspace_size", "pdec_query_backward_plan",
             "pdec_attn_prefill_backward", "pdec_read_probe", "pdec_issue_probe", "pdec_check_lengths",
             "pdec_decode_step", "pdec_paged_kv_append", "pdec_paged_kv_read", "pdec_paged_workspace_size",
-            "pdec_query_paged_plan", "pdec_paged_attn", "pdec_check_paged_lengths", "pdec_merge_states")
+            "pdec_query_paged_plan", "pdec_paged_attn", "pdec_check_paged_lengths", "pdec_merge_states",
+            "pdec_table_workspace_size", "pdec_paged_reserve", "pdec_paged_release", "pdec_rope",
+            "pdec_paged_rope_kv_append")
 
 AGGR_MODES = {"uniform": 0, "learned": 1, "attention": 2}
 
@@ -93,6 +95,25 @@ class PagedPlan(ctypes.Structure):
 
     _fields_ = [("rows_few", ctypes.c_int32), ("rows_many", ctypes.c_int32), ("workers", ctypes.c_int32),
                 ("merge_pass", ctypes.c_int32)]
+
+
+class TableDims(ctypes.Structure):
+    """Mirror of ``pdec_table_dims``."""
+
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_tokens", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class RopeSpec(ctypes.Structure):
+    """Mirror of ``pdec_rope_spec``; made by ``rope_spec``."""
+
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("slow_turns", ctypes.c_double), ("fast_turns", ctypes.c_double),
+                ("magnitude", ctypes.c_double), ("freqs", ctypes.c_void_p)]
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 
 
 class PdecError(RuntimeError):
@@ -164,6 +185,17 @@ def lib():
         L.pdec_paged_attn.argtypes = [pp] + [vp] * 11 + [sz, vp]
         L.pdec_check_paged_lengths.restype = ctypes.c_int
         L.pdec_check_paged_lengths.argtypes = [pp, vp, vp, i32]
+        tp, rp, i64 = ctypes.POINTER(TableDims), ctypes.POINTER(RopeSpec), ctypes.c_int64
+        L.pdec_table_workspace_size.restype = sz
+        L.pdec_table_workspace_size.argtypes = [tp]
+        L.pdec_paged_reserve.restype = ctypes.c_int
+        L.pdec_paged_reserve.argtypes = [tp] + [vp] * 10 + [sz, vp]
+        L.pdec_paged_release.restype = ctypes.c_int
+        L.pdec_paged_release.argtypes = [tp] + [vp] * 7 + [sz, vp]
+        L.pdec_rope.restype = ctypes.c_int
+        L.pdec_rope.argtypes = [rp, i64, i32, i32, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.pdec_paged_rope_kv_append.restype = ctypes.c_int
+        L.pdec_paged_rope_kv_append.argtypes = [pp, rp, vp, i64, vp, i64, vp, i64, vp, i64] + [vp] * 10
         L.pdec_merge_states.restype = ctypes.c_int
         L.pdec_merge_states.argtypes = [ctypes.c_int64, i32, i32] + [vp] * 7
         L.pdec_set_path.restype = ctypes.c_int
@@ -900,6 +932,202 @@ def merge_states(out_a, lse_a, out_b, lse_b, *, out=None, lse=None, stream=None)
     if rc != PDEC_OK:
         raise PdecError("pdec_merge_states", rc)
     return out, lse
+
+
+# ---- block tables ----
+
+@functools.lru_cache(maxsize=256)
+def _table_dims(table, num_tokens, page_size, num_pages, max_len):
+    """Dims of a call by its sizes and the workspace it needs; not to be written to."""
+    sizes = (table[0], num_tokens, page_size, num_pages, table[1], max_len)
+    for x in sizes:
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{x} is beyond 32 bits")
+    dims = TableDims(*sizes)
+    return dims, int(lib().pdec_table_workspace_size(ctypes.byref(dims)))
+
+
+def _table_args(block_table, free_pages, free_in, free_out, num_tokens, page_size, max_len, dev, workspace, stream):
+    """(dims, addresses of the table, the list and its two counts, workspace)."""
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be a [num_seqs, max_pages] tensor")
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
+        raise ValueError("free_pages must be a [num_pages] tensor")
+    table, i32 = tuple(block_table.shape), torch.int32
+    dims, size = _table_dims(table, int(num_tokens), int(page_size), free_pages.shape[0], int(max_len or 0))
+    if workspace is None:
+        workspace = _empty(stream, max(size, 16), torch.uint8, block_table.device)
+    return dims, (_ptr(block_table, "block_table", dev, i32, table), _ptr(free_pages, "free_pages", dev, i32, free_pages.shape),
+                  _ptr(free_in, "free_in", dev, i32, (1,)), _ptr(free_out, "free_out", dev, i32, (1,))), workspace
+
+
+def table_workspace_size(num_seqs: int) -> int:
+    """Bytes of workspace that ``paged_reserve`` and ``paged_release`` need for so many sequences."""
+    return _table_dims((int(num_seqs), 1), 1, 16, 1, 0)[1]
+
+
+def paged_reserve(new_tokens, seq_lens, block_table, free_pages, free_in, free_out, *, page_size, cu_tokens=None,
+                  positions=None, slots=None, num_tokens=None, max_len=None, workspace=None, stream=None):
+    """Pages of the pool for the sequences' new tokens (``pdec_paged_reserve``); returns cu_tokens [S+1].
+
+    new_tokens, seq_lens int32 [S]; block_table int32 [S,max_pages], whose entries that lack a page are written;
+    free_pages int32 [num_pages], of which the first free_in[0] are free; free_in, free_out int32 [1].
+    ``positions`` int32 [T] and ``slots`` int64 [T], if given, receive the tokens' positions and rows of the pool;
+    ``num_tokens`` is the batch's room (default: theirs).  Sequences are served in order while their pages and
+    tokens are there: the tokens that s was given are cu_tokens[s+1] - cu_tokens[s].
+    """
+    dev, _ = _device_of(new_tokens, "new_tokens", rows=False)
+    if num_tokens is None:
+        given = positions if positions is not None else slots
+        if given is None:
+            raise ValueError("num_tokens is required without positions and slots")
+        num_tokens = given.shape[0]
+    dims, (table, free, n_in, n_out), workspace = _table_args(block_table, free_pages, free_in, free_out, num_tokens,
+                                                              page_size, max_len, dev, workspace, stream)
+    S, T, i32 = dims.num_seqs, dims.num_tokens, torch.int32
+    if cu_tokens is None:
+        cu_tokens = _empty(stream, (S + 1,), i32, block_table.device)
+    rc = lib().pdec_paged_reserve(
+        dims, _ptr(new_tokens, "new_tokens", dev, i32, (S,)), _ptr(seq_lens, "seq_lens", dev, i32, (S,)), table, free, n_in,
+        n_out, _ptr(cu_tokens, "cu_tokens", dev, i32, (S + 1,)),
+        None if positions is None else _ptr(positions, "positions", dev, i32, (T,)),
+        None if slots is None else _ptr(slots, "slots", dev, torch.int64, (T,)),
+        _ptr(workspace, "workspace", dev, workspace.dtype, workspace.shape), workspace.nbytes,
+        _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_paged_reserve", rc)
+    return cu_tokens
+
+
+def paged_release(keep_len, block_table, free_pages, free_in, free_out, *, page_size, keep_from=None, max_len=None,
+                  workspace=None, stream=None):
+    """Pages that hold none of the keys keep_from .. keep_len - 1 of their sequence back to the pool
+    (``pdec_paged_release``): keep_len, keep_from int32 [S], the others as for ``paged_reserve``."""
+    dev, _ = _device_of(keep_len, "keep_len", rows=False)
+    dims, (table, free, n_in, n_out), workspace = _table_args(block_table, free_pages, free_in, free_out, 1, page_size,
+                                                              max_len, dev, workspace, stream)
+    S, i32 = dims.num_seqs, torch.int32
+    rc = lib().pdec_paged_release(
+        dims, None if keep_from is None else _ptr(keep_from, "keep_from", dev, i32, (S,)),
+        _ptr(keep_len, "keep_len", dev, i32, (S,)), table, free, n_in, n_out,
+        _ptr(workspace, "workspace", dev, workspace.dtype, workspace.shape), workspace.nbytes,
+        _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_paged_release", rc)
+
+
+# ---- rotary positions ----
+
+def rope_spec(head_dim, *, rotary_dim=None, interleaved=False, theta=10000.0, scaling="none", factor=1.0, original_len=0,
+              slow_turns=1.0, fast_turns=32.0, magnitude=1.0, freqs=None) -> RopeSpec:
+    """A rotation (``pdec_rope_spec``), kept for the calls that use it.
+
+    ``scaling``: "none", "linear", "ntk" or "by_parts" (the last with ``original_len``).  ``freqs``, a float64
+    [rotary_dim / 2] tensor on the device, is taken in place of theta's powers; the spec keeps it.
+    """
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    R = int(head_dim if rotary_dim is None else rotary_dim)
+    spec = RopeSpec(int(head_dim), R, int(bool(interleaved)), ROPE_SCALINGS[scaling], float(theta), float(factor),
+                    float(original_len), float(slow_turns), float(fast_turns), float(magnitude), None)
+    if freqs is not None:
+        if scaling != "none":
+            raise ValueError("a table of frequencies takes no scaling")
+        spec.scaling = 4
+        spec.freqs = _dev(freqs, "freqs", torch.float64, 1)
+        if freqs.shape[0] != R // 2:
+            raise ValueError(f"freqs must have {R // 2} elements, got {freqs.shape[0]}")
+        spec.table = freqs
+    return spec
+
+
+def _heads(t, name, dev, dtype, shape):
+    """(address, tokens' stride) of a [T,H,D] tensor whose tokens' heads lie one after another."""
+    try:
+        if t.get_device() == dev and t.dtype is dtype and t.shape == shape:
+            st = t.stride()
+            D = shape[2]
+            if st[2] == 1 and (st[1] == D or shape[1] == 1):
+                return t.data_ptr(), st[0] if shape[0] > 1 else shape[1] * D
+    except AttributeError:
+        pass
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on the device of the call")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    raise ValueError(f"{name}: a token's heads must lie one after another")
+
+
+def _check_spec(spec, dev):
+    if not isinstance(spec, RopeSpec):
+        raise TypeError("spec must be a RopeSpec (rope_spec)")
+    if spec.freqs and spec.table.get_device() != dev:
+        raise ValueError("the spec's freqs are on another device")
+
+
+def rope(q, k, positions, spec, *, backward=False, q_out=None, k_out=None, stream=None):
+    """Queries and keys turned by their tokens' positions (``pdec_rope``); returns (q_out, k_out).
+
+    q [T,H_q,D], k [T,H_k,D] (or None) float32 or bf16, whose tokens may be strided (slices of one projection);
+    positions int32 [T]; spec from ``rope_spec``.  ``backward``: gradients with respect to the turned rows in, with
+    respect to the plain rows out.  q_out, k_out: the rows' own tensors (in place) or others; new ones by default.
+    """
+    dev, code = _device_of(q, "q")
+    _check_spec(spec, dev)
+    if q.dim() != 3 or (k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 3)):
+        raise ValueError("q and k must be [T, heads, D]")
+    dtype, D = q.dtype, spec.head_dim
+    T = q.shape[0]
+    qs = (T, q.shape[1], D)
+    if q_out is None:
+        q_out = _empty(stream, qs, dtype, q.device)
+    ks, kp, kst, kop, kost = (T, 0, D), None, 0, None, 0
+    if k is not None:
+        ks = (T, k.shape[1], D)
+        if k_out is None:
+            k_out = _empty(stream, ks, dtype, q.device)
+        (kp, kst), (kop, kost) = _heads(k, "k", dev, dtype, ks), _heads(k_out, "k_out", dev, dtype, ks)
+    (qp, qst), (qop, qost) = _heads(q, "q", dev, dtype, qs), _heads(q_out, "q_out", dev, dtype, qs)
+    rc = lib().pdec_rope(spec, T, qs[1], ks[1], code, int(bool(backward)), _ptr(positions, "positions", dev, torch.int32, (T,)),
+                         qp, qst, qop, qost, kp, kst, kop, kost, _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_rope", rc)
+    return q_out, k_out
+
+
+def paged_rope_kv_append(q, k_new, v_new, k_pages, v_pages, block_table, cu_tokens, lens_in, lens_out, spec, *,
+                         pos_base=None, q_out=None, k_scales=None, v_scales=None, max_len=None, stream=None):
+    """``paged_kv_append`` with the new tokens' queries and keys turned by their positions
+    (``pdec_paged_rope_kv_append``): what ``rope`` and then the append leave, in one launch; returns q_out.
+
+    q [T,H_q,D], k_new/v_new [T,H_kv,D], strided or not as for ``rope``; key t of sequence s stands at position
+    pos_base[s] + t (``pos_base`` int32 [S]; without it: t).  q_out: q itself (in place) or another tensor; a new one
+    by default.  The rest as for ``paged_kv_append``.
+    """
+    dev, code = _device_of(q, "q")
+    _check_spec(spec, dev)
+    if q.dim() != 3:
+        raise ValueError("q must be [T, heads, D]")
+    pool, table = _paged_sizes(k_pages, "k_pages", block_table)
+    T, S, dtype, i32 = q.shape[0], table[0], q.dtype, torch.int32
+    qs, kvs = (T, q.shape[1], pool[3]), (T,) + pool[2:]
+    if q_out is None:
+        q_out = _empty(stream, qs, dtype, q.device)
+    dims = _paged_dims(T, qs[1], pool, table, code, _cache_code(k_pages), 0, max_len or 0, 1, 0.0)
+    k, v, ks, vs = _paged_cache(k_pages, v_pages, k_scales, v_scales, dtype, dev, pool)
+    rc = lib().pdec_paged_rope_kv_append(
+        dims, spec, *_heads(q, "q", dev, dtype, qs), *_heads(q_out, "q_out", dev, dtype, qs),
+        *_heads(k_new, "k_new", dev, dtype, kvs), *_heads(v_new, "v_new", dev, dtype, kvs),
+        None if pos_base is None else _ptr(pos_base, "pos_base", dev, i32, (S,)), _ptr(cu_tokens, "cu_tokens", dev, i32, (S + 1,)),
+        _ptr(block_table, "block_table", dev, i32, table), _ptr(lens_in, "lens_in", dev, i32, (S,)),
+        _ptr(lens_out, "lens_out", dev, i32, (S,)), k, v, ks, vs, _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != PDEC_OK:
+        raise PdecError("pdec_paged_rope_kv_append", rc)
+    return q_out
 
 
 def check_lengths(dims: Dims, num_videos: int, event_lens, prefix_lens=None, cu_prefix=None, cu_events=None) -> int:
