@@ -19,6 +19,9 @@
 // light.  Turning them where they are read would do it once per wave, four times
 // in all.  The products and all that follows are the same.
 //
+// 4-bit pages (paged_e2m1.h): the same, with half the bytes and, a word being eight
+// elements of one scale, one 16-byte store for four widening instructions.
+//
 // Units that all rows of a wave see whole take that pipelined loop.  Units
 // with hidden keys (the chunk's own tokens, the sequence's end, absent pages)
 // take a plain one, tile by tile, where a value that is not finite meets only
@@ -33,7 +36,7 @@
 #pragma once
 
 #include "kernel_branch.h"
-#include "paged_common.h"
+#include "paged_e2m1.h"
 
 namespace pdec {
 
@@ -69,7 +72,7 @@ __device__ inline void dma_4B_lanes(uint64_t addr, uint32_t lds_base, uint64_t l
                  : "memory");
 }
 
-template <int D, int NT, bool FP8>
+template <int D, int NT, bool FP8, bool Q4 = false>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
 {
     constexpr int NW = 4;
@@ -83,12 +86,19 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
     constexpr int AHEAD = FP8 ? 5 : 3;            // stage moved behind the barrier of stage st: st + AHEAD
     constexpr int FLIGHT = FP8 ? 2 * (PPW + 1) : PPW;  // pieces that may be under way at a barrier
     constexpr int SCALES = FP8 ? 64 : 0;          // bytes for the 32 scales of a raw slot
+    // 4 bits (FP8 too: raw slots, turned): a half is 16 consecutive rows of its head, one piece;
+    // the scales stand in the raw slot behind the rows
+    constexpr unsigned C4 = D / 32;               // 16-byte chunks, and scales, per key
+    constexpr unsigned ROWS4 = 16 * D, HALF4 = ROWS4 / 2, TURNS4 = ROWS4 / 1024;
+    constexpr uint64_t LANES4 = HALF4 == 1024 ? ~0ull : (1ull << (HALF4 / 16)) - 1;
+    static_assert(!Q4 || FP8, "4-bit rows are turned as 8-bit rows are");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[NB * C::STAGE + NW * NRAW * (RAW + SCALES)];
 
     const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
     PagedRun run;
     PagedPart part;
     if (!paged_begin(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
+    constexpr unsigned UNDER_WAY = Q4 ? 2 * (2 + 1) : FLIGHT;
     __shared__ int find_s[2][2][NW];  // see below; two sets, used in turn
     int turn_s = 0;
 
@@ -112,7 +122,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             const int key = 32 * (w % 2) + pkey + i * KPI;
             // bfloat16 pieces land in the ring's permuted places, raw ones in a row
             const int ch = FP8 ? lane % CPK : (lane % CPK) ^ (w_is_v ? branch_vswz<D>(key) : branch_kswz<D>(key));
-            off[i] = (uint32_t)(pkey + (i % (PPW / 2)) * KPI) * strideB + 16u * ch;
+            off[i] = Q4 ? 16u * lane : (uint32_t)(pkey + (i % (PPW / 2)) * KPI) * strideB + 16u * ch;
         }
         static_assert(16 % KPI == 0 && PPW * KPI == 32 && (PPW / 2 <= 4), "a wave's pieces are two halves of 16 keys");
         unsigned char* const ring_w = lds + (w_is_v ? C::STAGE_K : 0) + 32 * (w % 2) * C::ROWB;  // its keys of slot 0
@@ -121,7 +131,8 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         // 8-bit pages: the lane's first chunk, of key pkey, in raw slot 0 and in slot 0 of
         // the ring; the keys of every second piece have bit 3, which permutes K chunks
         const uint32_t raw0 = lds_u32(raw_w) + 16 * lane;
-        const uint32_t ring0 = lds_u32(ring_w) + pkey * C::ROWB + 16 * ((2 * (lane % CPK)) ^ (w_is_v ? branch_vswz<D>(pkey) : branch_kswz<D>(pkey)));
+        const int tkey = Q4 ? lane / (int)C4 : pkey, tch = Q4 ? 4 * (lane % (int)C4) : 2 * (lane % CPK);
+        const uint32_t ring0 = lds_u32(ring_w) + tkey * C::ROWB + 16 * (tch ^ (w_is_v ? branch_vswz<D>(tkey) : branch_kswz<D>(tkey)));
         const uint32_t kflip = w_is_v ? 0 : 128;
         const uint32_t sc_base = lds_u32(lds) + NB * C::STAGE + NW * NRAW * RAW + w * NRAW * SCALES;
         static_assert(!FP8 || D == 64 || KPI == 8, "branch_kswz takes bits 0 to 3 of a key at D = 128, 1 to 3 at D = 64");
@@ -213,10 +224,17 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 const int row = (t + 16 * h) & ((1 << a.page_shift) - 1);
                 p.base[h] = base0 + (((uint64_t)(uint32_t)page << a.page_shift) + (uint32_t)row) * strideB;
                 sc[h] = scales + ((((uint64_t)(uint32_t)page * a.H_kv + part.head) << a.page_shift) + (uint32_t)row);
+                if constexpr (Q4) {  // a row of its head's
+                    p.base[h] = pool + (sc[h] - scales) * (D / 2);
+                    sc[h] = scales + (sc[h] - scales) * C4;
+                }
             }
             p.dst = m_base + (FP8 ? (st % NRAW) * RAW : (st % NB) * C::STAGE);
             p.lanes = ring_lanes(st, nst);
-            if constexpr (FP8) {  // lanes 0 .. 3 the first half's 16 bytes, 4 .. 7 the second's
+            if constexpr (Q4) {  // 4 C4 lanes the first half's 16 C4 bytes, as many the second's
+                p.scale = (lane & (4 * C4) ? sc[1] : sc[0]) + 4 * (lane & (4 * C4 - 1));
+                p.scale_dst = p.dst + ROWS4;
+            } else if constexpr (FP8) {  // lanes 0 .. 3 the first half's 16 bytes, 4 .. 7 the second's
                 p.scale = (lane & 4 ? sc[1] : sc[0]) + 4 * (lane & 3);
                 p.scale_dst = sc_base + (st % NRAW) * SCALES;
             }
@@ -226,6 +244,12 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             dma_16B_page(pd.base[i / (PPW / 2)], off[i & 3], pd.dst + 1024 * i, pd.lanes);
         };
         auto issue_stage = [&](const Pending& pd) __attribute__((always_inline)) {
+            if constexpr (Q4) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) dma_16B_page(pd.base[h], off[0], pd.dst + HALF4 * h, pd.lanes & LANES4);
+                dma_4B_lanes(pd.scale, pd.scale_dst, pd.lanes & ((1ull << (8 * C4)) - 1));
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < PPW; ++i) issue_piece(pd, i);
             if constexpr (FP8) dma_4B_lanes(pd.scale, pd.scale_dst, pd.lanes & 255u);
@@ -243,16 +267,23 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
         float scale[2];
         struct Turn { uint32_t from, sc, to; };
         auto turn_of = [&](int st) __attribute__((always_inline)) {
-            return Turn{raw0 + (st % NRAW) * RAW, sc_base + (st % NRAW) * SCALES + pkey, ring0 + (st % NB) * C::STAGE};
+            const uint32_t from = raw0 + (st % NRAW) * RAW, to = ring0 + (st % NB) * C::STAGE;
+            // 4 bits: the lane's chunk i has the scale 64 i + lane
+            if constexpr (Q4) return Turn{from, from - 15 * lane + ROWS4, to};
+            return Turn{from, sc_base + (st % NRAW) * SCALES + pkey, to};
         };
         auto read_raw = [&](const Turn& u, int i) __attribute__((always_inline)) {
             raw[i & 1] = *reinterpret_cast<const lds_u32x4_t*>((uintptr_t)(u.from + 1024 * i));
-            scale[i & 1] = paged_scale(*reinterpret_cast<const lds_u8_t*>((uintptr_t)(u.sc + KPI * i)), 0);
+            scale[i & 1] = paged_scale(*reinterpret_cast<const lds_u8_t*>((uintptr_t)(u.sc + (Q4 ? 64 : KPI) * i)), 0);
         };
         auto turn = [&](const Turn& u, int m) __attribute__((always_inline)) {
             const int i = m / 4, j = m % 4;
-            if (j == 0 && i + 1 < PPW) read_raw(u, i + 1);
+            if (j == 0 && i + 1 < (Q4 ? (int)TURNS4 : PPW)) read_raw(u, i + 1);
             const uint32_t word = raw[i & 1][j];
+            if constexpr (Q4) {  // a word is eight elements: all of chunk 4 (lane % C4) + j of its key
+                *reinterpret_cast<lds_u32x4_t*>((uintptr_t)((u.to ^ (16 * j)) + i * (64 / C4) * C::ROWB)) = e2m1_bf16(word, scale[i & 1]);
+                return;
+            }
             wide[2 * (j & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, scale[i & 1], false));
             wide[2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, scale[i & 1], true));
             if (j & 1) {
@@ -260,7 +291,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 *reinterpret_cast<lds_u32x4_t*>((uintptr_t)((u.to ^ flip) + i * KPI * C::ROWB)) = wide;
             }
         };
-        constexpr int ITEMS = 4 * PPW;
+        constexpr int ITEMS = Q4 ? 4 * TURNS4 : 4 * PPW;
         auto turn_stage = [&](int st) __attribute__((always_inline)) {
             const Turn u = turn_of(st);
             read_raw(u, 0);
@@ -428,7 +459,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
                 phase_a(sb, sa, pk, kf, vf, vbuf, 0);
                 const Pending pd = pending(st + AHEAD, ahead);
                 ahead = pages(st + AHEAD + 1);
-                stage_barrier<FLIGHT>();
+                stage_barrier<UNDER_WAY>();
                 const Turn u = turn_of(st + 2);
                 if constexpr (FP8) read_raw(u, 0);
                 phase_b(
@@ -463,7 +494,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs a)
             {
                 const Pending pd = pending(st + AHEAD, ahead);
                 ahead = pages(st + AHEAD + 1);
-                stage_barrier<FLIGHT>();
+                stage_barrier<UNDER_WAY>();
                 if constexpr (FP8) {
                     turn_stage(st + 2);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the raw slot has been read

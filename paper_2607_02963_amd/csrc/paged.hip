@@ -150,7 +150,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     a.rows_to = INT32_MAX;
     a.heads = 1;
     p.few = p.many = a;
-    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d->head_dim) && d->cache_dtype != PDEC_DTYPE_E2M1;
+    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d->head_dim);
     // One sequence is the many rows' whatever its chunk, and so are all where none has
     // more rows than a 128-row item: a second kernel and its finish pass cost more than
     // the rows left empty (24 sequences of 300 to 4000 keys, one of 16 new tokens and the

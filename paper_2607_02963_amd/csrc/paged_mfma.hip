@@ -13,11 +13,11 @@ namespace pdec {
 
 namespace {
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool Q4 = false>
 void launch_rows(const PagedArgs& a, hipStream_t s)
 {
-    if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<D, 2, FP8>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
+    if (a.rows == 256) hipLaunchKernelGGL((paged_rows_kernel<D, 2, FP8, Q4>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_rows_kernel<D, 1, FP8, Q4>), dim3((unsigned)a.blocks), dim3(256), 0, s, a);
 }
 
 template <int D, bool FP8, int HW>
@@ -61,6 +61,10 @@ void launch_paged_few(const PagedArgs& a, int head_dim, int cache_dtype, hipStre
 
 void launch_paged_rows(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
 {
+    if (cache_dtype == PDEC_DTYPE_E2M1) {
+        head_dim == 128 ? launch_rows<128, true, true>(a, s) : launch_rows<64, true, true>(a, s);
+        return;
+    }
     const bool fp8 = cache_dtype == PDEC_DTYPE_E4M3;
     if (head_dim == 128) fp8 ? launch_rows<128, true>(a, s) : launch_rows<128, false>(a, s);
     else fp8 ? launch_rows<64, true>(a, s) : launch_rows<64, false>(a, s);
