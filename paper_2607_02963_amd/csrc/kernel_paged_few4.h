@@ -15,7 +15,9 @@
 // A lane's 16 bytes of a key row (8 at D = 64) have one scale, which the widening
 // v_cvt_scalef32_pk_bf16_fp4 takes with it.  A lane's 16 values have a scale each, so
 // that those multiply the probabilities, once for each block of 32 d, before they are
-// rounded: a power of two takes no bits.
+// rounded: a power of two takes no bits.  Where every row sees the block and no scale is
+// NaN, that is an addition to the exponents of two rounded probabilities at a time, of
+// scales that the wave has spread in LDS as bfloat16 exponents.
 #pragma once
 
 #include "kernel_paged_few.h"
@@ -41,7 +43,8 @@ __device__ inline void dma_16B_lanes(uint64_t addr, uint32_t lds_base, uint64_t 
 // inline assembly the compiler would not keep it apart from a v_exp_f32 before it).
 __device__ float mul_zero(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
 
-template <int D, int NT>
+// BIG: pages of 64 keys or more, a block to a page.
+template <int D, int NT, bool BIG>
 __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 {
     constexpr int NW = kFewWaves;
@@ -55,14 +58,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     constexpr int QB = 16 * ROWB;                // bytes of a quarter, one DMA instruction
     constexpr int SPK = D / kE2m1Block;          // scales per key
     constexpr int SC = 2 * KB * SPK;             // bytes of a block's scales
-    constexpr int PB = 9;                        // instructions per block: K's and V's quarters, the scales
+    constexpr int PT = BIG ? TENSOR / 1024 : 4;  // instructions of K or V per block
+    constexpr int PB = 2 * PT + 1;               // and of a block, its scales with them
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
-    constexpr uint64_t QLANES = QB == 1024 ? ~0ull : (1ull << (QB / 16)) - 1;
+    constexpr uint64_t QLANES = BIG || QB == 1024 ? ~0ull : (1ull << (QB / 16)) - 1;
     constexpr uint64_t SLANES = (1ull << (SC / 16)) - 1;
     static_assert(KB == 64 && QB <= 1024 && (NS - 1) * PB < 64, "a block's instructions, and the wait that counts them");
     static_assert(16 * OROW * 4 <= RING, "merge buffer");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + NW * NS * SC];
+    constexpr int EXPS = 2 * KB * SPK;           // bytes of a wave's exponents: SPK times KB keys
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + NW * NS * SC + NW * EXPS];
     __shared__ float m_s[NW][16], l_s[NW][16];
 
     const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
@@ -73,22 +78,21 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 
     const float c = a.qscale;
     const uint32_t ring = lds_u32(lds) + w * RING, sc_ring = lds_u32(lds) + NW * RING + w * NS * SC;
-    // byte offset of the lane's chunk in a quarter
-    uint32_t koffs[4], voffs;
-    {
-        const int k = lane / CPK & 15;  // (at D = 64 the upper lanes take no part)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) koffs[q] = (uint32_t)k * ROWB + 16 * ((lane % CPK) ^ few4_kswz<D>(16 * q + k));
-        voffs = (uint32_t)k * ROWB + 16 * ((lane % CPK) ^ few4_vswz<D>(k));
-    }
+    const uint32_t exps = lds_u32(lds) + NW * RING + NW * NS * SC + w * EXPS;
+    // byte offset of the lane's chunk in instruction i (of a quarter, or 1 KB: dma_rows): of V the
+    // same for all, of K with the bits flipped that the quarter's number permutes
+    constexpr int KPI = QLANES == ~0ull ? 1024 / ROWB : 16;  // keys of an instruction
+    const int ikey = lane / CPK % KPI;
+    const uint32_t koff = (uint32_t)ikey * ROWB + 16 * ((lane % CPK) ^ few4_kswz<D>(ikey));
+    const uint32_t voff = (uint32_t)ikey * ROWB + 16 * ((lane % CPK) ^ few4_vswz<D>(ikey & 15));
     // operand reads, relative to a slot: key 16 (l16 / 4) + l16 % 4 + 4 kt of K, the lane's elements;
-    // key 16 lg + l16 of V, eight bytes of tile dt
-    uint32_t kread, vread[DT];
+    // key 16 lg + l16 of V, eight bytes of tile dt (of which dt / 2 flips bits of the address that
+    // nothing else sets)
+    uint32_t kread;
     const int kkey = 16 * (l16 >> 2) + (l16 & 3), vkey = 16 * lg + l16;
     if constexpr (D == 128) kread = kkey * ROWB + 16 * (lg ^ few4_kswz<D>(kkey));
     else kread = kkey * ROWB + 16 * ((lg >> 1) ^ few4_kswz<D>(kkey)) + 8 * (lg & 1);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) vread[dt] = TENSOR + vkey * ROWB + 16 * ((dt >> 1) ^ few4_vswz<D>(l16)) + 8 * (dt & 1);
+    const uint32_t vread = TENSOR + vkey * ROWB + 16 * few4_vswz<D>(l16);
     const uint32_t ksread = kkey * SPK + (D == 128 ? lg : lg >> 1), vsread = KB * SPK + 16 * lg * SPK;
     typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
     typedef __attribute__((address_space(3))) const u32x2_t lds_u32x2_t;
@@ -112,12 +116,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 
         // the wave's block b: its first key, and its quarters' pages
         auto first = [&](int b) __attribute__((always_inline)) { return t0 + KB * (w + NW * b); };
-        struct Pages { int q[4]; };
+        struct Pages { int q[BIG ? 1 : 4]; };
         auto pages = [&](int b) __attribute__((always_inline)) {
             Pages x;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                x.q[q] = q > 0 && a.page_shift > 5 ? x.q[0] : paged_entry(table, min((first(b) + 16 * q) >> a.page_shift, a.max_pages - 1));
+            for (int q = 0; q < (BIG ? 1 : 4); ++q) x.q[q] = paged_entry(table, min((first(b) + 16 * q) >> a.page_shift, a.max_pages - 1));
             return x;
         };
         auto there = [&](int page) __attribute__((always_inline)) { return (uint32_t)page < (uint32_t)a.num_pages; };
@@ -126,20 +129,35 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
         auto issue = [&](int b, const Pages& x) __attribute__((always_inline)) {
             const uint64_t real = b < mine ? ~0ull : 1ull;
             const uint32_t dst = ring + (b % NS) * SLOT;
-            uint64_t row[4];  // the quarters' rows of the pool
+            uint32_t ko = koff;
+            asm volatile("" : "+v"(ko));  // one register, not one for every instruction
+            uint32_t koffs[PT], voffs[PT];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int page = there(x.q[q]) && b < mine ? x.q[q] : 0;
-                row[q] = (((uint64_t)(uint32_t)page * a.H_kv + head) << a.page_shift) + (uint32_t)((first(b) + 16 * q) & ((1 << a.page_shift) - 1));
+            for (int i = 0; i < PT; ++i) {
+                koffs[i] = ko ^ (16 * few4_kswz<D>(KPI * i));
+                voffs[i] = voff;
             }
+            auto row_of = [&](int q) {  // of the pool
+                const int page = there(x.q[BIG ? 0 : q]) && b < mine ? x.q[BIG ? 0 : q] : 0;
+                return (((uint64_t)(uint32_t)page * a.H_kv + head) << a.page_shift) + (uint32_t)((first(b) + 16 * q) & ((1 << a.page_shift) - 1));
+            };
+            if constexpr (BIG) {
+                const uint64_t row = row_of(0);
+                dma_rows(kbase + row * ROWB, koffs, dst, real);
+                dma_rows(vbase + row * ROWB, voffs, dst + TENSOR, real);
+                dma_16B_lanes(sc_lane + (row + 16 * sq_lane) * SPK, sc_ring + (b % NS) * SC, real & SLANES);
+            } else {
+                uint64_t row[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t off[2][1] = {{koffs[q]}, {voffs}};
-                dma_rows(kbase + row[q] * ROWB, off[0], dst + QB * q, real & QLANES);
-                dma_rows(vbase + row[q] * ROWB, off[1], dst + TENSOR + QB * q, real & QLANES);
+                for (int q = 0; q < 4; ++q) {
+                    row[q] = row_of(q);
+                    const uint32_t off[2][1] = {{koffs[q]}, {voff}};
+                    dma_rows(kbase + row[q] * ROWB, off[0], dst + QB * q, real & QLANES);
+                    dma_rows(vbase + row[q] * ROWB, off[1], dst + TENSOR + QB * q, real & QLANES);
+                }
+                const uint64_t lo = sq_lane & 1 ? row[1] : row[0], hi = sq_lane & 1 ? row[3] : row[2];
+                dma_16B_lanes(sc_lane + (sq_lane & 2 ? hi : lo) * SPK, sc_ring + (b % NS) * SC, real & SLANES);
             }
-            const uint64_t lo = sq_lane & 1 ? row[1] : row[0], hi = sq_lane & 1 ? row[3] : row[2];
-            dma_16B_lanes(sc_lane + (sq_lane & 2 ? hi : lo) * SPK, sc_ring + (b % NS) * SC, real & SLANES);
         };
 
         // ---- this lane's rows: 16 nt + l % 16; those past the last see nothing ----
@@ -178,14 +196,33 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
             wave_wait_vmcnt<(NS - 1) * PB>();  // block b has landed
             const uint32_t slot = ring + (b % NS) * SLOT, scs = sc_ring + (b % NS) * SC;
             const int t = first(b);
-            const bool have[4] = {there(now.q[0]), there(now.q[1]), there(now.q[2]), there(now.q[3])};
+            const bool have[4] = {there(now.q[0]), there(now.q[BIG ? 0 : 1]), there(now.q[BIG ? 0 : 2]), there(now.q[BIG ? 0 : 3])};
             if ((have[0] | have[1] | have[2] | have[3]) && t < most) {
                 const bool all = have[0] & have[1] & have[2] & have[3];
                 const bool full = t + KB <= least && all;
-                const bool mine_there = lg & 2 ? (lg & 1 ? have[3] : have[2]) : (lg & 1 ? have[1] : have[0]);
+                const bool mine_there = BIG ? have[0] : lg & 2 ? (lg & 1 ? have[3] : have[2]) : (lg & 1 ? have[1] : have[0]);
+                // the values' scales of key t + lane, spread by blocks of d as bfloat16 exponents
+                bool odd;  // one of them is NaN
+                {
+                    typedef __attribute__((address_space(3))) const uint16_t lds_u16c_t;
+                    typedef __attribute__((address_space(3))) const uint32_t lds_u32c_t;
+                    typedef __attribute__((address_space(3))) uint16_t lds_u16_t;
+                    uint32_t x;
+                    if constexpr (SPK == 4) x = *(lds_u32c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
+                    else x = *(lds_u16c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
+                    odd = __any((((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u) != 0);
+#pragma unroll
+                    for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)((x >> (8 * i) & 255u) << 7);
+                }
                 // one tile, or all: rows past the last see nothing, or their results are not stored
                 auto block = [&](auto count) __attribute__((always_inline)) {
                     constexpr int N = count;
+                    i32x2_t vraw[DT];
+                    uint32_t vat = slot + vread, eat = exps + 32 * lg;
+                    asm volatile("" : "+v"(vat), "+v"(eat));  // one register each, not one for every read
+                    auto read_v = [&](int dt) __attribute__((always_inline)) {
+                        return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2_t*)(uintptr_t)((vat ^ (16 * (dt >> 1))) + 8 * (dt & 1)));
+                    };
                     float p[N][16];  // scores, then probabilities, of keys t + 16 lg + j
                     {
                         f32x4_t s[N][4];
@@ -209,8 +246,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                             for (int i = 0; i < KS; ++i) {
                                 const bf16x8_t kf = as_bf16x8(e2m1_bf16(x[i], ks));
 #pragma unroll
-                                for (int nt = 0; nt < N; ++nt)
-                                    s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[nt][i]), s[nt][kt]);
+                                for (int nt = 0; nt < N; ++nt) s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[nt][i]), s[nt][kt]);
                             }
                         }
 #pragma unroll
@@ -218,10 +254,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
                             for (int j = 0; j < 16; ++j) p[nt][j] = s[nt][j >> 2][j & 3];
                     }
+                    // the values, asked for under the softmax
+                    if (N == 1) {
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) vraw[dt] = read_v(dt);
+                    }
 #pragma unroll
                     for (int nt = 0; nt < N; ++nt) {
                         if (!full) {
-                            const int lim = mine_there ? seen[nt] - t - 16 * lg : 0;
+                            int lim = mine_there ? seen[nt] - t - 16 * lg : 0;
+                            asm volatile("" : "+v"(lim));  // stays a branch
 #pragma unroll
                             for (int j = 0; j < 16; ++j) p[nt][j] = j >= lim ? kNegInf : p[nt][j];
                         }
@@ -247,34 +289,71 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         // rounded by half a step (2^-8) of each term, as out is
                         lsum[nt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     }
-                    uint32_t vs[4 * SPK];  // the scales of the lane's 16 values
-#pragma unroll
-                    for (int i = 0; i < SPK; ++i) {
-                        const u32x4_t x = *(lds_u32x4_t*)(uintptr_t)(scs + vsread + 16 * i);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) vs[4 * i + e] = x[e];
-                    }
-                    // a hidden value's scale may be NaN: its probability of 0 stays 0
-#pragma unroll
-                    for (int blk = 0; blk < SPK; ++blk) {
-                        if (N > 1) __builtin_amdgcn_sched_barrier(0);
-                        u32x4_t pf[N][2];
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            const float s0 = SPK == 4 ? paged_scale(vs[j], blk) : paged_scale(vs[j / 2], blk);
-                            const float s1 = SPK == 4 ? paged_scale(vs[j + 1], blk) : paged_scale(vs[j / 2], 2 + blk);
-#pragma unroll
-                            for (int nt = 0; nt < N; ++nt)
-                                pf[nt][j >> 3][(j >> 1) & 3] = pack_bf16x2(mul_zero(p[nt][j], s0), mul_zero(p[nt][j + 1], s1));
-                        }
+                    // O += V P of keys 16 lg + 8 h .. + 7, blk's 32 elements
+                    auto products = [&](int blk, int h, const u32x4_t (&pf)[N], auto fast) __attribute__((always_inline)) {
 #pragma unroll
                         for (int dt = 2 * blk; dt < 2 * blk + 2; ++dt) {
-                            const i32x2_t x = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2_t*)(uintptr_t)(slot + vread[dt]));
+                            if (N > 1) vraw[dt] = read_v(dt);
+                            uint32_t x = (uint32_t)(h ? vraw[dt].y : vraw[dt].x);
+                            if (!fast) asm volatile("" : "+v"(x));  // else both paths' widening comes before the branch
+                            const bf16x8_t vf = as_bf16x8(e2m1_bf16(x, 1.f));
+#pragma unroll
+                            for (int nt = 0; nt < N; ++nt) o[nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt]), o[nt][dt]);
+                        }
+                    };
+                    if (full && !odd) {
+                        // P times 2^k: k added to its exponent, in the upper half of 32 bits or less than 0.
+                        // A product below 2^-126 is 0 (and a P of 0 may become 2^-127: nothing beside its
+                        // row's largest, which is 2^-8 at least), one beyond the largest number NaN
+                        typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
+                        i16x2_t pe[N][8];
+#pragma unroll
+                        for (int nt = 0; nt < N; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                pe[nt][j] = __builtin_bit_cast(i16x2_t, pack_bf16x2(p[nt][2 * j], p[nt][2 * j + 1])) - (int16_t)(127 << 7);
+#pragma unroll
+                        for (int blk = 0; blk < SPK; ++blk)
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                const bf16x8_t vf = as_bf16x8(e2m1_bf16((uint32_t)(h ? x.y : x.x), 1.f));
+                                if (N > 1) __builtin_amdgcn_sched_barrier(0);
+                                const u32x4_t e = *(lds_u32x4_t*)(uintptr_t)(eat + 2 * KB * blk + 16 * h);
+                                u32x4_t pf[N];
 #pragma unroll
-                                for (int nt = 0; nt < N; ++nt) o[nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt][h]), o[nt][dt]);
+                                for (int j = 0; j < 4; ++j) {
+                                    const uint32_t ej = e[j];
+#pragma unroll
+                                    for (int nt = 0; nt < N; ++nt) {
+                                        const i16x2_t x = __builtin_elementwise_add_sat(pe[nt][4 * h + j], __builtin_bit_cast(i16x2_t, ej));
+                                        pf[nt][j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, (i16x2_t)0));
+                                    }
+                                }
+                                products(blk, h, pf, std::true_type{});
+                            }
+                    } else {
+                        // a hidden value's scale may be NaN: its probability of 0 stays 0
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t vs[2 * SPK];  // the scales of the lane's values 8 h .. 8 h + 7
+#pragma unroll
+                            for (int i = 0; i < SPK / 2; ++i) {
+                                const u32x4_t x = *(lds_u32x4_t*)(uintptr_t)(scs + vsread + 8 * SPK * h + 16 * i);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) vs[4 * i + e] = x[e];
+                            }
+#pragma unroll
+                            for (int blk = 0; blk < SPK; ++blk) {
+                                if (N > 1) __builtin_amdgcn_sched_barrier(0);
+                                u32x4_t pf[N];
+#pragma unroll
+                                for (int j = 0; j < 8; j += 2) {
+                                    const float s0 = SPK == 4 ? paged_scale(vs[j], blk) : paged_scale(vs[j / 2], blk);
+                                    const float s1 = SPK == 4 ? paged_scale(vs[j + 1], blk) : paged_scale(vs[j / 2], 2 + blk);
+#pragma unroll
+                                    for (int nt = 0; nt < N; ++nt)
+                                        pf[nt][j >> 1] = pack_bf16x2(mul_zero(p[nt][8 * h + j], s0), mul_zero(p[nt][8 * h + j + 1], s1));
+                                }
+                                products(blk, h, pf, std::false_type{});
                             }
                         }
                     }

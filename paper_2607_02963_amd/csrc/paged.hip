@@ -72,8 +72,9 @@ using namespace pdec;
 
 int chunk_bound(const pdec_paged_dims* d) { return d->max_chunk > 0 ? std::min(d->max_chunk, d->num_tokens) : d->num_tokens; }
 // Sequences of at most so many rows per kv head are the few-row kernel's: up to two
-// 16-row tiles at D = 128, four at D = 64 (both sides measured: kernel_paged_few.h).
-int few_rows(int head_dim) { return head_dim == 128 ? 32 : 64; }
+// 16-row tiles at D = 128, four at D = 64 (both sides measured: kernel_paged_few.h);
+// three at D = 64 over 4-bit pages, where four tiles' state would leave the registers.
+int few_rows(const pdec_paged_dims* d) { return d->head_dim == 128 ? 32 : d->cache_dtype == PDEC_DTYPE_E2M1 ? 48 : 64; }
 
 struct AttnPlan {
     PagedArgs few{}, many{};
@@ -150,7 +151,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     a.rows_to = INT32_MAX;
     a.heads = 1;
     p.few = p.many = a;
-    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d->head_dim);
+    p.use_many = d->dtype == PDEC_DTYPE_BF16 && R > few_rows(d);
     // One sequence is the many rows' whatever its chunk, and so are all where none has
     // more rows than a 128-row item: a second kernel and its finish pass cost more than
     // the rows left empty (24 sequences of 300 to 4000 keys, one of 16 new tokens and the
@@ -161,8 +162,8 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         // two 32-row tiles in each wave: a key read from LDS meets twice the rows
         p.many.rows = R <= 128 ? 128 : 256;
         if (p.use_few) {
-            p.many.rows_from = few_rows(d->head_dim) + 1;
-            p.few.rows_to = few_rows(d->head_dim);
+            p.many.rows_from = few_rows(d) + 1;
+            p.few.rows_to = few_rows(d);
         }
         // a work-group per compute unit; a start's price was swept (six chunks of 301 to 1023
         // tokens, 8-bit and bfloat16: 3 526 and 480 us, 6 456 and 418, 9 464 and 421, 14 471 and 424)

@@ -32,16 +32,13 @@ void launch_few(const PagedArgs& a, hipStream_t s)
     }
 }
 
-template <int D>
+template <int D, bool BIG>
 void launch_few4(const PagedArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)a.blocks), block(64 * kFewWaves);
-    if (a.rows == 16) hipLaunchKernelGGL((paged_few4_kernel<D, 1>), grid, block, 0, s, a);
-    else if (a.rows == 32) hipLaunchKernelGGL((paged_few4_kernel<D, 2>), grid, block, 0, s, a);
-    else if constexpr (D == 64) {
-        if (a.rows == 48) hipLaunchKernelGGL((paged_few4_kernel<D, 3>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((paged_few4_kernel<D, 4>), grid, block, 0, s, a);
-    }
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few4_kernel<D, 1, BIG>), grid, block, 0, s, a);
+    else if (a.rows == 32) hipLaunchKernelGGL((paged_few4_kernel<D, 2, BIG>), grid, block, 0, s, a);
+    else if constexpr (D == 64) hipLaunchKernelGGL((paged_few4_kernel<D, 3, BIG>), grid, block, 0, s, a);
 }
 
 }  // namespace
@@ -49,7 +46,9 @@ void launch_few4(const PagedArgs& a, hipStream_t s)
 void launch_paged_few(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
 {
     if (cache_dtype == PDEC_DTYPE_E2M1) {
-        head_dim == 128 ? launch_few4<128>(a, s) : launch_few4<64>(a, s);
+        const bool big = a.page_shift >= 6;
+        if (head_dim == 128) big ? launch_few4<128, true>(a, s) : launch_few4<128, false>(a, s);
+        else big ? launch_few4<64, true>(a, s) : launch_few4<64, false>(a, s);
         return;
     }
     const bool two = a.heads == 2, fp8 = cache_dtype == PDEC_DTYPE_E4M3;

@@ -19,20 +19,30 @@ def constant(name, const, **known):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-def test_few_rows(D):
-    k = {"D": D, "NW": 8, "kUnit": 64, "kE2m1Block": 32}
-    for c in ("RING", "ROWB", "KB", "TENSOR", "SLOT", "NS", "CPK", "QB", "SPK", "SC", "PB"):
+@pytest.mark.parametrize("BIG", [False, True])
+def test_few_rows(D, BIG):
+    k = {"D": D, "BIG": BIG, "NW": 8, "kUnit": 64, "kE2m1Block": 32}
+    for c in ("RING", "ROWB", "KB", "TENSOR", "SLOT", "NS", "CPK", "QB", "SPK", "SC", "PT", "PB", "EXPS"):
         k[c] = constant("kernel_paged_few4.h", c, **k)
-    assert k["NS"] == {64: 4, 128: 2}[D] and k["PB"] == 2 * 4 + 1
-    # eight instructions of a quarter each make the block, one of SC / 16 lanes its scales
-    assert 8 * k["QB"] == k["SLOT"] == 64 * 2 * D // 2 and k["SC"] == 64 * 2 * D // 32
-    assert k["QB"] // 16 <= 64 and k["SC"] // 16 <= 64
-    assert 8 * (k["RING"] + k["NS"] * k["SC"]) <= 160 * 1024 - 8 * 128  # with m_s and l_s
-    # a quarter's lanes cover its 16 rows, each chunk once, whatever the permutation
-    for swz in (lambda key: key >> 4 & (3 if D == 128 else 1), lambda key: key >> 2 & 3 if D == 128 else key >> 3 & 1):
-        for q in range(4):
-            offs = sorted((lane // k["CPK"]) * k["ROWB"] + 16 * ((lane % k["CPK"]) ^ swz(16 * q + lane // k["CPK"])) for lane in range(k["QB"] // 16))
-            assert offs == list(range(0, k["QB"], 16))
+    lanes = 64 if BIG else k["QB"] // 16
+    kpi = 1024 // k["ROWB"] if lanes == 64 else 16
+    assert k["NS"] == {64: 4, 128: 2}[D] and k["PB"] == 2 * k["PT"] + 1 and k["PT"] * kpi == 64
+    # the instructions make the block, one of SC / 16 lanes its scales
+    assert 2 * k["PT"] * 16 * lanes == k["SLOT"] == 64 * 2 * D // 2 and k["SC"] == 64 * 2 * D // 32 and k["SC"] // 16 <= 64
+    assert 8 * (k["RING"] + k["NS"] * k["SC"] + k["EXPS"]) <= 160 * 1024 - 8 * 128  # with m_s and l_s
+    # an instruction's lanes cover its rows, each chunk once, where the reads look for it
+    kswz = lambda key: key >> 4 & (3 if D == 128 else 1)
+    vswz = lambda key: key >> 2 & 3 if D == 128 else key >> 3 & 1
+    for i in range(k["PT"]):
+        for swz, flip, period in ((kswz, kswz(kpi * i), 64), (vswz, 0, 16)):
+            offs = []
+            for lane in range(lanes):
+                ikey = lane // k["CPK"] % kpi
+                off = (ikey * k["ROWB"] + 16 * ((lane % k["CPK"]) ^ swz(ikey % period))) ^ (16 * flip)
+                offs.append(off)
+                key = kpi * i + 16 * lane // k["ROWB"]  # where the lane's bytes land
+                assert off // k["ROWB"] == key - kpi * i and off % k["ROWB"] // 16 == (16 * lane % k["ROWB"] // 16) ^ swz(key % period)
+            assert sorted(offs) == list(range(0, 16 * lanes, 16))
     assert not any(few_rows(k, mine) for mine in range(12))
     assert any(few_rows(k, mine, 1) for mine in range(12))  # the model sees a wait that is one piece short
 
