@@ -10,8 +10,8 @@
 //
 // A wave takes a token (or, where tokens are few, some of its heads).  Lane i forms pair
 // i's cosine and sine, the angle in double and in turns, so that far positions keep them;
-// they pass through LDS to the lanes, 16 elements of a head each, the same for every head:
-// eight pairs' cosines and sines stay in registers.  bfloat16 rows turn in float32 (2^-24 of
+// they pass through LDS to the lanes, 32 bytes of a head each, the same for every head: their
+// pairs' cosines and sines stay in registers.  bfloat16 rows turn in float32 (2^-24 of
 // a term), rounded once; float32 rows in double, whose rate is float32's here, rounded once.
 //
 // What bounds them: the bytes, each read and written once.
@@ -49,25 +49,51 @@ __device__ inline double rope_turns(const RopeSpec& r, int i)
 template <typename T> struct RopeReal { typedef float type; };
 template <> struct RopeReal<float> { typedef double type; };
 
-// The lane's part of a head: 16 elements as two vectors of eight, at off[0] and off[1]; of
-// a turning part eight pairs: elements e of the two, or neighbours within each.
+// 16 bytes of a row, E elements.
+template <typename T>
+struct RopePiece {
+    static constexpr int E = 16 / sizeof(T);
+    u32x4_t x;
+    __device__ inline float get(int i) const
+    {
+        if constexpr (E == 4) return __uint_as_float(x[i]);
+        else return __uint_as_float((i & 1) ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16);
+    }
+    __device__ inline void set(const float (&v)[E])
+    {
+        if constexpr (E == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        }
+    }
+};
+
+// The lane's part of a head: two pieces of E elements, E pairs where it turns.  Of the turning
+// elements piece u of each half, so that neighbouring lanes' pieces are neighbours: halves
+// pair the one with the other, and interleaved pairs lie within each.  The rest the same way.
 template <int D, typename T>
 struct RopeLane {
     typedef typename RopeReal<T>::type real;
-    static constexpr int UNITS = D / 16, HEADS = 64 / UNITS;  // parts of a head; heads of a wave at a time
+    static constexpr int E = RopePiece<T>::E, UNITS = D / (2 * E), HEADS = 64 / UNITS;  // parts of a head; heads of a wave at a time
     int unit, head;   // part of the head, and head of the wave's
     bool turns;
-    int off[2];
-    real c[8], s[8];
+    int off[2], pair[2];  // the pieces, and the first pair of the first E / 2 and of the others
+    real c[E], s[E];
 
     __device__ inline void init(const RopeSpec& r, int lane)
     {
         unit = lane % UNITS;
         head = lane / UNITS;
-        turns = unit < r.R / 16;
-        const bool halves = turns && !r.interleaved;
-        off[0] = halves ? 8 * unit : 16 * unit;
-        off[1] = halves ? r.R / 2 + 8 * unit : 16 * unit + 8;
+        turns = unit < r.R / (2 * E);
+        const int u = turns ? unit : unit - r.R / (2 * E);
+        off[0] = (turns ? 0 : r.R) + E * u;
+        off[1] = off[0] + (turns ? r.R : D - r.R) / 2;
+        pair[0] = r.interleaved ? E / 2 * u : E * u;
+        pair[1] = pair[0] + (r.interleaved ? r.R / 4 : E / 2);
+        if (!turns) pair[0] = pair[1] = 0;
     }
     // Cosines and sines at position pos, through the wave's part of LDS.
     __device__ inline void at(const RopeSpec& r, double turns_i, int lane, int pos, real (*cs)[64])
@@ -82,27 +108,27 @@ struct RopeLane {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            c[e] = cs[0][8 * (unit & 7) + e];
-            s[e] = cs[1][8 * (unit & 7) + e];
+        for (int e = 0; e < E; ++e) {
+            c[e] = cs[0][pair[e / (E / 2)] + e % (E / 2)];
+            s[e] = cs[1][pair[e / (E / 2)] + e % (E / 2)];
         }
     }
-    __device__ inline void turn(const RopeSpec& r, Row8<T>& a, Row8<T>& b) const
+    __device__ inline void turn(const RopeSpec& r, RopePiece<T>& a, RopePiece<T>& b) const
     {
         if (!turns) return;
-        float x[8], y[8];
+        float x[E], y[E];
         if (r.interleaved) {
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
+            for (int e = 0; e < E; e += 2) {
                 const real a0 = a.get(e), a1 = a.get(e + 1), b0 = b.get(e), b1 = b.get(e + 1);
                 x[e] = (float)(a0 * c[e / 2] - a1 * s[e / 2]);
                 x[e + 1] = (float)(a1 * c[e / 2] + a0 * s[e / 2]);
-                y[e] = (float)(b0 * c[4 + e / 2] - b1 * s[4 + e / 2]);
-                y[e + 1] = (float)(b1 * c[4 + e / 2] + b0 * s[4 + e / 2]);
+                y[e] = (float)(b0 * c[(E + e) / 2] - b1 * s[(E + e) / 2]);
+                y[e + 1] = (float)(b1 * c[(E + e) / 2] + b0 * s[(E + e) / 2]);
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < E; ++e) {
                 const real a0 = a.get(e), b0 = b.get(e);
                 x[e] = (float)(a0 * c[e] - b0 * s[e]);
                 y[e] = (float)(b0 * c[e] + a0 * s[e]);
@@ -135,39 +161,41 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeRowsArgs a)
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     L me;
     me.init(a.spec, lane);
-    const double turns_i = lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0;
     const int its0 = (a.heads[0] + L::HEADS - 1) / L::HEADS, its = its0 + (a.heads[1] + L::HEADS - 1) / L::HEADS;
+    double turns_i = 0.0;
     for (int i = 0; i < a.tokens; ++i) {
         const int t = (blockIdx.x * 4 + w) * a.tokens + i;
         if (t >= a.num_tokens) return;
         const int pos = a.positions[t];
-        bool first = true;
+        const T* const in[2] = {static_cast<const T*>(a.in[0]) + t * a.in_stride[0], static_cast<const T*>(a.in[1]) + t * a.in_stride[1]};
+        T* const out[2] = {static_cast<T*>(a.out[0]) + t * a.out_stride[0], static_cast<T*>(a.out[1]) + t * a.out_stride[1]};
+        const bool copy[2] = {a.in[0] != a.out[0], a.in[1] != a.out[1]};
         for (int it0 = blockIdx.y; it0 < its; it0 += BATCH * a.split) {
-            Row8<T> x[BATCH][2];
+            RopePiece<T> x[BATCH][2];
             bool here[BATCH];
-            long at[BATCH];
-            int which[BATCH];
+            T* dst[BATCH];
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
                 const int it = it0 + k * a.split;
-                which[k] = it >= its0;
-                const int h = (which[k] ? it - its0 : it) * L::HEADS + me.head;
-                at[k] = (long)h * D;
-                here[k] = it < its && h < a.heads[which[k]] && (me.turns || a.in[which[k]] != a.out[which[k]]);
+                const bool keys = it >= its0;
+                const int h = (keys ? it - its0 : it) * L::HEADS + me.head;
+                here[k] = it < its && h < (keys ? a.heads[1] : a.heads[0]) && (me.turns || (keys ? copy[1] : copy[0]));
                 if (!here[k]) continue;
-                const T* src = static_cast<const T*>(a.in[which[k]]) + t * a.in_stride[which[k]] + at[k];
-                x[k][0].load(src + me.off[0]);
-                x[k][1].load(src + me.off[1]);
+                const T* src = (keys ? in[1] : in[0]) + (long)h * D;
+                dst[k] = (keys ? out[1] : out[0]) + (long)h * D;
+                x[k][0].x = *reinterpret_cast<const u32x4_t*>(src + me.off[0]);
+                x[k][1].x = *reinterpret_cast<const u32x4_t*>(src + me.off[1]);
             }
-            if (first) me.at(a.spec, turns_i, lane, pos, cs[w]);
-            first = false;
+            if (it0 == (int)blockIdx.y) {
+                if (i == 0) turns_i = lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0;  // under the loads
+                me.at(a.spec, turns_i, lane, pos, cs[w]);
+            }
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
                 if (!here[k]) continue;
                 me.turn(a.spec, x[k][0], x[k][1]);
-                T* dst = static_cast<T*>(a.out[which[k]]) + t * a.out_stride[which[k]] + at[k];
-                x[k][0].store(dst + me.off[0]);
-                x[k][1].store(dst + me.off[1]);
+                *reinterpret_cast<u32x4_t*>(dst[k] + me.off[0]) = x[k][0].x;
+                *reinterpret_cast<u32x4_t*>(dst[k] + me.off[1]) = x[k][1].x;
             }
         }
     }
@@ -229,12 +257,14 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
     if (t >= io.num_tokens || !paged_rope_place(a, t, page, slot, pos)) return;
     L me;
     me.init(a.spec, lane);
-    const double turns_i = lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0;
     const int its_q = (a.H_q + L::HEADS - 1) / L::HEADS, its_k = (io.H_kv + L::HEADS - 1) / L::HEADS;
     const int its = its_q + 2 * its_k;
-    bool first = true;
+    const T* const q_row = static_cast<const T*>(a.q) + t * a.q_stride;
+    const T* const k_row = static_cast<const T*>(io.k_rows) + t * a.k_stride;
+    const T* const v_row = static_cast<const T*>(io.v_rows) + t * a.v_stride;
+    const int v0 = L::E * me.unit, v1 = D / 2 + v0;  // a value's pieces
     for (int it0 = blockIdx.y; it0 < its; it0 += BATCH * a.split) {
-        Row8<T> x[BATCH][2];
+        RopePiece<T> x[BATCH][2];
         int kind[BATCH], head[BATCH];  // 0 queries, 1 keys, 2 values, 3 nothing
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
@@ -244,26 +274,24 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
             const int h0 = (kind[k] == 0 ? it : kind[k] == 1 ? it - its_q : it - its_q - its_k) * L::HEADS;
             head[k] = h0 + me.head;
             if (kind[k] == 3 || head[k] >= (kind[k] == 0 ? a.H_q : io.H_kv)) continue;
-            const T* src = kind[k] == 0 ? static_cast<const T*>(a.q) + t * a.q_stride
-                         : kind[k] == 1 ? static_cast<const T*>(io.k_rows) + t * a.k_stride
-                                        : static_cast<const T*>(io.v_rows) + t * a.v_stride;
+            const T* src = kind[k] == 0 ? q_row : kind[k] == 1 ? k_row : v_row;
             src += (long)head[k] * D;
-            x[k][0].load(src + (kind[k] == 2 ? 16 * me.unit : me.off[0]));
-            x[k][1].load(src + (kind[k] == 2 ? 16 * me.unit + 8 : me.off[1]));
+            x[k][0].x = *reinterpret_cast<const u32x4_t*>(src + (kind[k] == 2 ? v0 : me.off[0]));
+            x[k][1].x = *reinterpret_cast<const u32x4_t*>(src + (kind[k] == 2 ? v1 : me.off[1]));
         }
-        if (first) me.at(a.spec, turns_i, lane, pos, cs[w]);
-        first = false;
+        if (it0 == (int)blockIdx.y)
+            me.at(a.spec, lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0, lane, pos, cs[w]);  // under the loads
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
             if (kind[k] == 3) continue;
             const bool here = head[k] < (kind[k] == 0 ? a.H_q : io.H_kv);
             if (kind[k] < 2 && here) me.turn(a.spec, x[k][0], x[k][1]);
-            const int o0 = kind[k] == 2 ? 16 * me.unit : me.off[0], o1 = kind[k] == 2 ? 16 * me.unit + 8 : me.off[1];
+            const int o0 = kind[k] == 2 ? v0 : me.off[0], o1 = kind[k] == 2 ? v1 : me.off[1];
             if (kind[k] == 0) {
                 if (here && (me.turns || a.q_out != a.q)) {
                     T* dst = static_cast<T*>(a.q_out) + t * a.q_out_stride + (long)head[k] * D;
-                    x[k][0].store(dst + o0);
-                    x[k][1].store(dst + o1);
+                    *reinterpret_cast<u32x4_t*>(dst + o0) = x[k][0].x;
+                    *reinterpret_cast<u32x4_t*>(dst + o1) = x[k][1].x;
                 }
                 continue;
             }
@@ -271,8 +299,8 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
             if constexpr (FORM == kPlainRows) {
                 if (here) {
                     T* dst = reinterpret_cast<T*>(pages) + ((((long)page << io.page_shift) + slot) * io.H_kv + head[k]) * D;
-                    x[k][0].store(dst + o0);
-                    x[k][1].store(dst + o1);
+                    *reinterpret_cast<u32x4_t*>(dst + o0) = x[k][0].x;
+                    *reinterpret_cast<u32x4_t*>(dst + o1) = x[k][1].x;
                 }
             } else {
                 // the heads' rows in order, eight consecutive elements to a lane
@@ -280,8 +308,8 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();
                 if (here) {
-                    x[k][0].store(lin + me.head * D + o0);
-                    x[k][1].store(lin + me.head * D + o1);
+                    *reinterpret_cast<u32x4_t*>(lin + me.head * D + o0) = x[k][0].x;
+                    *reinterpret_cast<u32x4_t*>(lin + me.head * D + o1) = x[k][1].x;
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 __builtin_amdgcn_wave_barrier();

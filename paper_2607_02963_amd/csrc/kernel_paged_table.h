@@ -7,15 +7,16 @@
 //
 // Two passes.  The first counts, a wave to a sequence's row of the table: the entries that
 // lack a page, or whose page goes back.  In the second a work-group takes a few sequences,
-// sums the counts of all sequences before them (1024 at a time, four to a lane: the sums
-// are a few KB, and cheaper than a pass of their own), and then each wave deals a
+// sums the counts of all sequences before them (2048 at a time, eight to a lane: the counts
+// are a few KB, and summing them cheaper than a pass of its own), and then each wave deals a
 // sequence's pages, each lane a token's position and row.  A batch of up to 64 sequences
 // is one work-group's, in one launch.
 //
-// What bounds it: the chain of memory round trips (lengths, entries, the free list, the
-// entries again).
+// What bounds it: the chain of memory round trips: lengths, entries, the sums, the free
+// list, the entries again.
 #pragma once
 
+#include "kernel_mfma.h"
 #include "paged_common.h"
 
 namespace pdec {
@@ -30,7 +31,7 @@ struct PagedTableArgs {
     int32_t* cu;           // reserve only, as the next two
     int32_t* positions;    // may be null
     int64_t* slots;        // may be null
-    int2* counts;          // [S] pages and tokens, of the first pass
+    int2* counts;          // [S, even] pages and tokens, of the first pass; releasing, from the last sequence
     int num_seqs, num_tokens, page_shift, num_pages, max_pages, max_len;
 };
 
@@ -70,68 +71,97 @@ __device__ inline TableSeq table_seq(const PagedTableArgs& a, int s)
 // end (release): which of its U the lane's must be dealt with.
 template <bool RESERVE, int U>
 struct TableLook {
-    int e[U], entry[U];
-    uint64_t b[U];
-    __device__ inline void look(const PagedTableArgs& a, const int32_t* row, const TableSeq& x, int at, int cols)
+    int at, cols, entry[U];
+    __device__ inline int place(int u) const  // the lane's u-th entry
     {
-        const int lane = paged_lane();
+        const int i = at + 64 * u + paged_lane();
+        return RESERVE ? i : cols - 1 - i;
+    }
+    __device__ inline void load(const int32_t* row, const TableSeq& x, int first, int columns)
+    {
+        at = first;
+        cols = columns;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            e[u] = RESERVE ? at + 64 * u + lane : cols - 1 - (at + 64 * u + lane);
-            const bool in = RESERVE ? e[u] < x.hi : e[u] >= 0 && (e[u] < x.lo || e[u] >= x.hi);
-            entry[u] = in ? row[e[u]] : RESERVE ? 0 : -1;
+            const int e = place(u);
+            entry[u] = row[RESERVE ? max(min(e, x.hi - 1), 0) : max(e, 0)];  // no branch: all under way at once
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) b[u] = __ballot(table_there(a, entry[u]) != RESERVE);
+        for (int u = 0; u < U; ++u) {
+            const int e = place(u);
+            const bool in = RESERVE ? e < x.hi : e >= 0 && (e < x.lo || e >= x.hi);
+            entry[u] = in ? entry[u] : RESERVE ? 0 : -1;
+        }
     }
-    __device__ inline int count() const
+    __device__ inline uint64_t found(const PagedTableArgs& a, int u) const { return __ballot(table_there(a, entry[u]) != RESERVE); }
+    __device__ inline int count(const PagedTableArgs& a) const
     {
         int n = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) n += __builtin_popcountll(b[u]);
-        return n;
+        for (int u = 0; u < U; ++u) n += table_there(a, entry[u]) != RESERVE ? 1 : 0;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) n += __shfl_xor(n, off);
+        return __builtin_amdgcn_readfirstlane(n);
+    }
+    // give(entry's place, entry, number among those found) for each entry found
+    template <typename F>
+    __device__ inline void each(const PagedTableArgs& a, F give) const
+    {
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t b = found(a, u);
+            if (b) give((b >> paged_lane() & 1) != 0, place(u), entry[u], n + __builtin_popcountll(b & ((1ull << paged_lane()) - 1)));
+            n += __builtin_popcountll(b);
+        }
+    }
+    // Deals the entries found pages from free_pages[from], [from - 1], .. (reserve), or puts
+    // theirs to free_pages[from], [from + 1], ..
+    __device__ inline void deal(const PagedTableArgs& a, int32_t* row, int from) const
+    {
+        each(a, [&](bool mine, int e, int page, int i) {
+            if (!mine) return;
+            if constexpr (RESERVE) row[e] = a.free_pages[from - i];
+            else {
+                // (a page that is released twice would pass the list's end)
+                if (from + i < a.num_pages) a.free_pages[from + i] = page;
+                row[e] = -1;
+            }
+        });
     }
 };
+
+// A row's looks, U entries to a lane at a time: one memory round trip for most rows.
+template <bool RESERVE> constexpr int kTableLook = RESERVE ? 4 : 16;
+template <bool RESERVE>
+__device__ inline int table_begin(const TableSeq& x) { return RESERVE ? x.lo : 0; }
+template <bool RESERVE>
+__device__ inline int table_end(const TableSeq& x, int cols) { return RESERVE ? x.hi : cols; }
 
 // The wave's row: how many entries lack a page (reserve), or go back (release).
 template <bool RESERVE>
 __device__ inline int table_count(const PagedTableArgs& a, int s, const TableSeq& x, int cols)
 {
-    constexpr int U = 4;
-    const int32_t* row = a.block_table + (long)s * a.max_pages;
+    constexpr int U = kTableLook<RESERVE>;
     int n = 0;
-    for (int at = RESERVE ? x.lo : 0; at < (RESERVE ? x.hi : cols); at += 64 * U) {
+    for (int at = table_begin<RESERVE>(x); at < table_end<RESERVE>(x, cols); at += 64 * U) {
         TableLook<RESERVE, U> k;
-        k.look(a, row, x, at, cols);
-        n += k.count();
+        k.load(a.block_table + (long)s * a.max_pages, x, at, cols);
+        n += k.count(a);
     }
     return n;
 }
 
-// Deals the wave's row its pages from free_pages[from], [from - 1], .. (reserve), or puts
-// them to free_pages[from], [from + 1], ..
 template <bool RESERVE>
 __device__ inline void table_deal(const PagedTableArgs& a, int s, const TableSeq& x, int cols, int from)
 {
-    constexpr int U = 4;
+    constexpr int U = kTableLook<RESERVE>;
     int32_t* row = a.block_table + (long)s * a.max_pages;
-    const uint64_t below = (1ull << paged_lane()) - 1;
-    for (int at = RESERVE ? x.lo : 0; at < (RESERVE ? x.hi : cols); at += 64 * U) {
+    for (int at = table_begin<RESERVE>(x); at < table_end<RESERVE>(x, cols); at += 64 * U) {
         TableLook<RESERVE, U> k;
-        k.look(a, row, x, at, cols);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = __builtin_popcountll(k.b[u] & below);
-            if (k.b[u] >> paged_lane() & 1) {
-                if constexpr (RESERVE) row[k.e[u]] = a.free_pages[from - i];
-                else {
-                    // (a page that is released twice would pass the list's end)
-                    if (from + i < a.num_pages) a.free_pages[from + i] = k.entry[u];
-                    row[k.e[u]] = -1;
-                }
-            }
-            from += (RESERVE ? -1 : 1) * __builtin_popcountll(k.b[u]);
-        }
+        k.load(row, x, at, cols);
+        k.deal(a, row, from);
+        from += (RESERVE ? -1 : 1) * k.count(a);
     }
 }
 
@@ -142,126 +172,244 @@ __global__ __launch_bounds__(256) void paged_table_count_kernel(PagedTableArgs a
     if (s >= a.num_seqs) return;
     const TableSeq x = table_seq<RESERVE>(a, s);
     const int n = table_count<RESERVE>(a, s, x, (a.max_len + (1 << a.page_shift) - 1) >> a.page_shift);
-    if (paged_lane() == 0) a.counts[s] = make_int2(n, x.n);
+    if (paged_lane() == 0) a.counts[RESERVE ? s : a.num_seqs - 1 - s] = make_int2(n, x.n);
 }
 
-// A work-group's sequences: all (ONE), or `WAVES` of them.  Releasing, the sequences are
-// numbered from the last, so that the sums are of those behind.
-template <bool RESERVE, bool ONE>
-struct TableShape {
-    static constexpr int THREADS = ONE ? 1024 : 256, WAVES = THREADS / 64, SEQS = ONE ? kTableOne : WAVES, CHUNK = 4 * THREADS;
+// Sums of pages and tokens, in 64 bits: a batch outside the contract may ask for anything.
+struct TableSum {
+    uint64_t p, t;
+    __device__ inline TableSum operator+(const TableSum& y) const { return TableSum{p + y.p, t + y.t}; }
 };
 
-template <bool RESERVE, bool ONE>
-__global__ __launch_bounds__((TableShape<RESERVE, ONE>::THREADS)) void paged_table_kernel(PagedTableArgs a)
+__device__ inline TableSum table_scan(TableSum x)  // inclusive, over the wave
 {
-    typedef TableShape<RESERVE, ONE> C;
-    __shared__ uint64_t wave_s[2][C::WAVES];
+    const int lane = paged_lane();
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const TableSum y = {__shfl_up(x.p, off), __shfl_up(x.t, off)};
+        if (lane >= off) x = x + y;
+    }
+    return x;
+}
+
+// The work-group's tokens: positions and rows of the pool.  token[i], i < count: the first
+// token of its sequence i; len[i] its keys before; end: behind its last; page_of(i, entry):
+// what the table holds.
+template <int THREADS, typename F>
+__device__ inline void table_tokens(const PagedTableArgs& a, int count, const int* token, const int* len, int first, int end, F page_of)
+{
+    constexpr int U = 4;
+    for (int t0 = first + (int)threadIdx.x; t0 < end; t0 += U * THREADS) {
+        int key[U], entry[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * THREADS;
+            int lo = 0, n = count - 1;  // the last sequence that begins at or before t
+            while (n > 0) {
+                const int half = (n + 1) / 2;
+                if (token[lo + half] <= t) lo += half, n -= half;
+                else n = half - 1;
+            }
+            key[u] = len[lo] + t - token[lo];
+            entry[u] = t < end ? page_of(lo, key[u] >> a.page_shift) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * THREADS;
+            if (t >= end) break;
+            if (a.positions) a.positions[t] = key[u];
+            if (a.slots) a.slots[t] = ((int64_t)entry[u] << a.page_shift) + (key[u] & ((1 << a.page_shift) - 1));
+        }
+    }
+}
+
+// Up to kTableOne sequences: one work-group, their sums a wave's scan.
+// Releasing, the sequences are numbered from the last, so that the sums are of those behind.
+// PER: sequences of a wave, up to four.
+constexpr int kTableWaves = 16;
+template <bool RESERVE, int PER>
+__global__ __launch_bounds__(64 * kTableWaves) void paged_table_one_kernel(PagedTableArgs a)
+{
+    constexpr int U = RESERVE ? 4 : 32 / PER;  // a lane's entries of a row at first: as many as the registers hold
+    __shared__ int2 counts_s[kTableOne];
+    __shared__ int token_s[kTableOne], len_s[kTableOne];
+    const int lane = paged_lane(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), S = a.num_seqs;
+    const int cols = (a.max_len + (1 << a.page_shift) - 1) >> a.page_shift;
+    const int top = min(max(a.free_in[0], 0), a.num_pages);
+    auto seq = [&](int i) { return RESERVE ? i : S - 1 - i; };
+    TableSeq x[PER];
+    TableLook<RESERVE, U> look[PER];  // the rows' first entries, all asked for at once
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = w + k * kTableWaves;
+        x[k] = i < S ? table_seq<RESERVE>(a, seq(i)) : TableSeq{0, 0, 0, 0};
+    }
+    // a reservation's first pages, in case
+    const int ahead = RESERVE && lane < top ? a.free_pages[top - 1 - lane] : 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = w + k * kTableWaves;
+        look[k].load(a.block_table + (long)seq(min(i, S - 1)) * a.max_pages, x[k], table_begin<RESERVE>(x[k]), i < S ? cols : 0);
+    }
+    int n[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = w + k * kTableWaves;
+        n[k] = look[k].count(a);
+        const int next = table_begin<RESERVE>(x[k]) + 64 * U;
+        if (i < S && next < table_end<RESERVE>(x[k], cols)) n[k] = table_count<RESERVE>(a, seq(i), x[k], cols);  // a longer row
+        if (lane == 0 && i < S) {
+            counts_s[i] = make_int2(n[k], x[k].n);
+            len_s[i] = x[k].len;
+        }
+    }
+    __syncthreads();
+    // every wave forms the sums
+    const int2 mine = lane < S ? counts_s[lane] : make_int2(0, 0);
+    const TableSum own = {(uint32_t)mine.x, (uint32_t)mine.y}, sum = table_scan(own);
+    const bool served = lane < S && (!RESERVE || (sum.p <= (uint64_t)top && sum.t <= (uint64_t)a.num_tokens));
+    const int count = __builtin_popcountll(__ballot(served));  // the first so many
+    const int pages = count > 0 ? __builtin_amdgcn_readlane((int)min(sum.p, (uint64_t)INT32_MAX), count - 1) : 0;
+    const int tokens = count > 0 ? __builtin_amdgcn_readlane((int)sum.t, count - 1) : 0;
+    const int p0 = (int)min(sum.p - own.p, (uint64_t)a.num_pages), t0 = (int)(sum.t - own.t);
+    if (w == 0) {
+        if (lane == 0) a.free_out[0] = RESERVE ? top - pages : (int)min((long)top + pages, (long)a.num_pages);
+        if constexpr (RESERVE) {
+            if (lane == 0) a.cu[0] = 0;
+            if (lane < S) a.cu[lane + 1] = lane < count ? t0 + mine.y : tokens;
+            if (lane < S) token_s[lane] = t0;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int i = w + k * kTableWaves;
+        if (i >= count || n[k] == 0) continue;
+        const int at = __builtin_amdgcn_readlane(p0, i);
+        int32_t* row = a.block_table + (long)seq(i) * a.max_pages;
+        if (table_begin<RESERVE>(x[k]) + 64 * U < table_end<RESERVE>(x[k], cols))
+            table_deal<RESERVE>(a, seq(i), x[k], cols, RESERVE ? top - 1 - at : min(top + at, a.num_pages));
+        else if (RESERVE && at + n[k] <= 64) {
+            // from the pages that were asked for ahead
+            look[k].each(a, [&](bool mine, int e, int, int j) {
+                const int page = __shfl(ahead, at + j);
+                if (mine) row[e] = page;
+            });
+        } else {
+            look[k].deal(a, row, RESERVE ? top - 1 - at : min(top + at, a.num_pages));
+        }
+    }
+    if constexpr (RESERVE) {
+        if (!a.positions && !a.slots) return;
+        __syncthreads();  // the entries are written
+        table_tokens<64 * kTableWaves>(a, count, token_s, len_s, 0, tokens,
+                                       [&](int i, int e) { return a.block_table[(long)i * a.max_pages + e]; });
+    }
+}
+
+// More sequences: four to a work-group, the counts of the first pass summed up to them.
+template <bool RESERVE>
+__global__ __launch_bounds__(256) void paged_table_kernel(PagedTableArgs a)
+{
+    constexpr int WAVES = 4, PER = 8, CHUNK = 64 * WAVES * PER;
+    __shared__ TableSum wave_s[WAVES];
     __shared__ unsigned long long most_s[2];  // pages and tokens of the sequences that are served
-    __shared__ int2 counts_s[ONE ? C::SEQS : 1];
-    __shared__ int from_s[C::SEQS], token_s[C::SEQS];  // of each of the group's sequences; from -1: not served
+    __shared__ int from_s[WAVES], need_s[WAVES], token_s[WAVES], len_s[WAVES];  // from -1: not served
+    constexpr int LOOK = 64 * kTableLook<RESERVE>;
+    __shared__ int page_s[RESERVE ? WAVES : 1][RESERVE ? LOOK : 1], long_s[WAVES];  // a row's pages, unless they are more
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int cols = (a.max_len + (1 << a.page_shift) - 1) >> a.page_shift;
     const int top = min(max(a.free_in[0], 0), a.num_pages);
-    const int s0 = blockIdx.x * C::SEQS, s1 = min(s0 + C::SEQS, a.num_seqs);  // the group's, by their numbers
+    const int s0 = blockIdx.x * WAVES, s1 = min(s0 + WAVES, a.num_seqs);  // the group's, by their numbers
     auto seq = [&](int i) { return RESERVE ? i : a.num_seqs - 1 - i; };
-    TableSeq own[C::SEQS / C::WAVES];  // the wave's: s0 + w, s0 + w + WAVES, ..
-#pragma unroll
-    for (int k = 0; k < C::SEQS / C::WAVES; ++k) {
-        const int i = s0 + w + k * C::WAVES;
-        if (i < s1) own[k] = table_seq<RESERVE>(a, seq(i));
-    }
-    if constexpr (ONE) {
-#pragma unroll
-        for (int k = 0; k < C::SEQS / C::WAVES; ++k) {
-            const int i = w + k * C::WAVES;
-            if (i >= s1) break;
-            const int n = table_count<RESERVE>(a, seq(i), own[k], cols);
-            if (lane == 0) counts_s[i] = make_int2(n, own[k].n);
-        }
+    TableSeq own = {0, 0, 0, 0};
+    if (s0 + w < s1) own = table_seq<RESERVE>(a, seq(s0 + w));
+    int32_t* const row = a.block_table + (long)seq(min(s0 + w, s1 - 1)) * a.max_pages;
+    TableLook<RESERVE, kTableLook<RESERVE>> look;  // the row's first entries, under the sums
+    look.load(row, own, table_begin<RESERVE>(own), cols);
+    const bool is_long = table_begin<RESERVE>(own) + LOOK < table_end<RESERVE>(own, cols);
+    if (lane == 0) {
+        len_s[w] = own.len;
+        long_s[w] = is_long;
     }
     if (tid < 2) most_s[tid] = 0;
-    __syncthreads();
 
-    uint64_t sum[2] = {0, 0};  // of the chunks before
-    for (int c0 = 0; c0 < s1; c0 += C::CHUNK) {
-        uint64_t x[2][4];  // inclusive sums over the lane's four
+    TableSum sum = {0, 0};  // of the chunks before
+    for (int c0 = 0; c0 < s1; c0 += CHUNK) {
+        int4 n[PER / 2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = c0 + 4 * tid + j;
-            int2 n = make_int2(0, 0);
-            if (i < s1) n = ONE ? counts_s[ONE ? i : 0] : a.counts[seq(i)];
-            x[0][j] = (uint32_t)n.x + (j ? x[0][j - 1] : 0);
-            x[1][j] = (uint32_t)n.y + (j ? x[1][j - 1] : 0);
+        for (int j = 0; j < PER / 2; ++j) {
+            const int i = c0 + PER * tid + 2 * j;
+            n[j] = i < s1 ? *reinterpret_cast<const int4*>(a.counts + i) : make_int4(0, 0, 0, 0);
+            if (i + 1 >= s1) n[j].z = n[j].w = 0;
         }
-        uint64_t total[2];
+        TableSum x[PER];  // inclusive sums over the lane's
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            uint64_t y = x[k][3];
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const uint64_t z = __shfl_up(y, off);
-                if (lane >= off) y += z;
-            }
-            if (lane == 63) wave_s[k][w] = y;
-            total[k] = y - x[k][3];  // of the wave's lanes before
+        for (int j = 0; j < PER; ++j) {
+            x[j] = j & 1 ? TableSum{(uint32_t)n[j / 2].z, (uint32_t)n[j / 2].w} : TableSum{(uint32_t)n[j / 2].x, (uint32_t)n[j / 2].y};
+            if (j) x[j] = x[j] + x[j - 1];
         }
+        const TableSum y = table_scan(x[PER - 1]);
+        if (lane == 63) wave_s[w] = y;
         __syncthreads();
-        uint64_t before[2], all[2] = {0, 0};
+        TableSum before = {sum.p + y.p - x[PER - 1].p, sum.t + y.t - x[PER - 1].t};
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            before[k] = sum[k] + total[k];
-#pragma unroll
-            for (int i = 0; i < C::WAVES; ++i) {
-                if (i < w) before[k] += wave_s[k][i];
-                all[k] += wave_s[k][i];
-            }
-            sum[k] += all[k];
+        for (int i = 0; i < WAVES; ++i) {
+            if (i < w) before = before + wave_s[i];
+            sum = sum + wave_s[i];
         }
-        uint64_t p = 0, t = 0;  // of the last that is served
+        TableSum last = {0, 0};  // of the last that is served
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = c0 + 4 * tid + j;
-            const uint64_t pj = before[0] + x[0][j], tj = before[1] + x[1][j];
-            const bool served = i < s1 && (!RESERVE || (pj <= (uint64_t)top && tj <= (uint64_t)a.num_tokens));
-            if (served) p = pj, t = tj;
+        for (int j = 0; j < PER; ++j) {
+            const int i = c0 + PER * tid + j;
+            const TableSum in = before + x[j], ex = j ? before + x[j - 1] : before;
+            const bool served = i < s1 && (!RESERVE || (in.p <= (uint64_t)top && in.t <= (uint64_t)a.num_tokens));
+            if (served) last = in;
             if (i >= s0 && i < s1) {
-                const uint64_t p0 = before[0] + (j ? x[0][j - 1] : 0), t0 = before[1] + (j ? x[1][j - 1] : 0);
-                from_s[i - s0] = !served ? -1 : RESERVE ? top - (int)p0 : (int)min((uint64_t)top + p0, (uint64_t)a.num_pages);
-                token_s[i - s0] = (int)t0;
+                from_s[i - s0] = !served ? -1 : RESERVE ? top - (int)ex.p : (int)min((uint64_t)top + ex.p, (uint64_t)a.num_pages);
+                need_s[i - s0] = (int)(in.p - ex.p);
+                token_s[i - s0] = (int)ex.t;
             }
         }
-        if (p > 0) atomicMax(&most_s[0], (unsigned long long)p);
-        if (t > 0) atomicMax(&most_s[1], (unsigned long long)t);
+        if (last.p > 0) atomicMax(&most_s[0], (unsigned long long)last.p);
+        if (last.t > 0) atomicMax(&most_s[1], (unsigned long long)last.t);
         __syncthreads();
     }
 
     if (tid == 0 && s1 == a.num_seqs)
-        a.free_out[0] = RESERVE ? top - (int)most_s[0] : (int)min((uint64_t)top + sum[0], (uint64_t)a.num_pages);
+        a.free_out[0] = RESERVE ? top - (int)most_s[0] : (int)min((uint64_t)top + sum.p, (uint64_t)a.num_pages);
+    if (s0 + w < s1) {
+        const int from = __builtin_amdgcn_readfirstlane(from_s[w]);
+        if constexpr (RESERVE) {
 #pragma unroll
-    for (int k = 0; k < C::SEQS / C::WAVES; ++k) {
-        const int i = s0 + w + k * C::WAVES;
-        if (i >= s1) break;
-        const int from = __builtin_amdgcn_readfirstlane(from_s[i - s0]);
-        if (from >= 0) table_deal<RESERVE>(a, seq(i), own[k], cols, RESERVE ? from - 1 : from);
+            for (int u = 0; u < kTableLook<RESERVE>; ++u)
+                if (look.place(u) < own.hi) page_s[w][64 * u + lane] = look.entry[u];
+        }
+        if (from >= 0 && need_s[w] > 0) {
+            if (is_long) table_deal<RESERVE>(a, seq(s0 + w), own, cols, RESERVE ? from - 1 : from);
+            else if constexpr (RESERVE)
+                look.each(a, [&](bool mine, int e, int, int i) {
+                    if (mine) page_s[w][e - own.lo] = row[e] = a.free_pages[from - 1 - i];
+                });
+            else look.deal(a, row, from);
+        }
         if constexpr (RESERVE)
-            if (lane == 0) a.cu[i + 1] = from >= 0 ? token_s[i - s0] + own[k].n : (int)most_s[1];
+            if (lane == 0) a.cu[s0 + w + 1] = from >= 0 ? token_s[w] + own.n : (int)most_s[1];
     }
     if constexpr (RESERVE) {
         if (tid == 0 && s0 == 0) a.cu[0] = 0;
         if (!a.positions && !a.slots) return;
-        __syncthreads();  // the entries are written
-        for (int i = s0; i < s1; ++i) {
-            if (from_s[i - s0] < 0) break;  // nor are the later ones
-            const TableSeq x = table_seq<RESERVE>(a, i);
-            const int32_t* row = a.block_table + (long)i * a.max_pages;
-            const int t0 = token_s[i - s0];
-            for (int j = tid; j < x.n; j += C::THREADS) {
-                const int key = x.len + j;
-                if (a.positions) a.positions[t0 + j] = key;
-                if (a.slots) a.slots[t0 + j] = ((int64_t)row[key >> a.page_shift] << a.page_shift) + (key & ((1 << a.page_shift) - 1));
-            }
-        }
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) any |= long_s[i] != 0;
+        if (any) __syncthreads();  // the entries are written
+        else lds_barrier();
+        int count = 0;
+        while (count < s1 - s0 && from_s[count] >= 0) ++count;  // none behind one that is not served
+        if (count == 0) return;
+        const int first = token_s[0], end = count < s1 - s0 ? (int)most_s[1] : (int)sum.t;
+        table_tokens<256>(a, count, token_s, len_s, first, end, [&](int i, int e) {
+            return any ? a.block_table[(long)(s0 + i) * a.max_pages + e] : page_s[i][e - (len_s[i] >> a.page_shift)];
+        });
     }
 }
 

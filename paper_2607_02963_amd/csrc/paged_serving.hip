@@ -37,19 +37,20 @@ PagedTableArgs table_args(const pdec_table_dims* d)
     return a;
 }
 
-size_t table_workspace(const pdec_table_dims* d) { return std::max<size_t>((size_t)d->num_seqs * sizeof(int2), 16); }
+size_t table_workspace(const pdec_table_dims* d) { return ((size_t)d->num_seqs + 1) / 2 * 2 * sizeof(int2); }
 
 template <bool RESERVE>
 int launch_table(const PagedTableArgs& a, hipStream_t s)
 {
     if (a.num_seqs <= kTableOne) {
-        hipLaunchKernelGGL((paged_table_kernel<RESERVE, true>), dim3(1), dim3(TableShape<RESERVE, true>::THREADS), 0, s, a);
+        if (a.num_seqs <= 2 * kTableWaves) hipLaunchKernelGGL((paged_table_one_kernel<RESERVE, 2>), dim3(1), dim3(64 * kTableWaves), 0, s, a);
+        else hipLaunchKernelGGL((paged_table_one_kernel<RESERVE, 4>), dim3(1), dim3(64 * kTableWaves), 0, s, a);
         return launched();
     }
     const dim3 grid((unsigned)((a.num_seqs + 3) / 4));
     hipLaunchKernelGGL((paged_table_count_kernel<RESERVE>), grid, dim3(256), 0, s, a);
     if (launched() != PDEC_OK) return PDEC_ERR_HIP;
-    hipLaunchKernelGGL((paged_table_kernel<RESERVE, false>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_table_kernel<RESERVE>), grid, dim3(256), 0, s, a);
     return launched();
 }
 
@@ -178,7 +179,7 @@ int pdec_rope(const pdec_rope_spec* spec, int64_t num_tokens, int32_t num_q_head
         return PDEC_ERR_INVALID_ARG;
     a.positions = positions;
     a.num_tokens = (int)num_tokens;
-    const int per = 1024 / D;  // heads of a wave at a time
+    const int per = 64 * 32 / (D * (dtype == PDEC_DTYPE_F32 ? 4 : 2));  // heads of a wave at a time
     a.split = rope_split(num_tokens, (num_q_heads + per - 1) / per + (num_k_heads + per - 1) / per);
     a.tokens = 1;
     const dim3 grid((unsigned)((num_tokens + 4 * a.tokens - 1) / (4 * a.tokens)), (unsigned)a.split), block(256);
@@ -233,7 +234,7 @@ int pdec_paged_rope_kv_append(const pdec_paged_dims* d, const pdec_rope_spec* sp
     a.k_stride = k_stride;
     a.v_stride = v_stride;
     a.H_q = d->num_q_heads;
-    const int per = 1024 / d->head_dim;
+    const int per = 64 * 32 / (d->head_dim * (d->dtype == PDEC_DTYPE_F32 ? 4 : 2));
     a.split = rope_split(d->num_tokens, (a.H_q + per - 1) / per + 2 * ((d->num_kv_heads + per - 1) / per));
     const dim3 grid((unsigned)std::max((d->num_tokens + 3) / 4, (d->num_seqs + 63) / 64), (unsigned)a.split);
     hipStream_t s = static_cast<hipStream_t>(stream);
