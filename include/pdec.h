@@ -694,7 +694,7 @@ int pdec_merge_states(int64_t num_rows, int32_t head_dim, int32_t dtype, const v
  * [0, count) of an array.
  */
 typedef struct pdec_table_dims {
-    int32_t num_seqs;   /* S, 1..2^27                                                     */
+    int32_t num_seqs;   /* S, 1..2^20                                                     */
     int32_t num_tokens; /* reserve: tokens that the batch has room for, 1..2^27           */
     int32_t page_size;  /* tokens per page: a power of two, 16..1024                      */
     int32_t num_pages;  /* pages of the pool, and entries of free_pages, >= 1             */

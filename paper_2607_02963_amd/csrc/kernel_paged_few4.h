@@ -114,19 +114,26 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
         const int head = part.head;
         const uint64_t kbase = sgpr_base(a.k_pages), vbase = sgpr_base(a.v_pages);
 
-        // the wave's block b: its first key, and its quarters' pages
+        // The wave's block b: its first key; and its quarters' rows of the pool, looked up 64 quarters
+        // (BIG: blocks) at a time, a lane to each, and read back from the lanes: scalar loads in the
+        // loop would be waited for with every read of the LDS.  An absent page is read as page 0, and
+        // its keys masked.
         auto first = [&](int b) __attribute__((always_inline)) { return t0 + KB * (w + NW * b); };
-        struct Pages { int q[BIG ? 1 : 4]; };
-        auto pages = [&](int b) __attribute__((always_inline)) {
-            Pages x;
-#pragma unroll
-            for (int q = 0; q < (BIG ? 1 : 4); ++q) x.q[q] = paged_entry(table, min((first(b) + 16 * q) >> a.page_shift, a.max_pages - 1));
-            return x;
+        constexpr int Q = BIG ? 1 : 4, TURN = 64 / Q;  // look-ups of a block; blocks of a look-up
+        uint32_t row_lo = 0, row_hi = 0;
+        uint64_t there = 0, last_there = 0;  // of the turn at hand, and of the one before
+        auto look_up = [&](int b0) __attribute__((always_inline)) {
+            const int t = first(min(b0 + lane / Q, mine - 1)) + 16 * (lane % Q);
+            const int page = table[min(t >> a.page_shift, a.max_pages - 1)];
+            const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
+            const uint64_t row = (((uint64_t)(uint32_t)(ok ? page : 0) * a.H_kv + head) << a.page_shift) + (uint32_t)(t & ((1 << a.page_shift) - 1));
+            last_there = there;
+            row_lo = (uint32_t)row;
+            row_hi = (uint32_t)(row >> 32);
+            there = __ballot(ok);
         };
-        auto there = [&](int page) __attribute__((always_inline)) { return (uint32_t)page < (uint32_t)a.num_pages; };
-        // blocks past the last are pieces of one lane, so that every wait counts the same
-        // (ring.h); an absent page is read as page 0, and its keys masked
-        auto issue = [&](int b, const Pages& x) __attribute__((always_inline)) {
+        // blocks past the last are pieces of one lane, so that every wait counts the same (ring.h)
+        auto issue = [&](int b) __attribute__((always_inline)) {
             const uint64_t real = b < mine ? ~0ull : 1ull;
             const uint32_t dst = ring + (b % NS) * SLOT;
             uint32_t ko = koff;
@@ -137,9 +144,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                 koffs[i] = ko ^ (16 * few4_kswz<D>(KPI * i));
                 voffs[i] = voff;
             }
-            auto row_of = [&](int q) {  // of the pool
-                const int page = there(x.q[BIG ? 0 : q]) && b < mine ? x.q[BIG ? 0 : q] : 0;
-                return (((uint64_t)(uint32_t)page * a.H_kv + head) << a.page_shift) + (uint32_t)((first(b) + 16 * q) & ((1 << a.page_shift) - 1));
+            const int at = min(b, mine - 1) % TURN * Q;
+            auto row_of = [&](int q) {
+                return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)row_hi, at + q) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)row_lo, at + q);
             };
             if constexpr (BIG) {
                 const uint64_t row = row_of(0);
@@ -174,11 +181,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
         // keys that every row sees (rows past the last are masked or not, their results are not stored)
         const int least = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, row0 / a.G));
         const int most = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, (row0 + nrows - 1) / a.G));
+        if (mine > 0) {
+            look_up(0);
 #pragma unroll
-        for (int b = 0; b < NS; ++b)
-            if (mine > 0) issue(b, pages(min(b, mine - 1)));
-        Pages ahead = pages(min(NS, max(mine - 1, 0)));
-        Pages now = pages(0);
+            for (int b = 0; b < NS; ++b) issue(b);
+        }
 
         f32x4_t o[NT][DT];
         float m_ref[NT], lsum[NT];
@@ -196,12 +203,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
             wave_wait_vmcnt<(NS - 1) * PB>();  // block b has landed
             const uint32_t slot = ring + (b % NS) * SLOT, scs = sc_ring + (b % NS) * SC;
             const int t = first(b);
-            const bool have[4] = {there(now.q[0]), there(now.q[BIG ? 0 : 1]), there(now.q[BIG ? 0 : 2]), there(now.q[BIG ? 0 : 3])};
-            if ((have[0] | have[1] | have[2] | have[3]) && t < most) {
-                const bool all = have[0] & have[1] & have[2] & have[3];
-                const bool full = t + KB <= least && all;
-                const bool mine_there = BIG ? have[0] : lg & 2 ? (lg & 1 ? have[3] : have[2]) : (lg & 1 ? have[1] : have[0]);
-                // the values' scales of key t + lane, spread by blocks of d as bfloat16 exponents
+            // the look-up may be a turn ahead of the block at hand
+            const bool behind = b / TURN < (min(b + NS - 1, mine - 1)) / TURN;
+            const uint32_t have = (uint32_t)((behind ? last_there : there) >> (b % TURN * Q)) & ((1u << Q) - 1);  // its quarters'
+            if (have && t < most) {
+                const bool full = t + KB <= least && have == (1u << Q) - 1;
+                const bool mine_there = BIG || (have >> lg & 1);
+                // the values' scales of key t + lane, spread by blocks of d: k where bfloat16 has its exponent
                 bool odd;  // one of them is NaN
                 {
                     typedef __attribute__((address_space(3))) const uint16_t lds_u16c_t;
@@ -212,9 +220,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                     else x = *(lds_u16c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
                     odd = __any((((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u) != 0);
 #pragma unroll
-                    for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)((x >> (8 * i) & 255u) << 7);
+                    for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)(((x >> (8 * i) & 255u) << 7) - (127 << 7));
                 }
-                // one tile, or all: rows past the last see nothing, or their results are not stored
+                // the tiles that have rows; a row past the last sees nothing, or its result is not stored
                 auto block = [&](auto count) __attribute__((always_inline)) {
                     constexpr int N = count;
                     i32x2_t vraw[DT];
@@ -302,16 +310,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         }
                     };
                     if (full && !odd) {
-                        // P times 2^k: k added to its exponent, in the upper half of 32 bits or less than 0.
-                        // A product below 2^-126 is 0 (and a P of 0 may become 2^-127: nothing beside its
-                        // row's largest, which is 2^-8 at least), one beyond the largest number NaN
+                        // P times 2^k: k added to its exponent.  A product below 2^-126 is 0 (and a P of 0
+                        // may become 2^-127 times the scale: nothing beside its row's largest, which is
+                        // 2^-8 at least), one beyond the largest number NaN
                         typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
                         i16x2_t pe[N][8];
 #pragma unroll
                         for (int nt = 0; nt < N; ++nt)
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                pe[nt][j] = __builtin_bit_cast(i16x2_t, pack_bf16x2(p[nt][2 * j], p[nt][2 * j + 1])) - (int16_t)(127 << 7);
+                                pe[nt][j] = __builtin_bit_cast(i16x2_t, pack_bf16x2(p[nt][2 * j], p[nt][2 * j + 1]));
 #pragma unroll
                         for (int blk = 0; blk < SPK; ++blk)
 #pragma unroll
@@ -358,13 +366,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         }
                     }
                 };
-                if (NT > 1 && tiles > 1) block(std::integral_constant<int, NT>{});
+                if (NT > 2 && tiles > 2) block(std::integral_constant<int, NT>{});
+                else if (NT > 1 && tiles > 1) block(std::integral_constant<int, NT < 2 ? NT : 2>{});
                 else block(std::integral_constant<int, 1>{});
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
-            issue(b + NS, ahead);
-            ahead = pages(min(b + NS + 1, mine - 1));
-            now = pages(min(b + 1, mine - 1));
+            if ((b + NS) % TURN == 0 && b + NS < mine) look_up(b + NS);
+            issue(b + NS);
         }
 
         // ---- the waves' states joined, tile by tile; lane: row l % 16 of tile nt, d = 16 dt + 4 (l / 16) + i ----

@@ -101,8 +101,6 @@ struct RopeLane {
         double t = pos * turns_i, sn, cn;
         t -= rint(t);
         sincospi(2.0 * t, &sn, &cn);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the token before has been read
-        __builtin_amdgcn_wave_barrier();
         cs[0][lane] = (real)(cn * r.magnitude);
         cs[1][lane] = (real)((r.back ? -sn : sn) * r.magnitude);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -148,10 +146,10 @@ struct RopeRowsArgs {
     int heads[2];
     int num_tokens;
     int split;            // waves that share a token's heads
-    int tokens;           // of a wave
+    int wide;             // work-groups of the grid in x
 };
 
-// grid (tokens / (4 a.tokens), split).  An in-place call leaves what does not turn.
+// grid (a.wide, split, z), four tokens to a work-group.  An in-place call leaves what does not turn.
 template <int D, typename T>
 __global__ __launch_bounds__(256) void rope_rows_kernel(RopeRowsArgs a)
 {
@@ -162,41 +160,36 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeRowsArgs a)
     L me;
     me.init(a.spec, lane);
     const int its0 = (a.heads[0] + L::HEADS - 1) / L::HEADS, its = its0 + (a.heads[1] + L::HEADS - 1) / L::HEADS;
-    double turns_i = 0.0;
-    for (int i = 0; i < a.tokens; ++i) {
-        const int t = (blockIdx.x * 4 + w) * a.tokens + i;
-        if (t >= a.num_tokens) return;
-        const int pos = a.positions[t];
-        const T* const in[2] = {static_cast<const T*>(a.in[0]) + t * a.in_stride[0], static_cast<const T*>(a.in[1]) + t * a.in_stride[1]};
-        T* const out[2] = {static_cast<T*>(a.out[0]) + t * a.out_stride[0], static_cast<T*>(a.out[1]) + t * a.out_stride[1]};
-        const bool copy[2] = {a.in[0] != a.out[0], a.in[1] != a.out[1]};
-        for (int it0 = blockIdx.y; it0 < its; it0 += BATCH * a.split) {
-            RopePiece<T> x[BATCH][2];
-            bool here[BATCH];
-            T* dst[BATCH];
+    const int t = (blockIdx.z * a.wide + blockIdx.x) * 4 + w;
+    if (t >= a.num_tokens) return;
+    const int pos = a.positions[t];
+    const T* const in[2] = {static_cast<const T*>(a.in[0]) + t * a.in_stride[0], static_cast<const T*>(a.in[1]) + t * a.in_stride[1]};
+    T* const out[2] = {static_cast<T*>(a.out[0]) + t * a.out_stride[0], static_cast<T*>(a.out[1]) + t * a.out_stride[1]};
+    const bool copy[2] = {a.in[0] != a.out[0], a.in[1] != a.out[1]};
+    for (int it0 = blockIdx.y; it0 < its; it0 += BATCH * a.split) {
+        RopePiece<T> x[BATCH][2];
+        bool here[BATCH];
+        T* dst[BATCH];
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                const int it = it0 + k * a.split;
-                const bool keys = it >= its0;
-                const int h = (keys ? it - its0 : it) * L::HEADS + me.head;
-                here[k] = it < its && h < (keys ? a.heads[1] : a.heads[0]) && (me.turns || (keys ? copy[1] : copy[0]));
-                if (!here[k]) continue;
-                const T* src = (keys ? in[1] : in[0]) + (long)h * D;
-                dst[k] = (keys ? out[1] : out[0]) + (long)h * D;
-                x[k][0].x = *reinterpret_cast<const u32x4_t*>(src + me.off[0]);
-                x[k][1].x = *reinterpret_cast<const u32x4_t*>(src + me.off[1]);
-            }
-            if (it0 == (int)blockIdx.y) {
-                if (i == 0) turns_i = lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0;  // under the loads
-                me.at(a.spec, turns_i, lane, pos, cs[w]);
-            }
+        for (int k = 0; k < BATCH; ++k) {
+            const int it = it0 + k * a.split;
+            const bool keys = it >= its0;
+            const int h = (keys ? it - its0 : it) * L::HEADS + me.head;
+            here[k] = it < its && h < (keys ? a.heads[1] : a.heads[0]) && (me.turns || (keys ? copy[1] : copy[0]));
+            if (!here[k]) continue;
+            const T* src = (keys ? in[1] : in[0]) + (long)h * D;
+            dst[k] = (keys ? out[1] : out[0]) + (long)h * D;
+            x[k][0].x = *reinterpret_cast<const u32x4_t*>(src + me.off[0]);
+            x[k][1].x = *reinterpret_cast<const u32x4_t*>(src + me.off[1]);
+        }
+        if (it0 == (int)blockIdx.y)
+            me.at(a.spec, lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0, lane, pos, cs[w]);  // under the loads
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                if (!here[k]) continue;
-                me.turn(a.spec, x[k][0], x[k][1]);
-                *reinterpret_cast<u32x4_t*>(dst[k] + me.off[0]) = x[k][0].x;
-                *reinterpret_cast<u32x4_t*>(dst[k] + me.off[1]) = x[k][1].x;
-            }
+        for (int k = 0; k < BATCH; ++k) {
+            if (!here[k]) continue;
+            me.turn(a.spec, x[k][0], x[k][1]);
+            *reinterpret_cast<u32x4_t*>(dst[k] + me.off[0]) = x[k][0].x;
+            *reinterpret_cast<u32x4_t*>(dst[k] + me.off[1]) = x[k][1].x;
         }
     }
 }
@@ -209,7 +202,7 @@ struct PagedRopeArgs {
     const int32_t* pos_base;  // [S] or null
     long q_stride, q_out_stride, k_stride, v_stride;
     int H_q;
-    int split;
+    int split, wide;      // as for rope_rows_kernel
 };
 
 // The place of row r (uniform over the wave): page and row in it, page -1 for none; and its
@@ -233,7 +226,7 @@ __device__ inline bool paged_rope_place(const PagedRopeArgs& a, int r, int& page
 }
 
 // A wave takes a token, or every split-th of the steps over its heads: queries, then keys,
-// then values.  grid (max(tokens / 4, sequences / 64), split).  A key row is rounded to the
+// then values.  grid (a.wide, split, z), at least tokens / 4 and sequences / 64 work-groups.  A key row is rounded to the
 // rows' type before it is quantised: the cache holds what rope and then the append leave.
 template <int D, typename T, PagedForm FORM>
 __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
@@ -244,15 +237,16 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
     __shared__ __attribute__((aligned(16))) T rows_s[FORM == kPlainRows ? 1 : 4][FORM == kPlainRows ? 16 : L::HEADS * D];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const PagedIoArgs& io = a.io;
+    const int wg = blockIdx.z * a.wide + blockIdx.x;
     // the counts after the append, 64 sequences to a work-group
-    if (blockIdx.y == 0 && w == 0) {
-        const int s = 64 * blockIdx.x + lane;
+    if (blockIdx.y == 0 && w == 0 && wg <= (io.num_seqs - 1) / 64) {
+        const int s = 64 * wg + lane;
         if (s < io.num_seqs) {
             const int n = io.lens[s], m = min(max(io.cu[s + 1], 0), io.num_tokens) - min(max(io.cu[s], 0), io.num_tokens);
             io.lens_out[s] = n >= 0 && m > 0 && n <= io.max_len - m ? n + m : n;
         }
     }
-    const int t = blockIdx.x * 4 + w;
+    const int t = wg * 4 + w;
     int page, slot, pos;
     if (t >= io.num_tokens || !paged_rope_place(a, t, page, slot, pos)) return;
     L me;

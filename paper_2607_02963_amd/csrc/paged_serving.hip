@@ -12,13 +12,16 @@ namespace {
 
 using namespace pdec;
 
+// Sequences of a table call: its work-groups sum the counts of all before theirs.
+constexpr int kMostTableSeqs = 1 << 20;
+
 int check_table_dims(const pdec_table_dims* d)
 {
     if (!d) return PDEC_ERR_INVALID_ARG;
     if (d->num_seqs < 1 || d->num_tokens < 1 || d->page_size < 1 || d->num_pages < 1 || d->max_pages < 1 || d->max_len < 0)
         return PDEC_ERR_INVALID_ARG;
     if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0) return PDEC_ERR_UNSUPPORTED;
-    if (d->num_tokens > kMostRows || d->num_seqs > kMostRows) return PDEC_ERR_UNSUPPORTED;
+    if (d->num_tokens > kMostRows || d->num_seqs > kMostTableSeqs) return PDEC_ERR_UNSUPPORTED;
     const int64_t most = (int64_t)d->max_pages * d->page_size;
     if (most > ((int64_t)1 << 30)) return PDEC_ERR_UNSUPPORTED;
     if (d->max_len > most) return PDEC_ERR_INVALID_ARG;
@@ -101,6 +104,14 @@ bool row_stride(int64_t stride, int64_t elems, int dtype)
 // Waves that share a token's heads: as many as fill the card where tokens are few.
 int rope_split(int64_t tokens, int steps) { return (int)std::max<int64_t>(std::min<int64_t>(steps, 2048 / tokens), 1); }
 
+// At least `groups` work-groups, in x and z: the threads in x stay within 32 bits.
+constexpr int kRopeWide = 1 << 20;
+dim3 rope_grid(int groups, int split)
+{
+    const int wide = std::min(groups, kRopeWide);
+    return dim3((unsigned)wide, (unsigned)split, (unsigned)((groups + wide - 1) / wide));
+}
+
 }  // namespace
 
 extern "C" {
@@ -181,8 +192,8 @@ int pdec_rope(const pdec_rope_spec* spec, int64_t num_tokens, int32_t num_q_head
     a.num_tokens = (int)num_tokens;
     const int per = 64 * 32 / (D * (dtype == PDEC_DTYPE_F32 ? 4 : 2));  // heads of a wave at a time
     a.split = rope_split(num_tokens, (num_q_heads + per - 1) / per + (num_k_heads + per - 1) / per);
-    a.tokens = 1;
-    const dim3 grid((unsigned)((num_tokens + 4 * a.tokens - 1) / (4 * a.tokens)), (unsigned)a.split), block(256);
+    const dim3 grid = rope_grid(((int)num_tokens + 3) / 4, a.split), block(256);
+    a.wide = (int)grid.x;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool f32 = dtype == PDEC_DTYPE_F32;
     if (D == 128) {
@@ -236,7 +247,8 @@ int pdec_paged_rope_kv_append(const pdec_paged_dims* d, const pdec_rope_spec* sp
     a.H_q = d->num_q_heads;
     const int per = 64 * 32 / (d->head_dim * (d->dtype == PDEC_DTYPE_F32 ? 4 : 2));
     a.split = rope_split(d->num_tokens, (a.H_q + per - 1) / per + 2 * ((d->num_kv_heads + per - 1) / per));
-    const dim3 grid((unsigned)std::max((d->num_tokens + 3) / 4, (d->num_seqs + 63) / 64), (unsigned)a.split);
+    const dim3 grid = rope_grid(std::max((d->num_tokens + 3) / 4, (d->num_seqs + 63) / 64), a.split);
+    a.wide = (int)grid.x;
     hipStream_t s = static_cast<hipStream_t>(stream);
     for_types(d, [&](auto dim, auto t, auto form) {
         hipLaunchKernelGGL((paged_rope_append_kernel<dim(), decltype(t), form()>), grid, dim3(256), 0, s, a);

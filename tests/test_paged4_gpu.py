@@ -246,3 +246,25 @@ def test_scales_of_every_size(dtype, n):
     out, lse = c.attn()
     compare(dtype, out, lse, c.reference(), dtype)
 
+
+
+@pytest.mark.parametrize("page,D", [(16, 64), (64, 64), (32, 128), (128, 128)])
+def test_parts_of_more_blocks_than_are_looked_up_at_once(page, D):
+    """Work-groups with runs of tens of thousands of keys: 160 sequences read one sequence's pages with one token's
+    queries, and all have its result; some of its pages are absent."""
+    S, L, H_kv = 160, 14000, 8
+    c = Paged4([1], [L], 2 * H_kv, H_kv, D, page, "bf16", seed=31, absent=[(0, 3), (0, L // page // 2), (0, L // page - 1)]).put()
+    ref = c.reference()
+    q = c.dev["q"].expand(S, -1, -1).contiguous()
+    table = c.dev["block_table"].expand(S, -1).contiguous()
+    dims = pdec.paged_dims_of(q, c.dev["k_pages"], table, max_chunk=1, max_len=L)
+    assert pdec.query_paged_plan(dims)["rows_few"] == 16
+    assert S * L * H_kv / 256 > 64 * 8 * (64 if page >= 64 else 16)  # keys of a work-group; of a look-up
+    out, lse = pdec.paged_attn(q, c.dev["k_pages"], c.dev["v_pages"], table, c.i32(np.arange(S + 1)), c.i32([L] * S), max_chunk=1,
+                               max_len=L, **c.dev_scales)
+    for s in (0, 1, 77, S - 1):
+        compare("bf16", out[s:s + 1], lse[s:s + 1], ref, f"sequence {s}")
+    # the others: the same keys in other divisions
+    assert torch.isfinite(out.float()).all()
+    spread = (lse - lse[0]).abs().max().item()
+    assert spread <= 2.0 ** -15 * (abs(lse[0]).max().item() + 1)

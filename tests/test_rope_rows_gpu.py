@@ -307,3 +307,32 @@ def test_a_serving_loop(dtype, cache):
         pdec.paged_release(i32(lens), table, free, mid, count, page_size=page)
         held = sum(-(-t // page) for t in lens)
         assert count.item() == P - held and (table >= 0).sum().item() == held
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_more_tokens_than_a_grid_has_threads_in_one_direction(fused):
+    """Over four million tokens: the first, the last and some between against the definition, all against each other."""
+    T, D, period = (1 << 22) + 77, 64, 1 << 12
+    spec = dict(head_dim=D)
+    s = pdec.rope_spec(**spec)
+    x = rows(period, 1, D, "bf16", 12).cuda().repeat(T // period + 1, 1, 1)[:T].contiguous()
+    pos = torch.arange(T, device="cuda", dtype=torch.int32) % period
+    if not fused:
+        y, _ = pdec.rope(x, None, pos, s)
+    else:
+        page = 1024
+        n = T // page + 1
+        table = torch.arange(n, device="cuda", dtype=torch.int32)[:, None].contiguous()
+        cu = (torch.arange(n + 1, device="cuda") * page).clamp(max=T).to(torch.int32)
+        base = torch.arange(n, device="cuda", dtype=torch.int32) * page % period
+        pages = [torch.zeros((n, page, 1, D), dtype=x.dtype, device="cuda") for _ in "kv"]
+        lens, after = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+        y = pdec.paged_rope_kv_append(x, x, x, *pages, table, cu, lens, after, s, pos_base=base)
+        assert torch.equal(after, cu[1:] - cu[:-1])
+        assert torch.equal(pages[0].view(-1, 1, D)[:T], y) and torch.equal(pages[1].view(-1, 1, D)[:T], x)
+    assert torch.equal(y[period:2 * period], y[:period]) and torch.equal(y[-period - 77:-77], y[:period])
+    whole = T // period * period
+    assert torch.equal(y[:whole].view(-1, period, D), y[:period].view(1, period, D).expand(T // period, -1, -1))
+    close("bf16", y[:64], turned(x[:64].double().cpu().numpy(), np.arange(64), spec))
+    tail = np.arange(T - 50, T) % period
+    close("bf16", y[-50:], turned(x[-50:].double().cpu().numpy(), tail, spec))

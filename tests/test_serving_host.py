@@ -15,7 +15,7 @@ def table_dims(num_seqs=4, num_tokens=100, page_size=64, num_pages=1000, max_pag
     return pdec.TableDims(num_seqs, num_tokens, page_size, num_pages, max_pages, max_len)
 
 
-@pytest.mark.parametrize("kw", [dict(num_seqs=0), dict(num_seqs=(1 << 27) + 1), dict(num_tokens=0), dict(num_tokens=(1 << 27) + 1),
+@pytest.mark.parametrize("kw", [dict(num_seqs=0), dict(num_seqs=(1 << 20) + 1), dict(num_tokens=0), dict(num_tokens=(1 << 27) + 1),
                                 dict(page_size=0), dict(page_size=8), dict(page_size=48), dict(page_size=2048), dict(num_pages=0),
                                 dict(max_pages=0), dict(max_pages=1 << 25), dict(max_len=-1), dict(max_len=128 * 64 + 1)], ids=str)
 def test_bad_table_dims(kw):
