@@ -49,6 +49,15 @@ __device__ inline double rope_turns(const RopeSpec& r, int i)
 template <typename T> struct RopeReal { typedef float type; };
 template <> struct RopeReal<float> { typedef double type; };
 
+// Stores to global memory, where the compiler can not tell by itself that it is.
+typedef __attribute__((address_space(1))) u32x4_t rope_global_t;
+__device__ inline void rope_store(void* p, u32x4_t x) { *(rope_global_t*)(uintptr_t)p = x; }
+// Past the caches' working set.  The append's rows (queries among them) of 8192 tokens of 36
+// heads of 128 (151 MB) took 38 us kept in the caches and take 28, of 16384 68 and 63; up to
+// 4096 the two are alike, alone and with a reader of the queries behind.  (Float32 gradients
+// turned alone, 262 MB: 52 us past them, 47 not.)
+__device__ inline void rope_store_once(void* p, u32x4_t x) { __builtin_nontemporal_store(x, (rope_global_t*)(uintptr_t)p); }
+
 // 16 bytes of a row, E elements.
 template <typename T>
 struct RopePiece {
@@ -188,8 +197,8 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeRowsArgs a)
         for (int k = 0; k < BATCH; ++k) {
             if (!here[k]) continue;
             me.turn(a.spec, x[k][0], x[k][1]);
-            *reinterpret_cast<u32x4_t*>(dst[k] + me.off[0]) = x[k][0].x;
-            *reinterpret_cast<u32x4_t*>(dst[k] + me.off[1]) = x[k][1].x;
+            rope_store(dst[k] + me.off[0], x[k][0].x);
+            rope_store(dst[k] + me.off[1], x[k][1].x);
         }
     }
 }
@@ -247,8 +256,8 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
         }
     }
     const int t = wg * 4 + w;
-    int page, slot, pos;
-    if (t >= io.num_tokens || !paged_rope_place(a, t, page, slot, pos)) return;
+    if (t >= io.num_tokens) return;
+    int page = -1, slot = 0, pos = 0;
     L me;
     me.init(a.spec, lane);
     const int its_q = (a.H_q + L::HEADS - 1) / L::HEADS, its_k = (io.H_kv + L::HEADS - 1) / L::HEADS;
@@ -264,7 +273,6 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
         for (int k = 0; k < BATCH; ++k) {
             const int it = it0 + k * a.split;
             kind[k] = it < its_q ? 0 : it < its_q + its_k ? 1 : it < its ? 2 : 3;
-            if (kind[k] > 0 && page < 0) kind[k] = 3;
             const int h0 = (kind[k] == 0 ? it : kind[k] == 1 ? it - its_q : it - its_q - its_k) * L::HEADS;
             head[k] = h0 + me.head;
             if (kind[k] == 3 || head[k] >= (kind[k] == 0 ? a.H_q : io.H_kv)) continue;
@@ -273,19 +281,22 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
             x[k][0].x = *reinterpret_cast<const u32x4_t*>(src + (kind[k] == 2 ? v0 : me.off[0]));
             x[k][1].x = *reinterpret_cast<const u32x4_t*>(src + (kind[k] == 2 ? v1 : me.off[1]));
         }
-        if (it0 == (int)blockIdx.y)
-            me.at(a.spec, lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0, lane, pos, cs[w]);  // under the loads
+        if (it0 == (int)blockIdx.y) {  // under the first loads
+            const double turns_i = lane < a.spec.R / 2 ? rope_turns(a.spec, lane) : 0.0;
+            if (!paged_rope_place(a, t, page, slot, pos)) return;
+            me.at(a.spec, turns_i, lane, pos, cs[w]);
+        }
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
-            if (kind[k] == 3) continue;
+            if (kind[k] == 3 || (kind[k] > 0 && page < 0)) continue;
             const bool here = head[k] < (kind[k] == 0 ? a.H_q : io.H_kv);
             if (kind[k] < 2 && here) me.turn(a.spec, x[k][0], x[k][1]);
             const int o0 = kind[k] == 2 ? v0 : me.off[0], o1 = kind[k] == 2 ? v1 : me.off[1];
             if (kind[k] == 0) {
                 if (here && (me.turns || a.q_out != a.q)) {
                     T* dst = static_cast<T*>(a.q_out) + t * a.q_out_stride + (long)head[k] * D;
-                    *reinterpret_cast<u32x4_t*>(dst + o0) = x[k][0].x;
-                    *reinterpret_cast<u32x4_t*>(dst + o1) = x[k][1].x;
+                    rope_store_once(dst + o0, x[k][0].x);
+                    rope_store_once(dst + o1, x[k][1].x);
                 }
                 continue;
             }
@@ -293,8 +304,8 @@ __global__ __launch_bounds__(256) void paged_rope_append_kernel(PagedRopeArgs a)
             if constexpr (FORM == kPlainRows) {
                 if (here) {
                     T* dst = reinterpret_cast<T*>(pages) + ((((long)page << io.page_shift) + slot) * io.H_kv + head[k]) * D;
-                    *reinterpret_cast<u32x4_t*>(dst + o0) = x[k][0].x;
-                    *reinterpret_cast<u32x4_t*>(dst + o1) = x[k][1].x;
+                    rope_store_once(dst + o0, x[k][0].x);
+                    rope_store_once(dst + o1, x[k][1].x);
                 }
             } else {
                 // the heads' rows in order, eight consecutive elements to a lane
