@@ -1,5 +1,5 @@
 // Attention over paged caches on v_mfma_f32_16x16x4_f32: float32 queries, over
-// float32, 8-bit or 4-bit pages.
+// float32 or 8-bit pages.
 //
 // The work-group is 4 waves; wave w takes keys 16 w .. 16 w + 15 of every unit
 // (one page, as pages hold 16 tokens at least) with an online-softmax state of
@@ -9,9 +9,8 @@
 // holding D / 4 consecutive elements of a key (query) row and D / 16 of each of
 // four value rows.
 //
-// 8-bit and 4-bit rows are widened in registers.  A key's scale multiplies its score, a
-// value's scale the value, and a 4-bit row's scales its elements as they are widened:
-// powers of two, so none rounds.
+// 8-bit rows are widened in registers.  A key's scale multiplies its score, a
+// value's scale the value: powers of two, so neither rounds.
 //
 // What bounds it: for few rows the memory round trips and then the bytes of the
 // pages (one token of 28 heads over 32768 keys 39 us; the next unit's keys and
@@ -19,12 +18,12 @@
 // float32 products (133 TFLOP/s in a large library product).
 #pragma once
 
-#include "paged_e2m1.h"
+#include "kernel_mfma.h"
+#include "paged_common.h"
 
 namespace pdec {
 
 struct fp8_t { uint8_t bits; };  // one e4m3 element of a cache row
-struct fp4_t { uint8_t bits; };  // a byte of a cache row: two e2m1 elements
 
 // N consecutive cache elements of one row as raw words.
 template <typename TC, int N>
@@ -56,39 +55,6 @@ struct PagedRaw {
     }
 };
 
-template <int N>
-struct PagedRaw<fp4_t, N> {
-    static constexpr int BYTES = N / 2;
-    uint32_t w[(BYTES + 3) / 4];
-    __device__ inline void load(const unsigned char* p)
-    {
-        if constexpr (BYTES == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
-        else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
-        else {
-            typedef uint32_t words_t __attribute__((ext_vector_type(BYTES / 4)));
-            const words_t x = *reinterpret_cast<const words_t*>(p);
-#pragma unroll
-            for (int i = 0; i < BYTES / 4; ++i) w[i] = x[i];
-        }
-    }
-    // all elements, which have one scale
-    __device__ inline void get(float scale, float (&v)[N]) const
-    {
-        if constexpr (N == 4) {
-            const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[0], scale, 1);
-            v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
-        } else {
-#pragma unroll
-            for (int i = 0; i < N / 8; ++i) {
-                float x[8];
-                e2m1_f32(w[i], scale, x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[8 * i + j] = x[j];
-            }
-        }
-    }
-};
-
 __device__ inline f32x4_t paged_mfma4(float a, float b, f32x4_t c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -102,10 +68,7 @@ __global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_ker
     constexpr int DT = D / 16;   // 16-wide d tiles
     constexpr int OROW = D + 4;  // row pitch of the merge buffer, in floats
     constexpr int ESZ = (int)sizeof(TC);
-    constexpr bool SCALED = std::is_same<TC, fp8_t>::value;  // a scale per key
-    constexpr bool FP4 = std::is_same<TC, fp4_t>::value;     // four bits, head-major pages (paged_e2m1.h)
-    constexpr int SPK = D / kE2m1Block;
-    static_assert(KPL <= kE2m1Block && kE2m1Block % DT == 0, "a lane's elements of a key have one scale, and of a value");
+    constexpr bool SCALED = sizeof(TC) == 1;
     __shared__ __attribute__((aligned(16))) float o_s[NW * RT * OROW];
     __shared__ float m_s[NW][RT], l_s[NW][RT];
 
@@ -148,8 +111,7 @@ __global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_ker
 
         PagedRaw<TC, KPL> kx;
         PagedRaw<TC, DT> vx[4];
-        uint32_t ks = 0, vs = 0;  // scales of keys 4 lg .. 4 lg + 3; FP4: of the lane's elements of key l16
-        uint32_t vs4[4] = {0, 0, 0, 0};  // FP4: of its elements of values 4 lg + i
+        uint32_t ks = 0, vs = 0;  // scales of keys 4 lg .. 4 lg + 3
         // The wave's 16 keys of a unit are on one page.  Units none of whose keys a row
         // sees, and keys without a page, are passed over.
         const int32_t* table = a.block_table + (long)part.s * a.max_pages;
@@ -165,27 +127,11 @@ __global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_ker
         auto scale_at = [&](int u, int page) {
             return (((long)page * a.H_kv + part.head) << a.page_shift) + ((u * kUnit + 16 * w) & ((1 << a.page_shift) - 1)) + 4 * lg;
         };
-        auto row4 = [&](int u, int page) { return e2m1_row(page, part.head, a.H_kv, a.page_shift, (u * kUnit + 16 * w) & ((1 << a.page_shift) - 1)); };
         auto load_k = [&](int u, int page) {
-            if constexpr (FP4) {
-                const long r = row4(u, page) + l16;
-                kx.load(static_cast<const unsigned char*>(a.k_pages) + r * (D / 2) + KPL * lg / 2);
-                ks = a.k_scales[r * SPK + KPL * lg / kE2m1Block];
-                return;
-            }
             kx.load(static_cast<const unsigned char*>(a.k_pages) + (row_of(u, page) + l16) * rowb + ((long)part.head * D + KPL * lg) * ESZ);
             if constexpr (SCALED) ks = *reinterpret_cast<const uint32_t*>(a.k_scales + scale_at(u, page));
         };
         auto load_v = [&](int u, int page) {
-            if constexpr (FP4) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const long r = row4(u, page) + 4 * lg + i;
-                    vx[i].load(static_cast<const unsigned char*>(a.v_pages) + r * (D / 2) + DT * l16 / 2);
-                    vs4[i] = a.v_scales[r * SPK + DT * l16 / kE2m1Block];
-                }
-                return;
-            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 vx[i].load(static_cast<const unsigned char*>(a.v_pages) + (row_of(u, page) + 4 * lg + i) * rowb + ((long)part.head * D + DT * l16) * ESZ);
@@ -202,18 +148,12 @@ __global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_ker
             f32x4_t s[NT], s1[NT];  // two sums where there is one tile: the products of a sum wait for each other
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt] = s1[nt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            float kv[KPL];
-            if constexpr (FP4) kx.get(e2m1_scale(ksc), kv);
-            else {
-#pragma unroll
-                for (int j = 0; j < KPL; ++j) kv[j] = kx.get(j);
-            }
 #pragma unroll
             for (int j = 0; j < KPL; ++j)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    if (NT == 1 && (j & 1)) s1[nt] = paged_mfma4(kv[j], qv[nt][j], s1[nt]);
-                    else s[nt] = paged_mfma4(kv[j], qv[nt][j], s[nt]);
+                    if (NT == 1 && (j & 1)) s1[nt] = paged_mfma4(kx.get(j), qv[nt][j], s1[nt]);
+                    else s[nt] = paged_mfma4(kx.get(j), qv[nt][j], s[nt]);
                 }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -260,16 +200,15 @@ __global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_ker
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float sc = SCALED ? paged_scale(vs, i) : 1.f;
-                if constexpr (FP4) vx[i].get(e2m1_scale(vs4[i]), vf[i]);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    if constexpr (!FP4) vf[i][dt] = SCALED ? vx[i].get(dt) * sc : vx[i].get(dt);
+                    vf[i][dt] = SCALED ? vx[i].get(dt) * sc : vx[i].get(dt);
                     if (!all_see) odd |= strange(vf[i][dt]);
                 }
             }
-            // 8- and 4-bit values have been widened into other registers: the next ones come
+            // 8-bit values have been widened into other registers: the next ones come
             // under the products, float32 ones under the next scores
-            if ((SCALED || FP4) && u < part.u1) load_v(u, page);
+            if (SCALED && u < part.u1) load_v(u, page);
             auto products = [&]() {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -307,7 +246,7 @@ __global__ __launch_bounds__(256, NT == 1 || D == 64 ? 2 : 1) void paged_f32_ker
                         }
                     }
             }
-            if (!SCALED && !FP4 && u < part.u1) load_v(u, page);
+            if (!SCALED && u < part.u1) load_v(u, page);
         }
 
         // ---- merge of the four waves; lane: row l % 16 of tile nt, d = D/4 (l / 16) + DT j + dt ----

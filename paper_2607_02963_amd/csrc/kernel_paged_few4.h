@@ -1,5 +1,5 @@
-// Attention over 4-bit paged caches, few query rows per kv head, bfloat16 queries, on
-// v_mfma_f32_16x16x32_bf16.
+// Attention over 4-bit paged caches, few query rows per kv head (bfloat16) or any (float32),
+// on v_mfma_f32_16x16x32_bf16.
 //
 // The division of the work is that of the other caches' few-row kernel
 // (kernel_paged_few.h): eight waves, each with a ring of its own in LDS, a softmax state
@@ -18,6 +18,11 @@
 // rounded: a power of two takes no bits.  Where every row sees the block and no scale is
 // NaN, that is an addition to the exponents of two rounded probabilities at a time, of
 // scales that the wave has spread in LDS as bfloat16 exponents.
+//
+// float32 queries and probabilities are taken as the sums of three bfloat16 numbers, eight
+// of their 24 bits each: exact, and 4-bit keys and values are exact in bfloat16, so that
+// three products are the float32 product, at the rate of the bfloat16 ones (three times
+// 1200 TFLOP/s against 154 on the float32 matrix product).
 #pragma once
 
 #include "kernel_paged_few.h"
@@ -43,8 +48,21 @@ __device__ inline void dma_16B_lanes(uint64_t addr, uint32_t lds_base, uint64_t 
 // inline assembly the compiler would not keep it apart from a v_exp_f32 before it).
 __device__ float mul_zero(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
 
-// BIG: pages of 64 keys or more, a block to a page.
-template <int D, int NT, bool BIG>
+// x as the sum of three bfloat16 numbers of its sign, the first 16 bits of x and of what
+// each leaves; two at a time.
+__device__ inline void three_bf16(float x0, float x1, uint32_t (&y)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+        y[i] = (u0 >> 16) | (u1 & 0xffff0000u);
+        x0 -= __uint_as_float(u0 & 0xffff0000u);
+        x1 -= __uint_as_float(u1 & 0xffff0000u);
+    }
+}
+
+// BIG: pages of 64 keys or more, a block to a page.  T: an element of q and out.
+template <int D, int NT, bool BIG, typename T>
 __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 {
     constexpr int NW = kFewWaves;
@@ -61,6 +79,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     constexpr int PT = BIG ? TENSOR / 1024 : 4;  // instructions of K or V per block
     constexpr int PB = 2 * PT + 1;               // and of a block, its scales with them
     constexpr int KS = D / 32, DT = D / 16;
+    constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;  // bfloat16 numbers to a query element or probability
     constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
     constexpr uint64_t QLANES = BIG || QB == 1024 ? ~0ull : (1ull << (QB / 16)) - 1;
     constexpr uint64_t SLANES = (1ull << (SC / 16)) - 1;
@@ -169,14 +188,28 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 
         // ---- this lane's rows: 16 nt + l % 16; those past the last see nothing ----
         int seen[NT];
-        u32x4_t qf[NT][KS];
+        u32x4_t qf[NT][KS][TERMS];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = 16 * nt + l16, rr = row0 + min(r, nrows - 1);
             seen[nt] = r < nrows ? paged_seen(a, sq, rr / a.G) : 0;
-            const uint16_t* q = static_cast<const uint16_t*>(a.q) + paged_qrow(a, sq, head, rr) * D;
+            const T* q = static_cast<const T*>(a.q) + paged_qrow(a, sq, head, rr) * D + 8 * KS * lg;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) qf[nt][i] = *reinterpret_cast<const u32x4_t*>(q + 8 * KS * lg + 8 * i);
+            for (int i = 0; i < KS; ++i) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t*>(q + 8 * i);
+                if constexpr (TERMS == 1) qf[nt][i][0] = x;
+                else {
+                    const u32x4_t y = *reinterpret_cast<const u32x4_t*>(q + 8 * i + 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t z[3];
+                        if (j < 2) three_bf16(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]), z);
+                        else three_bf16(__uint_as_float(y[2 * j - 4]), __uint_as_float(y[2 * j - 3]), z);
+#pragma unroll
+                        for (int e = 0; e < TERMS; ++e) qf[nt][i][e][j] = z[e];
+                    }
+                }
+            }
         }
         // keys that every row sees (rows past the last are masked or not, their results are not stored)
         const int least = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, row0 / a.G));
@@ -254,7 +287,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                             for (int i = 0; i < KS; ++i) {
                                 const bf16x8_t kf = as_bf16x8(e2m1_bf16(x[i], ks));
 #pragma unroll
-                                for (int nt = 0; nt < N; ++nt) s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[nt][i]), s[nt][kt]);
+                                for (int nt = 0; nt < N; ++nt)
+#pragma unroll
+                                    for (int e = TERMS - 1; e >= 0; --e) s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[nt][i][e]), s[nt][kt]);
                             }
                         }
 #pragma unroll
@@ -293,12 +328,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                             p[nt][j] = fast_exp2(fmaf(p[nt][j], c, -m_ref[nt]));  // 0 for a hidden key
                             sum[j & 3] += p[nt][j];
                         }
-                        // the row sums take P unrounded; the product's operands are bf16, so P is
-                        // rounded by half a step (2^-8) of each term, as out is
+                        // the row sums take P unrounded; the product's operands are bf16, so with bf16
+                        // queries P is rounded by half a step (2^-8) of each term, as out is
                         lsum[nt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     }
                     // O += V P of keys 16 lg + 8 h .. + 7, blk's 32 elements
-                    auto products = [&](int blk, int h, const u32x4_t (&pf)[N], auto fast) __attribute__((always_inline)) {
+                    auto products = [&](int blk, int h, const u32x4_t (&pf)[N][TERMS], auto fast) __attribute__((always_inline)) {
 #pragma unroll
                         for (int dt = 2 * blk; dt < 2 * blk + 2; ++dt) {
                             if (N > 1) vraw[dt] = read_v(dt);
@@ -306,7 +341,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                             if (!fast) asm volatile("" : "+v"(x));  // else both paths' widening comes before the branch
                             const bf16x8_t vf = as_bf16x8(e2m1_bf16(x, 1.f));
 #pragma unroll
-                            for (int nt = 0; nt < N; ++nt) o[nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt]), o[nt][dt]);
+                            for (int nt = 0; nt < N; ++nt)
+#pragma unroll
+                                for (int e = TERMS - 1; e >= 0; --e) o[nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt][e]), o[nt][dt]);
                         }
                     };
                     if (full && !odd) {
@@ -314,27 +351,34 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         // may become 2^-127 times the scale: nothing beside its row's largest, which is
                         // 2^-8 at least), one beyond the largest number NaN
                         typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
-                        i16x2_t pe[N][8];
+                        i16x2_t pe[N][8][TERMS];
 #pragma unroll
                         for (int nt = 0; nt < N; ++nt)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                pe[nt][j] = __builtin_bit_cast(i16x2_t, pack_bf16x2(p[nt][2 * j], p[nt][2 * j + 1]));
+                            for (int j = 0; j < 8; ++j) {
+                                uint32_t y[3];
+                                if constexpr (TERMS == 1) y[0] = pack_bf16x2(p[nt][2 * j], p[nt][2 * j + 1]);
+                                else three_bf16(p[nt][2 * j], p[nt][2 * j + 1], y);
+#pragma unroll
+                                for (int e = 0; e < TERMS; ++e) pe[nt][j][e] = __builtin_bit_cast(i16x2_t, y[e]);
+                            }
 #pragma unroll
                         for (int blk = 0; blk < SPK; ++blk)
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 if (N > 1) __builtin_amdgcn_sched_barrier(0);
                                 const u32x4_t e = *(lds_u32x4_t*)(uintptr_t)(eat + 2 * KB * blk + 16 * h);
-                                u32x4_t pf[N];
+                                u32x4_t pf[N][TERMS];
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
                                     const uint32_t ej = e[j];
 #pragma unroll
-                                    for (int nt = 0; nt < N; ++nt) {
-                                        const i16x2_t x = __builtin_elementwise_add_sat(pe[nt][4 * h + j], __builtin_bit_cast(i16x2_t, ej));
-                                        pf[nt][j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, (i16x2_t)0));
-                                    }
+                                    for (int nt = 0; nt < N; ++nt)
+#pragma unroll
+                                        for (int i = 0; i < TERMS; ++i) {
+                                            const i16x2_t x = __builtin_elementwise_add_sat(pe[nt][4 * h + j][i], __builtin_bit_cast(i16x2_t, ej));
+                                            pf[nt][i][j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, (i16x2_t)0));
+                                        }
                                 }
                                 products(blk, h, pf, std::true_type{});
                             }
@@ -352,14 +396,22 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
                             for (int blk = 0; blk < SPK; ++blk) {
                                 if (N > 1) __builtin_amdgcn_sched_barrier(0);
-                                u32x4_t pf[N];
+                                u32x4_t pf[N][TERMS];
 #pragma unroll
                                 for (int j = 0; j < 8; j += 2) {
                                     const float s0 = SPK == 4 ? paged_scale(vs[j], blk) : paged_scale(vs[j / 2], blk);
                                     const float s1 = SPK == 4 ? paged_scale(vs[j + 1], blk) : paged_scale(vs[j / 2], 2 + blk);
 #pragma unroll
-                                    for (int nt = 0; nt < N; ++nt)
-                                        pf[nt][j >> 1] = pack_bf16x2(mul_zero(p[nt][8 * h + j], s0), mul_zero(p[nt][8 * h + j + 1], s1));
+                                    for (int nt = 0; nt < N; ++nt) {
+                                        const float x0 = mul_zero(p[nt][8 * h + j], s0), x1 = mul_zero(p[nt][8 * h + j + 1], s1);
+                                        if constexpr (TERMS == 1) pf[nt][0][j >> 1] = pack_bf16x2(x0, x1);
+                                        else {
+                                            uint32_t y[3];
+                                            three_bf16(x0, x1, y);
+#pragma unroll
+                                            for (int e = 0; e < TERMS; ++e) pf[nt][e][j >> 1] = y[e];
+                                        }
+                                    }
                                 }
                                 products(blk, h, pf, std::false_type{});
                             }
@@ -418,8 +470,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                 const bool any = __float_as_uint(L) != 0;  // L is 0, positive or NaN
                 const float inv = any ? 1.f / L : 0.f;
                 acc *= inv;
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + qr * D + 4 * d4) =
-                    make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
+                if constexpr (TERMS == 3) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + qr * D + 4 * d4) = acc;
+                else
+                    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + qr * D + 4 * d4) =
+                        make_uint2(pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3]));
                 if (d4 == 0 && a.lse) a.lse[qr] = any ? kLn2 * (M + __log2f(L)) : kNegInf;
             }
         }

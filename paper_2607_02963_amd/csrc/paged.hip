@@ -27,12 +27,10 @@ void launch_f32_rows(const PagedArgs& a, hipStream_t s)
 
 }  // namespace
 
-void launch_paged_f32(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
+void launch_paged_f32(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
 {
-    auto rows = [&](auto cache) { head_dim == 128 ? launch_f32_rows<128, decltype(cache)>(a, s) : launch_f32_rows<64, decltype(cache)>(a, s); };
-    if (cache_dtype == PDEC_DTYPE_E2M1) rows(fp4_t{});
-    else if (cache_dtype == PDEC_DTYPE_E4M3) rows(fp8_t{});
-    else rows(float{});
+    if (head_dim == 128) fp8 ? launch_f32_rows<128, fp8_t>(a, s) : launch_f32_rows<128, float>(a, s);
+    else fp8 ? launch_f32_rows<64, fp8_t>(a, s) : launch_f32_rows<64, float>(a, s);
 }
 
 namespace {
@@ -171,16 +169,16 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     }
     if (p.use_few) {
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
-        const bool f32 = d->dtype == PDEC_DTYPE_F32;
-        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 || d->head_dim == 128 ? 32 : most <= 48 ? 48 : 64;
+        const bool f32 = d->dtype == PDEC_DTYPE_F32, four = d->cache_dtype == PDEC_DTYPE_E2M1;
+        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 || (four && d->head_dim == 128) ? 32 : most <= 48 ? 48 : 64;
+        if (f32 && four && d->head_dim == 128) p.few.rows = 16;  // the registers of three terms (kernel_paged_few4.h)
         // heads' rows of a cache line or half of one: two heads to a work-group (kernel_paged_few.h)
-        if (!f32 && d->cache_dtype != PDEC_DTYPE_E2M1 && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0)
-            p.few.heads = 2;
+        if (!f32 && !four && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;
         // a start's price, in units; over 4-bit pages, whose units are the shortest, it was swept (4, 8, 16,
         // 24, 32): 32 tokens over 1200 to 16384 keys, heads of 128, 44.2, 42.7, 40.5, 41.1, 41.3 us; drafted
         // tokens of 13 sequences, heads of 64, 34.4, 32.3, 27.9, 26.3, 27.7
-        const int pad = f32 ? 1 : d->cache_dtype != PDEC_DTYPE_E2M1 ? 4 : d->head_dim == 128 ? 16 : 24;
-        if (!divide(d, p.few, f32 ? 512 : 256, 2, pad, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+        const int pad = four ? (d->head_dim == 128 ? 16 : 24) : f32 ? 1 : 4;
+        if (!divide(d, p.few, f32 && !four ? 512 : 256, 2, pad, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;
 }
@@ -337,8 +335,10 @@ int pdec_paged_attn(const pdec_paged_dims* d, const void* q, const void* k_pages
     }
     if (p.use_few) {
         place(p.few, ws);
-        if (d->dtype == PDEC_DTYPE_F32) launch_paged_f32(p.few, d->head_dim, d->cache_dtype, s);
-        else launch_paged_few(p.few, d->head_dim, d->cache_dtype, s);
+        const bool fp8 = d->cache_dtype == PDEC_DTYPE_E4M3, f32 = d->dtype == PDEC_DTYPE_F32;
+        if (d->cache_dtype == PDEC_DTYPE_E2M1) launch_paged_few4(p.few, d->head_dim, f32, s);
+        else if (f32) launch_paged_f32(p.few, d->head_dim, fp8, s);
+        else launch_paged_few(p.few, d->head_dim, fp8, s);
         if ((rc = launched()) != PDEC_OK || (rc = finish(p.few)) != PDEC_OK) return rc;
     }
     return PDEC_OK;

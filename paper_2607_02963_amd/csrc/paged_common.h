@@ -315,8 +315,9 @@ __device__ inline int paged_page(const PagedArgs& a, int s, int t)
 // 2^(byte - 127) of byte i of a word; 0 for a byte of 0
 __device__ inline float paged_scale(uint32_t word, int i) { return __uint_as_float(((word >> (8 * i)) & 255u) << 23); }
 
-void launch_paged_f32(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t stream);
-void launch_paged_few(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t stream);
+void launch_paged_f32(const PagedArgs& a, int head_dim, bool fp8, hipStream_t stream);
+void launch_paged_few(const PagedArgs& a, int head_dim, bool fp8, hipStream_t stream);
+void launch_paged_few4(const PagedArgs& a, int head_dim, bool f32, hipStream_t stream);
 void launch_paged_rows(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t stream);
 void launch_paged_finish(const PagedArgs& a, int head_dim, int dtype, hipStream_t stream);
 

@@ -32,26 +32,35 @@ void launch_few(const PagedArgs& a, hipStream_t s)
     }
 }
 
-template <int D, bool BIG>
+template <int D, bool BIG, typename T>
 void launch_few4(const PagedArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)a.blocks), block(64 * kFewWaves);
-    if (a.rows == 16) hipLaunchKernelGGL((paged_few4_kernel<D, 1, BIG>), grid, block, 0, s, a);
-    else if (a.rows == 32) hipLaunchKernelGGL((paged_few4_kernel<D, 2, BIG>), grid, block, 0, s, a);
-    else if constexpr (D == 64) hipLaunchKernelGGL((paged_few4_kernel<D, 3, BIG>), grid, block, 0, s, a);
+    if (a.rows == 16) hipLaunchKernelGGL((paged_few4_kernel<D, 1, BIG, T>), grid, block, 0, s, a);
+    else if constexpr (D == 64 || sizeof(T) == 2) {
+        if (a.rows == 32) hipLaunchKernelGGL((paged_few4_kernel<D, 2, BIG, T>), grid, block, 0, s, a);
+        else if constexpr (D == 64 && sizeof(T) == 2) hipLaunchKernelGGL((paged_few4_kernel<D, 3, BIG, T>), grid, block, 0, s, a);
+    }
+}
+
+template <typename T>
+void launch_few4(const PagedArgs& a, int head_dim, hipStream_t s)
+{
+    const bool big = a.page_shift >= 6;
+    if (head_dim == 128) big ? launch_few4<128, true, T>(a, s) : launch_few4<128, false, T>(a, s);
+    else big ? launch_few4<64, true, T>(a, s) : launch_few4<64, false, T>(a, s);
 }
 
 }  // namespace
 
-void launch_paged_few(const PagedArgs& a, int head_dim, int cache_dtype, hipStream_t s)
+void launch_paged_few4(const PagedArgs& a, int head_dim, bool f32, hipStream_t s)
 {
-    if (cache_dtype == PDEC_DTYPE_E2M1) {
-        const bool big = a.page_shift >= 6;
-        if (head_dim == 128) big ? launch_few4<128, true>(a, s) : launch_few4<128, false>(a, s);
-        else big ? launch_few4<64, true>(a, s) : launch_few4<64, false>(a, s);
-        return;
-    }
-    const bool two = a.heads == 2, fp8 = cache_dtype == PDEC_DTYPE_E4M3;
+    f32 ? launch_few4<float>(a, head_dim, s) : launch_few4<uint16_t>(a, head_dim, s);
+}
+
+void launch_paged_few(const PagedArgs& a, int head_dim, bool fp8, hipStream_t s)
+{
+    const bool two = a.heads == 2;
     if (head_dim == 128 && !fp8) launch_few<128, false, 1>(a, s);
     else if (head_dim == 128) two ? launch_few<128, true, 2>(a, s) : launch_few<128, true, 1>(a, s);
     else if (fp8) two ? launch_few<64, true, 2>(a, s) : launch_few<64, true, 1>(a, s);
