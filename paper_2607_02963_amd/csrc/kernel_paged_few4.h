@@ -15,9 +15,9 @@
 // A lane's 16 bytes of a key row (8 at D = 64) have one scale, which the widening
 // v_cvt_scalef32_pk_bf16_fp4 takes with it.  A lane's 16 values have a scale each, so
 // that those multiply the probabilities, once for each block of 32 d, before they are
-// rounded: a power of two takes no bits.  Where every row sees the block and no scale is
-// NaN, that is an addition to the exponents of two rounded probabilities at a time, of
-// scales that the wave has spread in LDS as bfloat16 exponents.
+// rounded: a power of two takes no bits.  Where every row sees the block and all its scales
+// are of 2^-63 .. 2^64, that is an addition to the exponents of two rounded probabilities at
+// a time, of scales that the wave has spread in LDS as bfloat16 exponents.
 //
 // float32 queries and probabilities are taken as the sums of three bfloat16 numbers, eight
 // of their 24 bits each: exact, and 4-bit keys and values are exact in bfloat16, so that
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                 const bool full = t + KB <= least && have == (1u << Q) - 1;
                 const bool mine_there = BIG || (have >> lg & 1);
                 // the values' scales of key t + lane, spread by blocks of d: k where bfloat16 has its exponent
-                bool odd;  // one of them is NaN
+                bool odd;  // one of them is beyond 2^-63 .. 2^64: its byte's first two bits are alike
                 {
                     typedef __attribute__((address_space(3))) const uint16_t lds_u16c_t;
                     typedef __attribute__((address_space(3))) const uint32_t lds_u32c_t;
@@ -251,7 +251,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                     uint32_t x;
                     if constexpr (SPK == 4) x = *(lds_u32c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
                     else x = *(lds_u16c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
-                    odd = __any((((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u) != 0);
+                    constexpr uint32_t FIRST = SPK == 4 ? 0x80808080u : 0x8080u;
+                    odd = __any(((x ^ (x << 1)) & FIRST) != FIRST);
 #pragma unroll
                     for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)(((x >> (8 * i) & 255u) << 7) - (127 << 7));
                 }
@@ -347,9 +348,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         }
                     };
                     if (full && !odd) {
-                        // P times 2^k: k added to its exponent.  A product below 2^-126 is 0 (and a P of 0
-                        // may become 2^-127 times the scale: nothing beside its row's largest, which is
-                        // 2^-8 at least), one beyond the largest number NaN
+                        // P times 2^k: k added to its exponent.  A P of 0 may become 2^-127 times the scale,
+                        // 2^-63 at most (of a larger scale that would be seen beside values of about one).  A
+                        // product below 2^-126 is 0: 2^-55 of a row's largest P, 2^-8 at least, by the scale
                         typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
                         i16x2_t pe[N][8][TERMS];
 #pragma unroll

@@ -247,6 +247,56 @@ def test_scales_of_every_size(dtype, n):
     compare(dtype, out, lse, c.reference(), dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("D,page", [(128, 32), (64, 64)])
+@pytest.mark.parametrize("size", [-100, -64, 66, 118])
+def test_values_far_from_one(dtype, n, D, page, size):
+    """Values of 2^size: the small ones in all keys, the large ones in keys whose probability, some e^-136, is below
+    float32's range, so that they add nothing to the others' values of about one."""
+    c = Paged4([n, n], [700, 333], 8, 2, D, page, dtype, seed=33)
+    rng = np.random.default_rng(4)
+    k, v = (rng.standard_normal(c.vals[name].shape) for name in "kv")
+    if size < 0:
+        v *= 2.0 ** size
+    else:
+        c.q[:, :, 0] = 4
+        for s, t in ((0, 5), (0, 100), (0, 640), (1, 0), (1, 200)):
+            at = c.table[s, t // page], t % page
+            k[at][:, 0] = -34 * D ** 0.5
+            v[at][:] *= 2.0 ** size
+    c.set("k", *quantise4(k))
+    c.set("v", *quantise4(v))
+    out, lse = c.attn()
+    compare(dtype, out, lse, c.reference(), dtype)
+
+
+@pytest.mark.parametrize("n,H_q,H_kv,D", [
+    (3, 8, 2, 64), (4, 14, 2, 64), (16, 12, 3, 64), (2, 14, 2, 128), (8, 8, 2, 128), (31, 8, 2, 64), (70, 14, 2, 128)])
+@pytest.mark.parametrize("lens", [[200], [250, 70, 130], [900, 2900, 70], [100] * 20])
+@pytest.mark.parametrize("page", [16, 128])
+def test_every_form_of_the_kernels_of_float32(n, H_q, H_kv, D, lens, page):
+    ns = [n] + [1 + (5 * i) % n for i in range(1, len(lens))]
+    c = Paged4(ns, lens, H_q, H_kv, D, page, "f32", seed=n).put()
+    dims = pdec.paged_dims_of(c.dev["q"], c.dev["k_pages"], c.dev["block_table"], max_chunk=n, max_len=max(lens))
+    plan = pdec.query_paged_plan(dims)
+    assert plan["rows_few"] == (16 if D == 128 or n * H_q // H_kv <= 16 else 32) and plan["rows_many"] == 0
+    out, lse = c.attn(max_chunk=n, max_len=max(lens))
+    compare("f32", out, lse, c.reference(), f"{lens}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 40])
+def test_queries_that_are_not_finite_stay_with_their_rows(dtype, n):
+    """A NaN among a query's elements makes its row NaN, out and lse, and no other row of its 16."""
+    c = Paged4([n, 2], [700, 300], 8, 2, 128, 64, dtype, seed=34).put()
+    o1, l1 = (x.clone() for x in c.attn())
+    c.dev["q"][0, 3, 77] = float("nan")
+    o2, l2 = c.attn()
+    assert torch.isnan(o2[0, 3].float()).all() and torch.isnan(l2[0, 3])
+    o2[0, 3], l2[0, 3] = o1[0, 3], l1[0, 3]
+    assert torch.equal(bits(o1), bits(o2)) and torch.equal(bits(l1), bits(l2))
+
 
 @pytest.mark.parametrize("page,D", [(16, 64), (64, 64), (32, 128), (128, 128)])
 def test_parts_of_more_blocks_than_are_looked_up_at_once(page, D):
