@@ -1091,6 +1091,8 @@ def rope(q, k, positions, spec, *, backward=False, q_out=None, k_out=None, strea
         if k_out is None:
             k_out = _empty(stream, ks, dtype, q.device)
         (kp, kst), (kop, kost) = _heads(k, "k", dev, dtype, ks), _heads(k_out, "k_out", dev, dtype, ks)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
     (qp, qst), (qop, qost) = _heads(q, "q", dev, dtype, qs), _heads(q_out, "q_out", dev, dtype, qs)
     rc = lib().pdec_rope(spec, T, qs[1], ks[1], code, int(bool(backward)), _ptr(positions, "positions", dev, torch.int32, (T,)),
                          qp, qst, qop, qost, kp, kst, kop, kost, _raw_stream(dev) if stream is None else stream.cuda_stream)

@@ -131,6 +131,12 @@ def test_strided_rows_in_place_and_a_table(dtype, spec):
     close(dtype, qt, turned(x[:, :H_q].double().numpy(), pos, spec, f=f))
 
 
+def test_an_output_of_keys_without_keys_is_refused():
+    q, pos = rows(2, 3, 64, "f32", 1).cuda(), i32([0, 1])
+    with pytest.raises(ValueError, match="k_out"):
+        pdec.rope(q, None, pos, pdec.rope_spec(64), k_out=q.clone())
+
+
 @pytest.mark.parametrize("spec", SPECS, ids=range(len(SPECS)))
 def test_the_gradient_is_the_formulas_and_that_of_differences(spec):
     """L = sum w y of float32 rows: dL/dx is the transposed turn of w; and as y is linear in x, (L(x + h e) -
