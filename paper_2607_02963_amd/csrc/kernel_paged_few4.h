@@ -4,8 +4,9 @@
 // The division of the work is that of the other caches' few-row kernel
 // (kernel_paged_few.h): eight waves, each with a ring of its own in LDS, a softmax state
 // of its own, joined at the part's end.  A wave's block is 64 keys, four quarters of 16,
-// each on one page; a quarter of K or V is one DMA instruction, the scales of a block's
-// keys and values one more.
+// each on one page; a quarter of K or V is one DMA instruction (two are, at D = 64: an
+// instruction takes the time of its lanes, used or not; drafted tokens, see below, took
+// 25.7 us by quarters), the scales of a block's keys and values one more.
 //
 // Products and layouts, for 64 keys t + 16 q + j of quarters q:
 //   S^T  = K  Q^T    four tiles of 16 keys; tile kt holds the keys 16 q + 4 kt + i, so
@@ -87,15 +88,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     constexpr int TENSOR = KB * ROWB, SLOT = 2 * TENSOR;
     constexpr int NS = RING / SLOT;              // ring slots of a wave
     constexpr int CPK = ROWB / 16;               // 16-byte chunks per key
-    constexpr int QB = 16 * ROWB;                // bytes of a quarter, one DMA instruction
+    constexpr int QB = 16 * ROWB;                // bytes of a quarter
+    constexpr bool TWO = !BIG && QB < 1024;      // a DMA instruction takes two quarters, half of the lanes each
     constexpr int SPK = D / kE2m1Block;          // scales per key
     constexpr int SC = 2 * KB * SPK;             // bytes of a block's scales
-    constexpr int PT = BIG ? TENSOR / 1024 : 4;  // instructions of K or V per block
+    constexpr int PT = TENSOR / 1024;            // DMA instructions of K or V per block
     constexpr int PB = 2 * PT + 1;               // and of a block, its scales with them
     constexpr int KS = D / 32, DT = D / 16;
     constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;  // bfloat16 numbers to a query element or probability
     constexpr int OROW = D + 4;                  // row pitch of the merge buffer, in floats
-    constexpr uint64_t QLANES = BIG || QB == 1024 ? ~0ull : (1ull << (QB / 16)) - 1;
     constexpr uint64_t SLANES = (1ull << (SC / 16)) - 1;
     static_assert(KB == 64 && QB <= 1024 && (NS - 1) * PB < 64, "a block's instructions, and the wait that counts them");
     static_assert(16 * OROW * 4 <= RING, "merge buffer");
@@ -114,9 +115,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     const uint32_t exps = lds_u32(lds) + NW * RING + NW * NS * SC + w * EXPS;
     // byte offset of the lane's chunk in instruction i (of a quarter, or 1 KB: dma_rows): of V the
     // same for all, of K with the bits flipped that the quarter's number permutes
-    constexpr int KPI = QLANES == ~0ull ? 1024 / ROWB : 16;  // keys of an instruction
-    const int ikey = lane / CPK % KPI;
-    const uint32_t koff = (uint32_t)ikey * ROWB + 16 * ((lane % CPK) ^ few4_kswz<D>(ikey));
+    constexpr int KPI = TWO ? 16 : 1024 / ROWB;  // keys of an instruction, on one page
+    const int ikey = lane / CPK % KPI, lkey = lane / CPK;
+    const uint32_t koff = (uint32_t)ikey * ROWB + 16 * ((lane % CPK) ^ few4_kswz<D>(lkey));
     const uint32_t voff = (uint32_t)ikey * ROWB + 16 * ((lane % CPK) ^ few4_vswz<D>(ikey & 15));
     // operand reads, relative to a slot: key 16 (l16 / 4) + l16 % 4 + 4 kt of K, the lane's elements;
     // key 16 lg + l16 of V, eight bytes of tile dt (of which dt / 2 flips bits of the address that
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
             uint32_t koffs[PT], voffs[PT];
 #pragma unroll
             for (int i = 0; i < PT; ++i) {
-                koffs[i] = ko ^ (16 * few4_kswz<D>(KPI * i));
+                koffs[i] = ko ^ (16 * few4_kswz<D>(1024 / ROWB * i));
                 voffs[i] = voff;
             }
             const int at = min(b, mine - 1) % TURN * Q;
@@ -189,11 +190,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
             } else {
                 uint64_t row[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    row[q] = row_of(q);
-                    const uint32_t off[2][1] = {{koffs[q]}, {voff}};
-                    dma_rows(kbase + row[q] * ROWB, off[0], dst + QB * q, real & QLANES);
-                    dma_rows(vbase + row[q] * ROWB, off[1], dst + TENSOR + QB * q, real & QLANES);
+                for (int q = 0; q < 4; ++q) row[q] = row_of(q);
+#pragma unroll
+                for (int i = 0; i < PT; ++i) {
+                    if constexpr (TWO) {
+                        const uint64_t at2 = (lane < 32 ? row[2 * i] : row[2 * i + 1]) * ROWB;
+                        dma_16B_lanes(kbase + at2 + koffs[i], dst + 1024 * i, real);
+                        dma_16B_lanes(vbase + at2 + voffs[i], dst + TENSOR + 1024 * i, real);
+                    } else {
+                        const uint32_t off[2][1] = {{koffs[i]}, {voffs[i]}};
+                        dma_rows(kbase + row[i] * ROWB, off[0], dst + 1024 * i, real);
+                        dma_rows(vbase + row[i] * ROWB, off[1], dst + TENSOR + 1024 * i, real);
+                    }
                 }
                 const uint64_t lo = sq_lane & 1 ? row[1] : row[0], hi = sq_lane & 1 ? row[3] : row[2];
                 dma_16B_lanes(sc_lane + (sq_lane & 2 ? hi : lo) * SPK, sc_ring + (b % NS) * SC, real & SLANES);
@@ -230,6 +238,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
         const int most = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, (row0 + nrows - 1) / a.G));
         if (mine > 0) {
             look_up(0);
+            // the query loads and the DMA complete in no order relative to each other: those first, so
+            // that the first block is waited for alone
+            wait_vmcnt<0>();
 #pragma unroll
             for (int b = 0; b < NS; ++b) issue(b);
         }
@@ -243,9 +254,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        // the query loads and the DMA complete in no order relative to each other
-        wait_vmcnt<0>();
-
         for (int b = 0; b < mine; ++b) {
             wave_wait_vmcnt<(NS - 1) * PB>();  // block b has landed
             const uint32_t slot = ring + (b % NS) * SLOT, scs = sc_ring + (b % NS) * SC;

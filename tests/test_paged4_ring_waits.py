@@ -8,7 +8,23 @@ import re
 
 import pytest
 
-from test_paged_ring_waits import CSRC, few_rows, landed
+from test_paged_ring_waits import CSRC, landed
+
+
+def few_rows(k, mine, slack=0):
+    """Reads of a block that had not landed or was not the slot's, with waits that leave `slack` pieces more; the first
+    block is waited for as the others are, with the ring's blocks under way."""
+    NS, PB = k["NS"], k["PB"]
+    bad, flight, asked = 0, [], {}
+    for b in range(NS if mine else 0):
+        asked[b % NS] = b
+        flight += [b] * PB
+    for b in range(mine):
+        flight = landed(flight, min((NS - 1) * PB + slack, len(flight)))
+        bad += asked[b % NS] != b or b in flight
+        asked[b % NS] = b + NS  # behind the reads of block b
+        flight += [b + NS] * PB
+    return bad
 
 def constant(name, const, **known):
     with open(os.path.join(CSRC, name)) as f:
@@ -24,13 +40,13 @@ def test_few_rows(D, BIG):
     k = {"D": D, "BIG": BIG, "NW": 8, "kUnit": 64, "kE2m1Block": 32}
     for c in ("RING", "ROWB", "KB", "TENSOR", "SLOT", "NS", "CPK", "QB", "SPK", "SC", "PT", "PB", "EXPS"):
         k[c] = constant("kernel_paged_few4.h", c, **k)
-    lanes = 64 if BIG else k["QB"] // 16
-    kpi = 1024 // k["ROWB"] if lanes == 64 else 16
+    lanes, kpi = 64, 1024 // k["ROWB"]
     assert k["NS"] == {64: 4, 128: 2}[D] and k["PB"] == 2 * k["PT"] + 1 and k["PT"] * kpi == 64
     # the instructions make the block, one of SC / 16 lanes its scales
     assert 2 * k["PT"] * 16 * lanes == k["SLOT"] == 64 * 2 * D // 2 and k["SC"] == 64 * 2 * D // 32 and k["SC"] // 16 <= 64
     assert 8 * (k["RING"] + k["NS"] * k["SC"] + k["EXPS"]) <= 160 * 1024 - 8 * 128  # with m_s and l_s
-    # an instruction's lanes cover its rows, each chunk once, where the reads look for it
+    # an instruction's lanes cover its rows, each chunk once, where the reads look for it (at D = 64 over small pages
+    # two quarters of 16 keys, each on its page: here as if they followed each other)
     kswz = lambda key: key >> 4 & (3 if D == 128 else 1)
     vswz = lambda key: key >> 2 & 3 if D == 128 else key >> 3 & 1
     for i in range(k["PT"]):
