@@ -32,8 +32,8 @@
 // the same with the DMA alone, without products and softmax, 35; each further byte moves at
 // 5.7 TB/s, and about 14 us are fixed: the call's start, the parts' starts, the joins of
 // eight waves' states and the finish pass.  2 to 9 drafted tokens of 13 sequences, 32
-// heads of 64 over 8 (35 MB): 26 us, with the DMA alone 19.  The multiplying path alone took
-// 46.3 and 37.5 before exponents were added and parts were priced.
+// heads of 64 over 8 (35 MB): 25 us, with the DMA alone 19.  The multiplying path alone took
+// 46.3 and 37.5 before exponents were added, parts priced and units weighed by their tiles.
 //
 // Up to two tiles of 16 rows at D = 128, three at D = 64 (one and two in float32): one more
 // and the state leaves the registers.  bfloat16 batches of more rows take the kernel
@@ -108,7 +108,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     const int lane = paged_lane(), l16 = lane & 15, lg = lane >> 4;
     PagedRun run;
     PagedPart part;
-    if (!paged_begin(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
+    constexpr bool WEIGHED = NT > 1;  // the pairs' blocks differ in price
+    if (!paged_begin<WEIGHED>(a, paged_worker(a, wg_id()), run, wi_id() == 0)) return;
 
     const float c = a.qscale;
     const uint32_t ring = lds_u32(lds) + w * RING, sc_ring = lds_u32(lds) + NW * RING + w * NS * SC;
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     const int sq_lane = lane / SPK & 3;
     const uint64_t sc_lane = reinterpret_cast<uint64_t>(lane & (4 * SPK) ? a.v_scales : a.k_scales) + 16 * (lane % SPK);
 
-    while (paged_next(a, run, part)) {
+    while (paged_next<WEIGHED>(a, run, part)) {
         if (w == 0 && lane == 0) paged_note(a, run, part);
         const PagedSeq sq = part.seq;
         const int R = sq.n * a.G, row0 = part.group * RT, nrows = min(RT, R - row0);

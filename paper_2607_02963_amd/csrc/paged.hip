@@ -89,9 +89,10 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // whole 22); 400 keys are as well or better whole (14 and 11 us, 36 and 28).
 constexpr int kWholeUnits = 4;
 
-// The division of one launch's work over `workers` work-groups (paged_common.h),
-// and its workspace bytes; false if its unit count passes 32 bits.
-bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int pad, size_t* bytes)
+// The division of one launch's work over `workers` work-groups (paged_common.h: `least`
+// and `pad` in positions, of which a unit is `price` at most), and its workspace bytes;
+// false if its count of positions passes 32 bits.
+bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int pad, int price, size_t* bytes)
 {
     const int64_t R = (int64_t)a.max_chunk * a.G;
     if (R > INT32_MAX / 2) return false;
@@ -99,7 +100,7 @@ bool divide(const pdec_paged_dims* d, PagedArgs& a, int workers, int least, int 
     const int64_t units = (a.max_len + kUnit - 1) / kUnit;
     const int64_t real_groups = (int64_t)d->num_tokens * a.G / a.rows + d->num_seqs;  // at most, over the batch
     // (the number of groups passes 2^50 for sizes that no tensor has: no product with it)
-    if (real_groups > INT32_MAX / 2 / a.H_kv / (units + pad + 1)) return false;
+    if (real_groups > INT32_MAX / 2 / a.H_kv / (units * price + pad + 1)) return false;
     const int64_t pairs = (int64_t)d->num_seqs * a.groups * (a.H_kv / a.heads);
     if (pairs > INT32_MAX / 2) return false;
     a.workers = workers;
@@ -165,7 +166,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         }
         // a work-group per compute unit; a start's price was swept (six chunks of 301 to 1023
         // tokens, 8-bit and bfloat16: 3 526 and 480 us, 6 456 and 418, 9 464 and 421, 14 471 and 424)
-        if (!divide(d, p.many, 256, 4, 6, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
+        if (!divide(d, p.many, 256, 4, 6, 1, &p.many_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     if (p.use_few) {
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
@@ -174,11 +175,14 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         if (f32 && four && d->head_dim == 128) p.few.rows = 16;  // the registers of three terms (kernel_paged_few4.h)
         // heads' rows of a cache line or half of one: two heads to a work-group (kernel_paged_few.h)
         if (!f32 && !four && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;
-        // a start's price, in units; over 4-bit pages, whose units are the shortest, it was swept (4, 8, 16,
-        // 24, 32): 32 tokens over 1200 to 16384 keys, heads of 128, 44.2, 42.7, 40.5, 41.1, 41.3 us; drafted
-        // tokens of 13 sequences, heads of 64, 34.4, 32.3, 27.9, 26.3, 27.7
-        const int pad = four ? (d->head_dim == 128 ? 16 : 24) : f32 ? 1 : 4;
-        if (!divide(d, p.few, f32 && !four ? 512 : 256, 2, pad, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
+        // a start's price, in positions; over 4-bit pages, whose units are the shortest, it was swept.  Units of
+        // one tile (4, 8, 16, 24, 32): 32 tokens over 1200 to 16384 keys, heads of 128, 44.2, 42.7, 40.5, 41.1,
+        // 41.3 us.  Items of more rows, whose units are 3 positions and up (paged_price; 36, 48, 72, 96): 2 to 9
+        // drafted tokens of 13 sequences, heads of 64, -, 25.9, 24.7, 25.7, 1 to 4 of 32 sequences, heads of 128,
+        // 47.7, 47.1, 45.9, - (units alike, at the best price: 25.5, 49.1)
+        const bool weighed = four && p.few.rows > 16;
+        const int pad = weighed ? 72 : four ? (d->head_dim == 128 ? 16 : 24) : f32 ? 1 : 4, price = weighed ? 2 + p.few.rows / 16 : 1;
+        if (!divide(d, p.few, f32 && !four ? 512 : 256, 2 * price, pad, price, &p.few_bytes)) return PDEC_ERR_UNSUPPORTED;
     }
     return PDEC_OK;
 }

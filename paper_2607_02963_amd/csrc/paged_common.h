@@ -50,8 +50,8 @@ struct PagedArgs {
     int rows_from;    // this launch serves the sequences with rows_from <= R <= rows_to
     int rows_to;
     int workers;      // work-groups that share the units, a multiple of 8
-    int least;        // units per work-group, at least
-    int pad;          // price of a pair's start, in units
+    int least;        // positions per work-group, at least
+    int pad;          // price of a pair's start, in positions
     int blocks;       // work-groups of the launch, a multiple of 8
     int whole;        // 1: work-group i takes pair i whole, nothing is cut
     int by_pair;      // 1: cut[] is indexed by pair, 0: by the work-group a pair begins in
@@ -79,11 +79,16 @@ __device__ inline int paged_seen(const PagedArgs& a, const PagedSeq& x, int i)
 
 // A work-group's place in its run.  Positions count every pair's pad and units,
 // the pad first.  Uniform over the work-group.
+//
+// WEIGHED (below): a unit is paged_price positions, and the work-group's that has the first
+// of them.  No work-group between a cut pair's first and last is without a unit of it if
+// `least` is a price or more.
 struct PagedRun {
     int w;          // its number
     int head, s, group;  // the pair at hand: kv head (or `heads` of them), sequence, row group
     PagedSeq seq;
     int u, units;   // next position in it, and its units
+    int price;      // positions of each, if WEIGHED
     int left;       // positions left of the run
     int pos;        // next position in the list of all
     int per, more;  // positions per work-group, the first `more` one more
@@ -95,7 +100,7 @@ struct PagedPart {
     PagedSeq seq;
     bool whole;     // all of the pair
     int slot;       // where its state goes if not
-    int end;        // position behind the pair
+    int last;       // first position of the pair's last unit
 };
 
 __device__ inline int paged_lane() { return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)); }
@@ -108,6 +113,26 @@ __device__ inline int paged_units_of(const PagedArgs& a, const PagedSeq& x, int 
     return max(1, (paged_seen(a, x, last / a.G) + kUnit - 1) / kUnit);
 }
 
+// Positions of a unit.  Weighed, by the row group's tiles of 16 rows: of the kernel that asks
+// for it (kernel_paged_few4.h) a block of one, two and three tiles takes 1.7, 2.3 and 3.1 us.
+template <bool WEIGHED>
+__device__ inline int paged_price(const PagedArgs& a, const PagedSeq& x, int group)
+{
+    if constexpr (WEIGHED) return 2 + (min(max(x.n * a.G - group * a.rows, 1), a.rows) + 15) / 16;
+    return 1;
+}
+
+// Units that begin in front of position x of a pair's units.
+template <bool WEIGHED>
+__device__ inline int paged_begun(int x, int price)
+{
+    if constexpr (WEIGHED) {
+        const uint32_t y = (uint32_t)(max(x, 0) + price - 1);
+        return (int)(price == 3 ? y / 3 : price == 4 ? y / 4 : y / 5);  // up to three tiles
+    }
+    return max(x, 0);
+}
+
 // Units of pair j = sequence * groups + row group (the same for every head);
 // 0 where there are no such rows, at least 1 where there are.
 __device__ inline int paged_units(const PagedArgs& a, int j)
@@ -118,6 +143,7 @@ __device__ inline int paged_units(const PagedArgs& a, int j)
 
 // False if the work-group has nothing to do.  Every wave computes the same; one
 // lane of the work-group (the caller says which) notes for the finish pass what is cut.
+template <bool WEIGHED = false>
 __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool note)
 {
     const int J = a.num_seqs * a.groups, lane = paged_lane(), sets = a.H_kv / a.heads;
@@ -156,7 +182,7 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             if (!by_seq) {
                 const int s = k / a.groups;
                 x = paged_seq(a, s);
-                const int n = paged_units_of(a, x, k - s * a.groups);
+                const int n = paged_units_of(a, x, k - s * a.groups) * paged_price<WEIGHED>(a, x, k - s * a.groups);
                 return n > 0 ? n + a.pad : 0;
             }
             x = paged_seq(a, k);
@@ -164,7 +190,7 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             for (int g = 0; g < a.groups; ++g) {
                 const int u = paged_units_of(a, x, g);
                 if (u == 0) break;
-                n += u + a.pad;
+                n += u * paged_price<WEIGHED>(a, x, g) + a.pad;
             }
             return n;
         };
@@ -202,11 +228,16 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             r.group = j - r.s * a.groups;
             r.u = rest;
             r.units = __builtin_amdgcn_readlane(n, at) - a.pad;
+            if constexpr (WEIGHED) {
+                r.units = paged_units_of(a, r.seq, r.group);
+                r.price = paged_price<WEIGHED>(a, r.seq, r.group);
+            }
             return true;
         }
         r.s = j0 + at;
         for (int g0 = 0; g0 < a.groups; g0 += 64) {  // a lane per group
-            const int u = g0 + lane < a.groups ? paged_units_of(a, r.seq, g0 + lane) : 0, c = u > 0 ? u + a.pad : 0;
+            const int u = g0 + lane < a.groups ? paged_units_of(a, r.seq, g0 + lane) : 0;
+            const int c = u > 0 ? u * paged_price<WEIGHED>(a, r.seq, g0 + lane) + a.pad : 0;
             const int upto = (int)scan(c), all = __builtin_amdgcn_readlane(upto, 63);
             if (rest >= all) {
                 rest -= all;
@@ -216,6 +247,7 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
             r.group = g0 + at;
             r.u = rest - __builtin_amdgcn_readlane(upto - c, at);
             r.units = __builtin_amdgcn_readlane(u, at);
+            if constexpr (WEIGHED) r.price = paged_price<WEIGHED>(a, r.seq, r.group);
             return true;
         }
         return false;
@@ -225,17 +257,19 @@ __device__ inline bool paged_begin(const PagedArgs& a, int w, PagedRun& r, bool 
     r.seq = paged_seq(a, r.s);
     r.units = paged_units_of(a, r.seq, r.group);
     r.left = r.units;
+    if constexpr (WEIGHED) r.left *= r.price = paged_price<WEIGHED>(a, r.seq, r.group);
     return r.units > 0;
 }
 
 // The next part of the run; false at its end.  (All that leaves the loop is scalar
 // and no store is by the lane: one inside the loop would make everything that
 // leaves it a vector value.)
+template <bool WEIGHED = false>
 __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
 {
     const int pad = a.whole ? 0 : a.pad, sets = a.H_kv / a.heads;
     while (r.left > 0) {
-        while (r.u >= r.units + pad || r.units == 0) {  // positions are left, so another pair follows
+        while (r.u >= r.units * (WEIGHED ? r.price : 1) + pad || r.units == 0) {  // positions are left, so another pair follows
             r.u = 0;
             ++r.group;
             if (r.group >= a.groups || (r.units = paged_units_of(a, r.seq, r.group)) == 0) {
@@ -253,21 +287,22 @@ __device__ inline bool paged_next(const PagedArgs& a, PagedRun& r, PagedPart& p)
                     r.s += b ? __builtin_ctzll(b) - 1 : 63;  // the one before it
                 }
             }
+            if constexpr (WEIGHED) r.price = paged_price<WEIGHED>(a, r.seq, r.group);
         }
-        const int take = min(r.left, r.units + pad - r.u);
-        p.u0 = max(r.u - pad, 0);
-        p.u1 = max(r.u + take - pad, 0);
+        const int price = WEIGHED ? r.price : 1, take = min(r.left, r.units * price + pad - r.u);
+        p.u0 = paged_begun<WEIGHED>(r.u - pad, price);
+        p.u1 = paged_begun<WEIGHED>(r.u + take - pad, price);
         p.head = r.head;
         p.s = r.s;
         p.group = r.group;
         p.seq = r.seq;
         p.whole = p.u0 == 0 && p.u1 == r.units;
         p.slot = 2 * r.w + (p.u0 == 0 ? 1 : 0);
-        p.end = r.pos - r.u + r.units + pad;
+        p.last = r.pos - r.u + r.units * price + pad - price;
         r.pos += take;
         r.left -= take;
         r.u += take;
-        if (p.u1 > p.u0) return true;  // else of the pair's price only
+        if (p.u1 > p.u0) return true;  // else of the pair's price, or a unit's, only
     }
     return false;
 }
@@ -278,7 +313,7 @@ __device__ inline void paged_note(const PagedArgs& a, const PagedRun& r, const P
 {
     if (a.whole || p.u0 > 0) return;
     const int j = p.s * a.groups + p.group;
-    const int at = p.end - 1, first = r.more * (r.per + 1);  // the work-group of the pair's last position
+    const int at = p.last, first = r.more * (r.per + 1);  // the work-group of the pair's last unit
     const int last = min(at < first ? at / (r.per + 1) : r.more + (at - first) / r.per, a.workers - 1);
     const int4 cut = make_int4(p.whole ? -1 : r.w, last, j, p.head);
     if (a.by_pair) a.cut[p.head * a.num_seqs * a.groups + j] = cut;
