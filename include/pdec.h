@@ -703,7 +703,8 @@ typedef struct pdec_table_dims {
                         /* the entries of so many keys are looked at                      */
 } pdec_table_dims;
 
-/* Bytes of workspace the two calls need (0 for invalid dims).  Host only. */
+/* Bytes of workspace the two calls need: 0 for up to 64 sequences, which need none
+ * (NULL is taken), and for invalid dims.  Host only. */
 size_t pdec_table_workspace_size(const pdec_table_dims* dims);
 
 /*

@@ -17,7 +17,7 @@
 // What bounds them: the bytes, each read and written once.  8001 float32 tokens, 28 and 4
 // heads of 128 (262 MB) 56 us, 4.7 TB/s of the 5.2 of a large copy (87% of the wave cycles
 // wait); the append of 15236 bfloat16 tokens with their queries (281 MB) 59 us, 4.7 TB/s.
-// With few tokens it is the call on the host: 32 tokens 10.8 us, the kernels 3.6 and 4.5.
+// With few tokens it is the call on the host: 32 tokens 9.5 and 10.6 us, the kernels 3.6 and 4.5.
 #pragma once
 
 #include "kernel_paged_io.h"

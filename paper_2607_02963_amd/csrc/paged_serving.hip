@@ -40,7 +40,11 @@ PagedTableArgs table_args(const pdec_table_dims* d)
     return a;
 }
 
-size_t table_workspace(const pdec_table_dims* d) { return ((size_t)d->num_seqs + 1) / 2 * 2 * sizeof(int2); }
+// One work-group keeps its sequences' counts to itself.
+size_t table_workspace(const pdec_table_dims* d)
+{
+    return d->num_seqs <= kTableOne ? 0 : ((size_t)d->num_seqs + 1) / 2 * 2 * sizeof(int2);
+}
 
 template <bool RESERVE>
 int launch_table(const PagedTableArgs& a, hipStream_t s)
@@ -126,7 +130,7 @@ int pdec_paged_reserve(const pdec_table_dims* d, const int32_t* new_tokens, cons
     if (rc != PDEC_OK) return rc;
     if (!aligned(new_tokens, 4) || !aligned(seq_lens, 4) || !aligned(block_table, 4) || !aligned(free_pages, 4) ||
         !aligned(free_in, 4) || !aligned(free_out, 4) || free_in == free_out || !aligned(cu_tokens, 4) ||
-        (positions && !aligned(positions, 4)) || (slots && !aligned(slots, 8)) || !aligned(workspace, 16))
+        (positions && !aligned(positions, 4)) || (slots && !aligned(slots, 8)) || (table_workspace(d) > 0 && !aligned(workspace, 16)))
         return PDEC_ERR_INVALID_ARG;
     if (workspace_bytes < table_workspace(d)) return PDEC_ERR_WORKSPACE;
     PagedTableArgs a = table_args(d);
@@ -150,7 +154,7 @@ int pdec_paged_release(const pdec_table_dims* d, const int32_t* keep_from, const
     const int rc = check_table_dims(d);
     if (rc != PDEC_OK) return rc;
     if ((keep_from && !aligned(keep_from, 4)) || !aligned(keep_len, 4) || !aligned(block_table, 4) || !aligned(free_pages, 4) ||
-        !aligned(free_in, 4) || !aligned(free_out, 4) || free_in == free_out || !aligned(workspace, 16))
+        !aligned(free_in, 4) || !aligned(free_out, 4) || free_in == free_out || (table_workspace(d) > 0 && !aligned(workspace, 16)))
         return PDEC_ERR_INVALID_ARG;
     if (workspace_bytes < table_workspace(d)) return PDEC_ERR_WORKSPACE;
     PagedTableArgs a = table_args(d);

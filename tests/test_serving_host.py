@@ -26,8 +26,9 @@ def test_bad_table_dims(kw):
 
 
 def test_bad_table_pointers():
-    d, L = ctypes.byref(table_dims()), pdec.lib()
+    d, L = ctypes.byref(table_dims(num_seqs=65)), pdec.lib()
     ws = L.pdec_table_workspace_size(d)
+    assert ws > 0 and L.pdec_table_workspace_size(ctypes.byref(table_dims(num_seqs=64))) == 0  # none needed
     for fn, names in ((L.pdec_paged_reserve, ["new", "lens", "table", "free", "in", "out", "cu", "positions", "slots", "ws"]),
                       (L.pdec_paged_release, ["keep_from", "keep_len", "table", "free", "in", "out", "ws"])):
         for i, name in enumerate(names):
