@@ -1062,10 +1062,12 @@ def _heads(t, name, dev, dtype, shape):
 
 
 def _empty_rows(stream, t):
-    """A contiguous tensor like t (half a microsecond quicker than by its sizes, where t is one)."""
-    if stream is None and t.is_contiguous():
+    """What ``_empty`` allocates for rows like t, which is a microsecond quicker than by sizes.  Rows that the calls
+    take, strided or not, have contiguous ones like them."""
+    if stream is None:
         return torch.empty_like(t)
-    return _empty(stream, t.shape, t.dtype, t.device)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
 
 
 def _check_spec(spec, dev):

@@ -131,6 +131,23 @@ def test_strided_rows_in_place_and_a_table(dtype, spec):
     close(dtype, qt, turned(x[:, :H_q].double().numpy(), pos, spec, f=f))
 
 
+@pytest.mark.parametrize("T,H", [(1, 3), (4, 1), (5, 3)])
+def test_outputs_are_contiguous_whatever_the_rows_strides(T, H):
+    """Of one token or head strides say nothing; rows whose heads do not lie one after another are refused."""
+    spec, pos = pdec.rope_spec(64), i32(range(T))
+    x = rows(2 * T, 2 * H, 64, "f32", 8).cuda()
+    want, _ = pdec.rope(x[:T, :H].contiguous(), None, pos, spec)
+    for q in (x[:T, :H], x[:T].transpose(0, 1)[:H].transpose(0, 1), x.as_strided((T, H, 64), (2 * H * 64, 64, 1))):
+        out, _ = pdec.rope(q, None, pos, spec)
+        assert out.is_contiguous() and torch.equal(bits(out), bits(want))
+        out, _ = pdec.rope(q, None, pos, spec, stream=torch.cuda.current_stream())
+        assert out.is_contiguous() and torch.equal(bits(out), bits(want))
+    if H > 1:
+        for q in (x[::2, ::2][:T, :H], x.permute(1, 0, 2)[:H].contiguous().permute(1, 0, 2)[:T]):
+            with pytest.raises(ValueError, match="one after another"):
+                pdec.rope(q, None, pos, spec)
+
+
 def test_an_output_of_keys_without_keys_is_refused():
     q, pos = rows(2, 3, 64, "f32", 1).cuda(), i32([0, 1])
     with pytest.raises(ValueError, match="k_out"):
