@@ -32,7 +32,7 @@
 // the same with the DMA alone, without products and softmax, 35; each further byte moves at
 // 5.7 TB/s, and about 14 us are fixed: the call's start, the parts' starts, the joins of
 // eight waves' states and the finish pass.  2 to 9 drafted tokens of 13 sequences, 32
-// heads of 64 over 8 (35 MB): 25 us, with the DMA alone 19.  The multiplying path alone took
+// heads of 64 over 8 (35 MB): 24 us, with the DMA alone 19.  The multiplying path alone took
 // 46.3 and 37.5 before exponents were added, parts priced and units weighed by their tiles.
 //
 // Up to two tiles of 16 rows at D = 128, three at D = 64 (one and two in float32): one more
