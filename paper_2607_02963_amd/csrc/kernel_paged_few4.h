@@ -35,9 +35,13 @@
 // heads of 64 over 8 (35 MB): 24 us, with the DMA alone 19.  The multiplying path alone took
 // 46.3 and 37.5 before exponents were added, parts priced and units weighed by their tiles.
 //
-// Up to two tiles of 16 rows at D = 128, three at D = 64 (one and two in float32): one more
-// and the state leaves the registers.  bfloat16 batches of more rows take the kernel
-// for many rows, float32 ones more items of these.
+// Up to three tiles of 16 rows at D = 128, four at D = 64 (one and two in float32): one more
+// and the state leaves the registers.  So many are worked on one (D = 128) or two (D = 64)
+// after the other, keys and values widened anew, with the queries in LDS: 5 tokens of 32
+// sequences, 35 rows of 128, 70.5 us (all tiles at once, spilling, 133; the kernel for many
+// rows 109), 13 of 20 sequences, 52 rows of 64, 47 (60; 66).  With four tiles at D = 128, 64
+// rows of 16 sequences took 32.6 us, of the kernel for many rows 26.6.  bfloat16 batches of
+// more rows take that, float32 ones more items of these.
 #pragma once
 
 #include "kernel_paged_few.h"
@@ -101,7 +105,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     static_assert(KB == 64 && QB <= 1024 && (NS - 1) * PB < 64, "a block's instructions, and the wait that counts them");
     static_assert(16 * OROW * 4 <= RING, "merge buffer");
     constexpr int EXPS = 2 * KB * SPK;           // bytes of a wave's exponents: SPK times KB keys
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + NW * NS * SC + NW * EXPS];
+    // the queries' operands in LDS, a KB for each tile's step of 32 d, read once a block, where the
+    // registers do not hold them beside the state
+    constexpr bool QLDS = TERMS == 1 && NT * D >= 256;
+    constexpr int TURN_T = D == 128 && NT > 2 ? 1 : D == 64 && NT > 3 ? 2 : NT;  // tiles at a time
+    constexpr int QS = QLDS ? NT * KS * 1024 : 0;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NW * RING + NW * NS * SC + NW * EXPS + QS];
     __shared__ float m_s[NW][16], l_s[NW][16];
 
     const int w = __builtin_amdgcn_readfirstlane(wi_id() >> 6);
@@ -129,7 +138,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
     else kread = kkey * ROWB + 16 * ((lg >> 1) ^ few4_kswz<D>(kkey)) + 8 * (lg & 1);
     const uint32_t vread = TENSOR + vkey * ROWB + 16 * few4_vswz<D>(l16);
     const uint32_t ksread = kkey * SPK + (D == 128 ? lg : lg >> 1), vsread = KB * SPK + 16 * lg * SPK;
+    const uint32_t qs = lds_u32(lds) + NW * RING + NW * NS * SC + NW * EXPS;
     typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
+    typedef __attribute__((address_space(3))) u32x4_t lds_u32x4w_t;
     typedef __attribute__((address_space(3))) const u32x2_t lds_u32x2_t;
     typedef __attribute__((address_space(3))) const uint8_t lds_u8_t;
     typedef __attribute__((ext_vector_type(2))) int i32x2_t;
@@ -211,12 +222,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 
         // ---- this lane's rows: 16 nt + l % 16; those past the last see nothing ----
         int seen[NT];
-        u32x4_t qf[NT][KS][TERMS];
+        u32x4_t qf[QLDS ? 1 : NT][KS][TERMS];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = 16 * nt + l16, rr = row0 + min(r, nrows - 1);
             seen[nt] = r < nrows ? paged_seen(a, sq, rr / a.G) : 0;
             const T* q = static_cast<const T*>(a.q) + paged_qrow(a, sq, head, rr) * D + 8 * KS * lg;
+            if constexpr (QLDS) {  // a step to a wave
+                static_assert(NW % KS == 0, "a wave's steps are of one place in the rows");
+                if (nt % (NW / KS) == w / KS) *(lds_u32x4w_t*)(uintptr_t)(qs + 1024 * (nt * KS + w % KS) + 16 * lane) = *reinterpret_cast<const u32x4_t*>(q + 8 * (w % KS));
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 const u32x4_t x = *reinterpret_cast<const u32x4_t*>(q + 8 * i);
@@ -255,6 +271,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
+        if constexpr (QLDS) lds_barrier();  // all steps are there
         for (int b = 0; b < mine; ++b) {
             wave_wait_vmcnt<(NS - 1) * PB>();  // block b has landed
             const uint32_t slot = ring + (b % NS) * SLOT, scs = sc_ring + (b % NS) * SC;
@@ -280,8 +297,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                     for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)(((x >> (8 * i) & 255u) << 7) - (127 << 7));
                 }
                 // the tiles that have rows; a row past the last sees nothing, or its result is not stored
-                auto block = [&](auto count) __attribute__((always_inline)) {
-                    constexpr int N = count;
+                auto block = [&](auto count, auto from) __attribute__((always_inline)) {
+                    constexpr int N = count, F = from;  // tiles F .. F + N - 1
                     // registers: one tile's operands at a time (and where they are there, not: drafted tokens, heads
                     // of 64, 25.0 and 24.3 us, 1 to 8 of 32 sequences 54.9 and 53.3, 9 to 12 of 20 38.4 and 37.7)
                     constexpr bool TIGHT = N > 1 && (D == 128 || TERMS > 1);
@@ -294,6 +311,38 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                     float p[N][16];  // scores, then probabilities, of keys t + 16 lg + j
                     {
                         f32x4_t s[N][4];
+                        if constexpr (QLDS) {
+                            uint32_t x[4][KS];
+                            float ks[4];
+#pragma unroll
+                            for (int kt = 0; kt < 4; ++kt) {
+                                ks[kt] = e2m1_scale(*(lds_u8_t*)(uintptr_t)(scs + ksread + 4 * kt * SPK));
+                                if constexpr (D == 128) {
+                                    const u32x4_t y = *(lds_u32x4_t*)(uintptr_t)(slot + kread + 4 * kt * ROWB);
+#pragma unroll
+                                    for (int i = 0; i < KS; ++i) x[kt][i] = y[i];
+                                } else {
+                                    const u32x2_t y = *(lds_u32x2_t*)(uintptr_t)(slot + kread + 4 * kt * ROWB);
+#pragma unroll
+                                    for (int i = 0; i < KS; ++i) x[kt][i] = y[i];
+                                }
+#pragma unroll
+                                for (int nt = 0; nt < N; ++nt) s[nt][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                            }
+#pragma unroll
+                            for (int i = 0; i < KS; ++i) {
+                                if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+                                u32x4_t qv[N];
+#pragma unroll
+                                for (int nt = 0; nt < N; ++nt) qv[nt] = *(lds_u32x4_t*)(uintptr_t)(qs + 1024 * ((F + nt) * KS + i) + 16 * lane);
+#pragma unroll
+                                for (int kt = 0; kt < 4; ++kt) {
+                                    const bf16x8_t kf = as_bf16x8(e2m1_bf16(x[kt][i], ks[kt]));
+#pragma unroll
+                                    for (int nt = 0; nt < N; ++nt) s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qv[nt]), s[nt][kt]);
+                                }
+                            }
+                        } else
 #pragma unroll
                         for (int kt = 0; kt < 4; ++kt) {
                             if (TIGHT) __builtin_amdgcn_sched_barrier(0);
@@ -316,7 +365,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
                                 for (int nt = 0; nt < N; ++nt)
 #pragma unroll
-                                    for (int e = TERMS - 1; e >= 0; --e) s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[nt][i][e]), s[nt][kt]);
+                                    for (int e = TERMS - 1; e >= 0; --e) s[nt][kt] = mfma_16x16x32(kf, as_bf16x8(qf[F + nt][i][e]), s[nt][kt]);
                             }
                         }
 #pragma unroll
@@ -332,7 +381,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
                     for (int nt = 0; nt < N; ++nt) {
                         if (!full) {
-                            int lim = mine_there ? seen[nt] - t - 16 * lg : 0;
+                            int lim = mine_there ? seen[F + nt] - t - 16 * lg : 0;
                             asm volatile("" : "+v"(lim));  // stays a branch
 #pragma unroll
                             for (int j = 0; j < 16; ++j) p[nt][j] = j >= lim ? kNegInf : p[nt][j];
@@ -340,24 +389,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         float mx = p[nt][0];
 #pragma unroll
                         for (int j = 1; j < 16; ++j) mx = paged_top(mx, p[nt][j]);
-                        if (__any(mx * c > m_ref[nt] + 8.f)) {  // rare after a row's first keys
+                        if (__any(mx * c > m_ref[F + nt] + 8.f)) {  // rare after a row's first keys
                             const float mt = max_over_groups(mx) * c;
-                            const bool up = mt > m_ref[nt] + 8.f;
-                            const float alpha = up ? fast_exp2(m_ref[nt] - mt) : 1.f;
-                            m_ref[nt] = up ? mt : m_ref[nt];
-                            lsum[nt] *= alpha;
+                            const bool up = mt > m_ref[F + nt] + 8.f;
+                            const float alpha = up ? fast_exp2(m_ref[F + nt] - mt) : 1.f;
+                            m_ref[F + nt] = up ? mt : m_ref[F + nt];
+                            lsum[F + nt] *= alpha;
 #pragma unroll
-                            for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= alpha;
+                            for (int dt = 0; dt < DT; ++dt) o[F + nt][dt] *= alpha;
                         }
                         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            p[nt][j] = fast_exp2(fmaf(p[nt][j], c, -m_ref[nt]));  // 0 for a hidden key
+                            p[nt][j] = fast_exp2(fmaf(p[nt][j], c, -m_ref[F + nt]));  // 0 for a hidden key
                             sum[j & 3] += p[nt][j];
                         }
                         // the row sums take P unrounded; the product's operands are bf16, so with bf16
                         // queries P is rounded by half a step (2^-8) of each term, as out is
-                        lsum[nt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                        lsum[F + nt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     }
                     // O += V P of keys 16 lg + 8 h .. + 7, blk's 32 elements
                     auto products = [&](int blk, int h, const u32x4_t (&pf)[N][TERMS], auto fast) __attribute__((always_inline)) {
@@ -370,7 +419,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
 #pragma unroll
                             for (int nt = 0; nt < N; ++nt)
 #pragma unroll
-                                for (int e = TERMS - 1; e >= 0; --e) o[nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt][e]), o[nt][dt]);
+                                for (int e = TERMS - 1; e >= 0; --e) o[F + nt][dt] = mfma_16x16x32(vf, as_bf16x8(pf[nt][e]), o[F + nt][dt]);
                         }
                     };
                     if (full && !odd) {
@@ -445,9 +494,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         }
                     }
                 };
-                if (NT > 2 && tiles > 2) block(std::integral_constant<int, NT>{});
-                else if (NT > 1 && tiles > 1) block(std::integral_constant<int, NT < 2 ? NT : 2>{});
-                else block(std::integral_constant<int, 1>{});
+                typedef std::integral_constant<int, 0> first_t;
+                if constexpr (TURN_T < NT) {  // some tiles after the others, which widen the keys and values again
+                    typedef std::integral_constant<int, TURN_T> turn_t;
+                    block(turn_t{}, first_t{});
+                    if (tiles > TURN_T) block(turn_t{}, turn_t{});
+                    if constexpr (2 * TURN_T < NT)
+                        if (tiles > 2 * TURN_T) block(turn_t{}, std::integral_constant<int, 2 * TURN_T>{});
+                } else if (NT > 2 && tiles > 2) block(std::integral_constant<int, NT>{}, first_t{});
+                else if (NT > 1 && tiles > 1) block(std::integral_constant<int, NT < 2 ? NT : 2>{}, first_t{});
+                else block(std::integral_constant<int, 1>{}, first_t{});
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
             if ((b + NS) % TURN == 0 && b + NS < mine) look_up(b + NS);

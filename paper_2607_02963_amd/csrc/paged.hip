@@ -71,8 +71,8 @@ using namespace pdec;
 int chunk_bound(const pdec_paged_dims* d) { return d->max_chunk > 0 ? std::min(d->max_chunk, d->num_tokens) : d->num_tokens; }
 // Sequences of at most so many rows per kv head are the few-row kernel's: up to two
 // 16-row tiles at D = 128, four at D = 64 (both sides measured: kernel_paged_few.h);
-// three at D = 64 over 4-bit pages, where four tiles' state would leave the registers.
-int few_rows(const pdec_paged_dims* d) { return d->head_dim == 128 ? 32 : d->cache_dtype == PDEC_DTYPE_E2M1 ? 48 : 64; }
+// three at D = 128 over 4-bit pages (kernel_paged_few4.h).
+int few_rows(const pdec_paged_dims* d) { return d->head_dim == 64 ? 64 : d->cache_dtype == PDEC_DTYPE_E2M1 ? 48 : 32; }
 
 struct AttnPlan {
     PagedArgs few{}, many{};
@@ -171,7 +171,7 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
     if (p.use_few) {
         const int64_t most = std::min<int64_t>(R, p.few.rows_to);
         const bool f32 = d->dtype == PDEC_DTYPE_F32, four = d->cache_dtype == PDEC_DTYPE_E2M1;
-        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 || (four && d->head_dim == 128) ? 32 : most <= 48 ? 48 : 64;
+        p.few.rows = most <= 16 ? 16 : most <= 32 || f32 ? 32 : most <= 48 ? 48 : 64;
         if (f32 && four && d->head_dim == 128) p.few.rows = 16;  // the registers of three terms (kernel_paged_few4.h)
         // heads' rows of a cache line or half of one: two heads to a work-group (kernel_paged_few.h)
         if (!f32 && !four && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;

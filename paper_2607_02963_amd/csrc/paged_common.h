@@ -128,7 +128,7 @@ __device__ inline int paged_begun(int x, int price)
 {
     if constexpr (WEIGHED) {
         const uint32_t y = (uint32_t)(max(x, 0) + price - 1);
-        return (int)(price == 3 ? y / 3 : price == 4 ? y / 4 : y / 5);  // up to three tiles
+        return (int)(price == 3 ? y / 3 : price == 4 ? y / 4 : price == 5 ? y / 5 : y / 6);  // up to four tiles
     }
     return max(x, 0);
 }

@@ -39,7 +39,10 @@ void launch_few4(const PagedArgs& a, hipStream_t s)
     if (a.rows == 16) hipLaunchKernelGGL((paged_few4_kernel<D, 1, BIG, T>), grid, block, 0, s, a);
     else if constexpr (D == 64 || sizeof(T) == 2) {
         if (a.rows == 32) hipLaunchKernelGGL((paged_few4_kernel<D, 2, BIG, T>), grid, block, 0, s, a);
-        else if constexpr (D == 64 && sizeof(T) == 2) hipLaunchKernelGGL((paged_few4_kernel<D, 3, BIG, T>), grid, block, 0, s, a);
+        else if constexpr (sizeof(T) == 2) {
+            if (a.rows == 48) hipLaunchKernelGGL((paged_few4_kernel<D, 3, BIG, T>), grid, block, 0, s, a);
+            else if constexpr (D == 64) hipLaunchKernelGGL((paged_few4_kernel<D, 4, BIG, T>), grid, block, 0, s, a);
+        }
     }
 }
 

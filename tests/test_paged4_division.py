@@ -13,7 +13,7 @@ import test_paged_division as plain
 def weighed():
     main = plain.MAIN
     for a, b in (("paged_begin(a, w", "paged_begin<true>(a, w"), ("paged_next(a, run", "paged_next<true>(a, run"),
-                 ("rows = 16 << in(0, 4)", "rows = 16 * in(1, 3)"), ("in(0, 6), in(1, 4)", "in(0, 18), in(5, 12)")):
+                 ("rows = 16 << in(0, 4)", "rows = 16 * in(1, 4)"), ("in(0, 6), in(1, 4)", "in(0, 18), in(6, 12)")):
         assert a in main
         main = main.replace(a, b)
     return main

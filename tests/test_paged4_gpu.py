@@ -98,7 +98,8 @@ def test_hidden_memory_does_not_matter(dtype, D):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("D,H_q,H_kv,n", [(64, 8, 4, 60), (128, 14, 2, 60), (128, 28, 1, 50), (128, 4, 2, 9), (64, 4, 2, 9)])
+@pytest.mark.parametrize("D,H_q,H_kv,n", [(64, 8, 4, 60), (128, 14, 2, 60), (128, 28, 1, 50), (128, 4, 2, 9), (64, 4, 2, 9),
+                                              (128, 10, 2, 9), (64, 14, 2, 9)])
 def test_nan_blocks_of_later_tokens_stay_with_those_that_see_them(dtype, D, H_q, H_kv, n):
     """Blocks of the values of tokens 2 and 5 and of the keys of token 7 are NaN: the tokens before them are as
     without, bit for bit, and those that see a value's block have NaN in its 32 elements only."""
@@ -150,7 +151,8 @@ def test_calls_agree_bit_for_bit_whatever_the_workspace_holds(dtype):
 
 @pytest.mark.parametrize("n,H_q,H_kv,D", [
     (3, 8, 2, 64), (3, 12, 3, 64), (4, 14, 2, 64), (11, 8, 2, 64), (16, 12, 3, 64), (2, 14, 2, 128), (4, 21, 3, 128),
-    (8, 8, 2, 128), (9, 14, 2, 128), (31, 8, 2, 64), (33, 12, 3, 64), (70, 14, 2, 128)])
+    (8, 8, 2, 128), (9, 14, 2, 128), (5, 14, 2, 128), (12, 8, 2, 128), (9, 14, 2, 64), (31, 8, 2, 64), (33, 12, 3, 64),
+    (70, 14, 2, 128)])
 @pytest.mark.parametrize("lens", [[200], [2900], [250, 70, 130], [900, 2900, 70], [100] * 20])
 @pytest.mark.parametrize("page", [16, 32, 128])
 def test_every_form_of_the_kernels(n, H_q, H_kv, D, lens, page):

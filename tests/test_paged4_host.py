@@ -66,7 +66,7 @@ def test_the_binding_refuses_other_shapes_and_types():
         pdec.paged_attn(q, k, k, table, None, None)
 
 
-@pytest.mark.parametrize("D,n,want", [(128, 1, 16), (128, 4, 32), (64, 1, 16), (64, 3, 32), (64, 6, 48)])
+@pytest.mark.parametrize("D,n,want", [(128, 1, 16), (128, 4, 32), (64, 1, 16), (64, 3, 32), (64, 6, 48), (128, 6, 48), (64, 9, 64)])
 def test_the_rows_of_an_item(D, n, want):
     plan = pdec.query_paged_plan(dims(D=D, num_tokens=4 * n, max_chunk=n))
     assert plan["rows_few"] == want and plan["rows_many"] == 0

@@ -44,7 +44,8 @@ def test_few_rows(D, BIG):
     assert k["NS"] == {64: 4, 128: 2}[D] and k["PB"] == 2 * k["PT"] + 1 and k["PT"] * kpi == 64
     # the instructions make the block, one of SC / 16 lanes its scales
     assert 2 * k["PT"] * 16 * lanes == k["SLOT"] == 64 * 2 * D // 2 and k["SC"] == 64 * 2 * D // 32 and k["SC"] // 16 <= 64
-    assert 8 * (k["RING"] + k["NS"] * k["SC"] + k["EXPS"]) <= 160 * 1024 - 8 * 128  # with m_s and l_s
+    # (with the queries of three or four tiles)
+    assert 48 * 2 * 128 + 8 * (k["RING"] + k["NS"] * k["SC"] + k["EXPS"]) <= 160 * 1024 - 8 * 128  # with m_s and l_s
     # an instruction's lanes cover its rows, each chunk once, where the reads look for it (at D = 64 over small pages
     # two quarters of 16 keys, each on its page: here as if they followed each other)
     kswz = lambda key: key >> 4 & (3 if D == 128 else 1)
