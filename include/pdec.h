@@ -643,8 +643,9 @@ int pdec_query_paged_plan(const pdec_paged_dims* dims, pdec_paged_plan* plan);
  * (causal) or t < len (not causal) on pages that are present;
  *   out = sum_t p_t v_t, p_t = exp(scale <q, k_t> - lse), lse the log-sum-exp;
  * a query that sees nothing gets 0 and -inf.  Hidden keys and values, whatever
- * they hold (infinities and NaNs too), do not reach a query's result.  (Nor, in a
- * 4-bit cache, does a NaN value whose probability is below float32's range.)
+ * they hold (infinities and NaNs too), do not reach a query's result.  A NaN value
+ * makes the results of all queries that see it NaN, also where its probability is
+ * below float32's range.
  *   q, out [num_tokens, H_q, D], lse [num_tokens, H_q] float32 or NULL;
  *   workspace >= pdec_paged_workspace_size(dims) bytes, device, 16-byte
  *   aligned, contents ignored.

@@ -253,11 +253,20 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
         // keys that every row sees (rows past the last are masked or not, their results are not stored)
         const int least = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, row0 / a.G));
         const int most = __builtin_amdgcn_readfirstlane(paged_seen(a, sq, (row0 + nrows - 1) / a.G));
+        if (mine > 0) look_up(0);
+        // the query loads and the DMA complete in no order relative to each other: those first, so that the
+        // first block is waited for alone; the compiler sees a use of them here, or it might wait for them,
+        // and so for all of the DMA, in the loop (2 to 8 tokens of 32 sequences, heads of 64, 50.5 and 54 us)
+        wait_vmcnt<0>();
+        if constexpr (!QLDS) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int e = 0; e < TERMS; ++e) asm volatile("" : "+v"(qf[nt][i][e]));
+        }
         if (mine > 0) {
-            look_up(0);
-            // the query loads and the DMA complete in no order relative to each other: those first, so
-            // that the first block is waited for alone
-            wait_vmcnt<0>();
 #pragma unroll
             for (int b = 0; b < NS; ++b) issue(b);
         }
@@ -284,14 +293,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                 const bool mine_there = BIG || (have >> lg & 1);
                 // the values' scales of key t + lane, spread by blocks of d: k where bfloat16 has its exponent
                 bool odd;  // one of them is beyond 2^-63 .. 2^64: its byte's first two bits are alike
-                {
+                constexpr uint32_t FIRST = SPK == 4 ? 0x80808080u : 0x8080u;  // bytes' first bits
+                auto value_scales = [&](uint32_t base) __attribute__((always_inline)) -> uint32_t {  // of key t + lane
                     typedef __attribute__((address_space(3))) const uint16_t lds_u16c_t;
                     typedef __attribute__((address_space(3))) const uint32_t lds_u32c_t;
+                    if constexpr (SPK == 4) return *(lds_u32c_t*)(uintptr_t)(base + KB * SPK + SPK * lane);
+                    else return *(lds_u16c_t*)(uintptr_t)(base + KB * SPK + SPK * lane);
+                };
+                {
                     typedef __attribute__((address_space(3))) uint16_t lds_u16_t;
-                    uint32_t x;
-                    if constexpr (SPK == 4) x = *(lds_u32c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
-                    else x = *(lds_u16c_t*)(uintptr_t)(scs + KB * SPK + SPK * lane);
-                    constexpr uint32_t FIRST = SPK == 4 ? 0x80808080u : 0x8080u;
+                    const uint32_t x = value_scales(scs);
                     odd = __any(((x ^ (x << 1)) & FIRST) != FIRST);
 #pragma unroll
                     for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)(((x >> (8 * i) & 255u) << 7) - (127 << 7));
@@ -459,7 +470,23 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                 products(blk, h, pf, std::true_type{});
                             }
                     } else {
-                        // a hidden value's scale may be NaN: its probability of 0 stays 0
+                        // a hidden value's scale may be NaN: its probability of 0 stays 0.  What sees a NaN value is
+                        // NaN, also where its probability is below float32's range
+                        uint32_t again = scs;
+                        asm volatile("" : "+v"(again));  // else the word read above is kept
+                        const uint32_t x = value_scales(again);
+                        if (__any(((x & x << 1 & x << 2 & x << 3) & FIRST) != 0)) {  // 240 and up
+#pragma unroll
+                            for (int blk = 0; blk < SPK; ++blk) {
+                                const uint64_t nan = __ballot((x >> (8 * blk) & 255u) == 255u && mine_there);  // key t + lane
+                                if (nan == 0) continue;
+#pragma unroll
+                                for (int nt = 0; nt < N; ++nt) {
+                                    const int n = min(max(seen[F + nt] - t, 0), 64);
+                                    if (n > 0 && (nan << (64 - n)) != 0) o[F + nt][2 * blk] = o[F + nt][2 * blk + 1] = f32x4_t(__builtin_nanf(""));
+                                }
+                            }
+                        }
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t vs[2 * SPK];  // the scales of the lane's values 8 h .. 8 h + 7
