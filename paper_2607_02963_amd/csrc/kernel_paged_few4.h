@@ -18,7 +18,9 @@
 // that those multiply the probabilities, once for each block of 32 d, before they are
 // rounded: a power of two takes no bits.  Where every row sees the block and all its scales
 // are of 2^-63 .. 2^64, that is an addition to the exponents of two rounded probabilities at
-// a time, of scales that the wave has spread in LDS as bfloat16 exponents.
+// a time, of scales that the wave has spread in LDS as bfloat16 exponents.  A probability of
+// 0 has no exponent: with the sign bit set in all others the addition is a subtraction of
+// 2^15 less the exponent that stops at 0, which keeps it and clears the bit.
 //
 // float32 queries and probabilities are taken as the sums of three bfloat16 numbers, eight
 // of their 24 bits each: exact, and 4-bit keys and values are exact in bfloat16, so that
@@ -66,6 +68,16 @@ __device__ inline void dma_16B_lanes(uint64_t addr, uint32_t lds_base, uint64_t 
 // x y, 0 if one is 0, whatever the other (v_mul_legacy_f32, which has no builtin; as
 // inline assembly the compiler would not keep it apart from a v_exp_f32 before it).
 __device__ float mul_zero(float x, float y) __asm("llvm.amdgcn.fmul.legacy");
+
+// Two numbers of 15 bits, with bit 15 set in each that is not 0 (which the compiler would do
+// by comparisons, one by one).
+__device__ inline uint32_t mark_not_0(uint32_t x)
+{
+    uint32_t some, y;
+    asm("v_pk_min_u16 %0, %1, %2" : "=v"(some) : "v"(x), "s"(0x00010001u));
+    asm("v_pk_mad_u16 %0, %1, %2, %3" : "=v"(y) : "v"(some), "s"(0x80008000u), "v"(x));
+    return y;
+}
 
 // x as the sum of three bfloat16 numbers of its sign, the first 16 bits of x and of what
 // each leaves; two at a time.
@@ -291,7 +303,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
             if (have && t < most) {
                 const bool full = t + KB <= least && have == (1u << Q) - 1;
                 const bool mine_there = BIG || (have >> lg & 1);
-                // the values' scales of key t + lane, spread by blocks of d: k where bfloat16 has its exponent
+                // the values' scales of key t + lane, spread by blocks of d: 2^15 less k where bfloat16 has its exponent
                 bool odd;  // one of them is beyond 2^-63 .. 2^64: its byte's first two bits are alike
                 constexpr uint32_t FIRST = SPK == 4 ? 0x80808080u : 0x8080u;  // bytes' first bits
                 auto value_scales = [&](uint32_t base) __attribute__((always_inline)) -> uint32_t {  // of key t + lane
@@ -305,7 +317,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                     const uint32_t x = value_scales(scs);
                     odd = __any(((x ^ (x << 1)) & FIRST) != FIRST);
 #pragma unroll
-                    for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)(((x >> (8 * i) & 255u) << 7) - (127 << 7));
+                    for (int i = 0; i < SPK; ++i) *(lds_u16_t*)(uintptr_t)(exps + 2 * KB * i + 2 * lane) = (uint16_t)(0x8000u + (127 << 7) - ((x >> (8 * i) & 255u) << 7));
                 }
                 // the tiles that have rows; a row past the last sees nothing, or its result is not stored
                 auto block = [&](auto count, auto from) __attribute__((always_inline)) {
@@ -434,11 +446,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         }
                     };
                     if (full && !odd) {
-                        // P times 2^k: k added to its exponent.  A P of 0 may become 2^-127 times the scale,
-                        // 2^-63 at most (of a larger scale that would be seen beside values of about one).  A
-                        // product below 2^-126 is 0: 2^-55 of a row's largest P, 2^-8 at least, by the scale
-                        typedef __attribute__((ext_vector_type(2))) int16_t i16x2_t;
-                        i16x2_t pe[N][8][TERMS];
+                        // P times 2^k: k added to its exponent, of what is not 0.  A product below 2^-126 comes out
+                        // smaller, or 0; a float32 P's term below 2^-126 larger, by 2^-127 of a P at most
+                        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+                        u16x2_t pe[N][8][TERMS];
 #pragma unroll
                         for (int nt = 0; nt < N; ++nt)
 #pragma unroll
@@ -447,7 +458,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                 if constexpr (TERMS == 1) y[0] = pack_bf16x2(p[nt][2 * j], p[nt][2 * j + 1]);
                                 else three_bf16(p[nt][2 * j], p[nt][2 * j + 1], y);
 #pragma unroll
-                                for (int e = 0; e < TERMS; ++e) pe[nt][j][e] = __builtin_bit_cast(i16x2_t, y[e]);
+                                for (int e = 0; e < TERMS; ++e) pe[nt][j][e] = __builtin_bit_cast(u16x2_t, mark_not_0(y[e]));
                             }
 #pragma unroll
                         for (int blk = 0; blk < SPK; ++blk)
@@ -463,8 +474,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                     for (int nt = 0; nt < N; ++nt)
 #pragma unroll
                                         for (int i = 0; i < TERMS; ++i) {
-                                            const i16x2_t x = __builtin_elementwise_add_sat(pe[nt][4 * h + j][i], __builtin_bit_cast(i16x2_t, ej));
-                                            pf[nt][i][j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, (i16x2_t)0));
+                                            pf[nt][i][j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(pe[nt][4 * h + j][i], __builtin_bit_cast(u16x2_t, ej)));
                                         }
                                 }
                                 products(blk, h, pf, std::true_type{});

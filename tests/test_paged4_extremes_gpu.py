@@ -1,5 +1,5 @@
-"""Attention over 4-bit paged caches at the ends of the number range, against the definition in 64 bits: NaN values
-under probabilities below float32's range."""
+"""Attention over 4-bit paged caches at the ends of the number range, against the definition in 64 bits: NaN values,
+and large ones, under probabilities below float32's range."""
 import numpy as np
 import pytest
 import torch
@@ -51,3 +51,24 @@ def test_a_nan_value_reaches_the_rows_that_see_it_whatever_its_probability(dtype
     for s, heads in ((0, slice(4, 8)), (0, slice(0, 4)), (1, slice(0, 4))):
         want[s * n:s * n + n, heads, 32:64] = True
     assert np.array_equal(np.isnan(o3.float().cpu().numpy()), want) and torch.equal(l1, l3)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 3, 6, 40])
+@pytest.mark.parametrize("D,page", [(128, 32), (64, 64)])
+@pytest.mark.parametrize("small,large", [(-60, 60), (-60, 0), (0, 60), (None, 60)])
+def test_a_probability_of_0_adds_nothing(dtype, n, D, page, small, large):
+    """Values of 2^small (None: 0), and of 2^large in keys whose probability, some e^-136, is below float32's range:
+    their part of a result, 2^large e^-136, is 2^-136 and less."""
+    c = Paged4([n, n], [700, 333], 8, 2, D, page, dtype, seed=33)
+    where = [(0, 5), (0, 100), (0, 101), (0, 640), (1, 0), (1, 200)]
+    far_keys(c, where)
+    v = np.random.default_rng(5).standard_normal(c.vals["v"].shape)
+    far = [(c.table[s, t // page], t % page) for s, t in where]
+    big = [v[at] * 2.0 ** large for at in far]
+    v *= 0.0 if small is None else 2.0 ** small
+    for at, x in zip(far, big):
+        v[at] = x
+    c.set("v", *quantise4(v))
+    out, lse = c.attn()
+    compare(dtype, out, lse, c.reference(), f"{dtype} {small} {large}")
