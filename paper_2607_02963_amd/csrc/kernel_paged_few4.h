@@ -432,13 +432,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                         lsum[F + nt] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     }
                     // O += V P of keys 16 lg + 8 h .. + 7, blk's 32 elements
-                    auto products = [&](int blk, int h, const u32x4_t (&pf)[N][TERMS], auto fast) __attribute__((always_inline)) {
+                    auto products = [&](int blk, int h, const u32x4_t (&pf)[N][TERMS], float scale, auto fast) __attribute__((always_inline)) {
 #pragma unroll
                         for (int dt = 2 * blk; dt < 2 * blk + 2; ++dt) {
                             if (TIGHT) vraw[dt] = read_v(dt);
                             uint32_t x = (uint32_t)(h ? vraw[dt].y : vraw[dt].x);
                             if (!fast) asm volatile("" : "+v"(x));  // else both paths' widening comes before the branch
-                            const bf16x8_t vf = as_bf16x8(e2m1_bf16(x, 1.f));
+                            const bf16x8_t vf = as_bf16x8(e2m1_bf16(x, scale));
 #pragma unroll
                             for (int nt = 0; nt < N; ++nt)
 #pragma unroll
@@ -477,15 +477,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                             pf[nt][i][j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(pe[nt][4 * h + j][i], __builtin_bit_cast(u16x2_t, ej)));
                                         }
                                 }
-                                products(blk, h, pf, std::true_type{});
+                                products(blk, h, pf, 1.f, std::true_type{});
                             }
                     } else {
-                        // a hidden value's scale may be NaN: its probability of 0 stays 0.  What sees a NaN value is
-                        // NaN, also where its probability is below float32's range
+                        // P is 2^8 at most, and a scale 2^-127 .. 2^127.  So that their product is a normal number, a block
+                        // with a scale of 2^113 and up takes P times 2^(k-8), one with a scale below 2^-95 and none beyond
+                        // 2^32 P times 2^(k+64), and the values are widened times the rest.
+                        // A hidden value's P is 0 and stays 0.  What sees a NaN value is NaN, whatever its P
                         uint32_t again = scs;
                         asm volatile("" : "+v"(again));  // else the word read above is kept
                         const uint32_t x = value_scales(again);
-                        if (__any(((x & x << 1 & x << 2 & x << 3) & FIRST) != 0)) {  // 240 and up
+                        const bool huge = __any((x & x << 1 & x << 2 & x << 3 & FIRST) != 0);
+                        const bool tiny = __any((~(x | x << 1 | x << 2) & FIRST) != 0) && !__any((x & (x << 1 | x << 2) & FIRST) != 0);
+                        const int shift = huge ? -8 : tiny ? 64 : 0;
+                        const float up = __uint_as_float((uint32_t)(127 - shift) << 23);
+                        auto scale_of = [&](uint32_t word, int i) __attribute__((always_inline)) {
+                            return __int_as_float(max(__float_as_int(paged_scale(word, i)) + shift * (1 << 23), 0));
+                        };
+                        if (huge) {
 #pragma unroll
                             for (int blk = 0; blk < SPK; ++blk) {
                                 const uint64_t nan = __ballot((x >> (8 * blk) & 255u) == 255u && mine_there);  // key t + lane
@@ -512,8 +521,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                 u32x4_t pf[N][TERMS];
 #pragma unroll
                                 for (int j = 0; j < 8; j += 2) {
-                                    const float s0 = SPK == 4 ? paged_scale(vs[j], blk) : paged_scale(vs[j / 2], blk);
-                                    const float s1 = SPK == 4 ? paged_scale(vs[j + 1], blk) : paged_scale(vs[j / 2], 2 + blk);
+                                    const float s0 = SPK == 4 ? scale_of(vs[j], blk) : scale_of(vs[j / 2], blk);
+                                    const float s1 = SPK == 4 ? scale_of(vs[j + 1], blk) : scale_of(vs[j / 2], 2 + blk);
 #pragma unroll
                                     for (int nt = 0; nt < N; ++nt) {
                                         const float x0 = mul_zero(p[nt][8 * h + j], s0), x1 = mul_zero(p[nt][8 * h + j + 1], s1);
@@ -526,7 +535,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                         }
                                     }
                                 }
-                                products(blk, h, pf, std::false_type{});
+                                products(blk, h, pf, up, std::false_type{});
                             }
                         }
                     }
