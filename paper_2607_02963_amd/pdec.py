@@ -948,7 +948,8 @@ def _table_dims(table, num_tokens, page_size, num_pages, max_len):
 
 
 def _table_args(block_table, free_pages, free_in, free_out, num_tokens, page_size, max_len, dev, workspace, stream):
-    """(dims, addresses of the table, the list and its two counts, address and bytes of the workspace)."""
+    """(dims, addresses of the table, the list and its two counts, the workspace or None).  The caller holds the
+    workspace until its call is enqueued: memory allocated meanwhile must not be the same."""
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be a [num_seqs, max_pages] tensor")
     if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
@@ -957,9 +958,13 @@ def _table_args(block_table, free_pages, free_in, free_out, num_tokens, page_siz
     dims, size = _table_dims(table, int(num_tokens), int(page_size), free_pages.shape[0], int(max_len or 0))
     if workspace is None and size > 0:
         workspace = _empty(stream, size, torch.uint8, block_table.device)
-    ws = (None, 0) if workspace is None else (_ptr(workspace, "workspace", dev, workspace.dtype, workspace.shape), workspace.nbytes)
     return dims, (_ptr(block_table, "block_table", dev, i32, table), _ptr(free_pages, "free_pages", dev, i32, free_pages.shape),
-                  _ptr(free_in, "free_in", dev, i32, (1,)), _ptr(free_out, "free_out", dev, i32, (1,))), ws
+                  _ptr(free_in, "free_in", dev, i32, (1,)), _ptr(free_out, "free_out", dev, i32, (1,))), workspace
+
+
+def _table_workspace(workspace, dev):
+    """Address and bytes."""
+    return (None, 0) if workspace is None else (_ptr(workspace, "workspace", dev, workspace.dtype, workspace.shape), workspace.nbytes)
 
 
 def table_workspace_size(num_seqs: int) -> int:
@@ -983,8 +988,8 @@ def paged_reserve(new_tokens, seq_lens, block_table, free_pages, free_in, free_o
         if given is None:
             raise ValueError("num_tokens is required without positions and slots")
         num_tokens = given.shape[0]
-    dims, (table, free, n_in, n_out), ws = _table_args(block_table, free_pages, free_in, free_out, num_tokens, page_size,
-                                                       max_len, dev, workspace, stream)
+    dims, (table, free, n_in, n_out), workspace = _table_args(block_table, free_pages, free_in, free_out, num_tokens,
+                                                              page_size, max_len, dev, workspace, stream)
     S, T, i32 = dims.num_seqs, dims.num_tokens, torch.int32
     if cu_tokens is None:
         cu_tokens = _empty(stream, (S + 1,), i32, block_table.device)
@@ -993,7 +998,7 @@ def paged_reserve(new_tokens, seq_lens, block_table, free_pages, free_in, free_o
         n_out, _ptr(cu_tokens, "cu_tokens", dev, i32, (S + 1,)),
         None if positions is None else _ptr(positions, "positions", dev, i32, (T,)),
         None if slots is None else _ptr(slots, "slots", dev, torch.int64, (T,)),
-        *ws, _raw_stream(dev) if stream is None else stream.cuda_stream)
+        *_table_workspace(workspace, dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
     if rc != PDEC_OK:
         raise PdecError("pdec_paged_reserve", rc)
     return cu_tokens
@@ -1004,13 +1009,13 @@ def paged_release(keep_len, block_table, free_pages, free_in, free_out, *, page_
     """Pages that hold none of the keys keep_from .. keep_len - 1 of their sequence back to the pool
     (``pdec_paged_release``): keep_len, keep_from int32 [S], the others as for ``paged_reserve``."""
     dev, _ = _device_of(keep_len, "keep_len", rows=False)
-    dims, (table, free, n_in, n_out), ws = _table_args(block_table, free_pages, free_in, free_out, 1, page_size, max_len,
-                                                       dev, workspace, stream)
+    dims, (table, free, n_in, n_out), workspace = _table_args(block_table, free_pages, free_in, free_out, 1, page_size,
+                                                              max_len, dev, workspace, stream)
     S, i32 = dims.num_seqs, torch.int32
     rc = lib().pdec_paged_release(
         dims, None if keep_from is None else _ptr(keep_from, "keep_from", dev, i32, (S,)),
         _ptr(keep_len, "keep_len", dev, i32, (S,)), table, free, n_in, n_out,
-        *ws, _raw_stream(dev) if stream is None else stream.cuda_stream)
+        *_table_workspace(workspace, dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
     if rc != PDEC_OK:
         raise PdecError("pdec_paged_release", rc)
 
