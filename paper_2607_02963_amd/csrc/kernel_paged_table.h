@@ -10,7 +10,8 @@
 // sums the counts of all sequences before them (2048 at a time, eight to a lane: the counts
 // are a few KB, and summing them cheaper than a pass of its own), and then each wave deals a
 // sequence's pages, each lane a token's position and row.  A batch of up to 64 sequences
-// is one work-group's, in one launch.
+// is one work-group's, in one launch.  Of many sequences a pass between the two sums each
+// 2048, and a work-group sums those sums and one 2048.
 //
 // What bounds it: the chain of memory round trips: lengths, entries, the sums, the free
 // list, the entries again.  32 sequences a token each: 5.8 us on the device, 7.6 as a call.
@@ -35,10 +36,12 @@ struct PagedTableArgs {
     int32_t* positions;    // may be null
     int64_t* slots;        // may be null
     int2* counts;          // [S, even] pages and tokens, of the first pass; releasing, from the last sequence
+    ulonglong2* totals;    // [S / kTableChunk] theirs of kTableChunk sequences each, if asked for
     int num_seqs, num_tokens, page_shift, num_pages, max_pages, max_len;
 };
 
 constexpr int kTableOne = 64;  // sequences that one work-group takes alone
+constexpr int kTableChunk = 2048;  // sequences whose counts a work-group sums at a time
 
 __device__ inline bool table_there(const PagedTableArgs& a, int entry) { return (uint32_t)entry < (uint32_t)a.num_pages; }
 
@@ -309,12 +312,38 @@ __global__ __launch_bounds__(64 * kTableWaves) void paged_table_one_kernel(Paged
     }
 }
 
-// More sequences: four to a work-group, the counts of the first pass summed up to them.
-template <bool RESERVE>
+// A work-group sums the counts of kTableChunk sequences.
+__global__ __launch_bounds__(256) void paged_table_totals_kernel(PagedTableArgs a)
+{
+    constexpr int WAVES = 4, PER = kTableChunk / 256;
+    __shared__ TableSum wave_s[WAVES];
+    const int first = blockIdx.x * kTableChunk + PER * (int)threadIdx.x;
+    TableSum x = {0, 0};
+#pragma unroll
+    for (int j = 0; j < PER; j += 2) {
+        if (first + j >= a.num_seqs) break;
+        const int4 n = *reinterpret_cast<const int4*>(a.counts + first + j);
+        x = x + TableSum{(uint32_t)n.x, (uint32_t)n.y};
+        if (first + j + 1 < a.num_seqs) x = x + TableSum{(uint32_t)n.z, (uint32_t)n.w};
+    }
+    x = table_scan(x);
+    if (paged_lane() == 63) wave_s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    x = wave_s[0];
+    for (int i = 1; i < WAVES; ++i) x = x + wave_s[i];
+    a.totals[blockIdx.x] = make_ulonglong2(x.p, x.t);
+}
+
+// More sequences: four to a work-group, the counts of the first pass summed up to them, whole
+// chunks by their totals.
+template <bool RESERVE, bool TOTALS>
 __global__ __launch_bounds__(256) void paged_table_kernel(PagedTableArgs a)
 {
     constexpr int WAVES = 4, PER = 8, CHUNK = 64 * WAVES * PER;
+    static_assert(CHUNK == kTableChunk && CHUNK % WAVES == 0, "a work-group's sequences are of one chunk");
     __shared__ TableSum wave_s[WAVES];
+    __shared__ int fit_s;
     __shared__ unsigned long long most_s[2];  // pages and tokens of the sequences that are served
     __shared__ int from_s[WAVES], need_s[WAVES], token_s[WAVES], len_s[WAVES];  // from -1: not served
     constexpr int LOOK = 64 * kTableLook<RESERVE>;
@@ -337,7 +366,42 @@ __global__ __launch_bounds__(256) void paged_table_kernel(PagedTableArgs a)
     if (tid < 2) most_s[tid] = 0;
 
     TableSum sum = {0, 0};  // of the chunks before
-    for (int c0 = 0; c0 < s1; c0 += CHUNK) {
+    int chunk = 0, last_chunk = s0 / CHUNK;
+    if constexpr (TOTALS) {
+        // whole chunks that are served, in front of the group's; the first that is not is the last to look at
+        if (tid == 0) fit_s = 0;
+        __syncthreads();
+        for (int i0 = 0; i0 < last_chunk; i0 += 256) {
+            const int i = i0 + tid;
+            const ulonglong2 n = i < last_chunk ? a.totals[i] : make_ulonglong2(0, 0);
+            const TableSum y = table_scan(TableSum{n.x, n.y});
+            if (lane == 63) wave_s[w] = y;
+            __syncthreads();
+            TableSum in = sum + y;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) {
+                if (k < w) in = in + wave_s[k];
+                sum = sum + wave_s[k];
+            }
+            const bool fits = i < last_chunk && (!RESERVE || (in.p <= (uint64_t)top && in.t <= (uint64_t)a.num_tokens));
+            const int n_fit = __builtin_popcountll(__ballot(fits));
+            if (fits && lane == n_fit - 1) {  // the sums grow, so the wave's first n_fit
+                atomicMax(&most_s[0], (unsigned long long)in.p);
+                atomicMax(&most_s[1], (unsigned long long)in.t);
+                atomicAdd(&fit_s, n_fit);
+            }
+            __syncthreads();
+        }
+        chunk = fit_s;
+        sum = TableSum{most_s[0], most_s[1]};
+        if (chunk < last_chunk) {
+            if (tid < WAVES) from_s[tid] = -1;
+            last_chunk = chunk;
+        }
+        __syncthreads();
+    }
+    for (; chunk <= last_chunk; ++chunk) {
+        const int c0 = chunk * CHUNK;
         int4 n[PER / 2];
 #pragma unroll
         for (int j = 0; j < PER / 2; ++j) {
