@@ -243,8 +243,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedIoArgs a)
     }
 }
 
-// A wave takes N consecutive rows of one tensor.  grid (rows / (4 N), 2).
-template <int D, typename T, PagedForm FORM, int N>
+// A wave takes N consecutive rows of one tensor.  grid (rows / (4 N), 2).  ONCE: past the caches
+// (a template's, as of a branch's two stores the compiler makes one ordinary one).
+template <int D, typename T, PagedForm FORM, int N, bool ONCE>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -298,9 +299,7 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedIoArgs a)
                 }
                 row[i].set(v);
             }
-            // a 4-bit cache's rows are four times its bytes: kept in the caches, 30700 of 4 heads of 128
-            // (with 7600 appended before) took 25.5 us, past them 21.4
-            if constexpr (FORM == kE2m1Rows) row[i].store_once(out + (long)i * elems + e);
+            if constexpr (ONCE) row[i].store_once(out + (long)i * elems + e);
             else row[i].store(out + (long)i * elems + e);
         }
     }

@@ -193,6 +193,11 @@ size_t workspace_of(const AttnPlan& p) { return std::max<size_t>(align256(p.few_
 // Tokens from which a wave of the append takes four: 16384 tokens of 4 heads of 128 took
 // 15.3 us by one and take 12.0; up to 4096 both take the call's own 8.9.
 constexpr int kAppendMany = 2048;
+// Dense bytes from which the rows of a 4-bit cache, four times its own bytes, pass the caches by.  Rows of
+// 4 heads of 128 by themselves, kept and past them: 20000 (41 MB) 10.6 and 10.0 us, 30000 14.2 and 13.4, 60000
+// 28.8 and 24.5 (30700 with 7600 appended before 25.5 and 21.4); with readers of both tensors behind: 16000 21
+// and 23, 20000 26.2 and 27.8, 30000 37.5 and 37.9, 60000 70.4 and 67.8; up to 12000 alike.
+constexpr int64_t kReadOnce = 48 << 20;
 constexpr int kReadRows = 4;  // rows per wave of the read-back (32768 rows: 24.2 us, by 8 26.8, by 16 25.7)
 
 template <int D, typename T, PagedForm FORM, int N>
@@ -206,7 +211,14 @@ template <int D, typename T, PagedForm FORM>
 void launch_read(const PagedIoArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.num_tokens + 4 * kReadRows - 1) / (4 * kReadRows)), 2);
-    hipLaunchKernelGGL((paged_read_kernel<D, T, FORM, kReadRows>), grid, dim3(256), 0, s, a);
+    const int64_t bytes = 2 * (int64_t)a.num_tokens * a.H_kv * D * (int64_t)sizeof(T);
+    if constexpr (FORM == kE2m1Rows) {
+        if (bytes > kReadOnce) {
+            hipLaunchKernelGGL((paged_read_kernel<D, T, FORM, kReadRows, true>), grid, dim3(256), 0, s, a);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((paged_read_kernel<D, T, FORM, kReadRows, false>), grid, dim3(256), 0, s, a);
 }
 
 }  // namespace
