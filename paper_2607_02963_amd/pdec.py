@@ -1026,12 +1026,13 @@ def rope_spec(head_dim, *, rotary_dim=None, interleaved=False, theta=10000.0, sc
               slow_turns=1.0, fast_turns=32.0, magnitude=1.0, freqs=None) -> RopeSpec:
     """A rotation (``pdec_rope_spec``), kept for the calls that use it.
 
-    ``scaling``: "none", "linear", "ntk" or "by_parts" (the last with ``original_len``).  ``freqs``, a float64
-    [rotary_dim / 2] tensor on the device, is taken in place of theta's powers; the spec keeps it.
+    ``rotary_dim``: the elements of a head that turn, all without it or with 0.  ``scaling``: "none", "linear", "ntk" or
+    "by_parts" (the last with ``original_len``).  ``freqs``, a float64 [rotary_dim / 2] tensor on the device, is taken in
+    place of theta's powers; the spec keeps it.  ``magnitude``: 0 means 1.
     """
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"unknown scaling {scaling!r}")
-    R = int(head_dim if rotary_dim is None else rotary_dim)
+    R = int(rotary_dim or head_dim)
     spec = RopeSpec(int(head_dim), R, int(bool(interleaved)), ROPE_SCALINGS[scaling], float(theta), float(factor),
                     float(original_len), float(slow_turns), float(fast_turns), float(magnitude), None)
     if freqs is not None:
