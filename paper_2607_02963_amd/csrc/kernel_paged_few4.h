@@ -480,24 +480,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                 products(blk, h, pf, 1.f, std::true_type{});
                             }
                     } else {
-                        // P is 2^8 at most, and a scale 2^-127 .. 2^127.  So that their product is a normal number, a block
-                        // with a scale of 2^113 and up takes P times 2^(k-8), one with a scale below 2^-95 and none beyond
-                        // 2^32 P times 2^(k+64), and the values are widened times the rest.
-                        // A hidden value's P is 0 and stays 0.  What sees a NaN value is NaN, whatever its P
+                        // P times the scale, of a hidden value 0 whatever its scale.  P is 2^8 at most, and a scale 2^-127 ..
+                        // 2^127: a product of 2^128 and up, whose value is 0 or its sum beyond float32's range, becomes the
+                        // largest number; and where the row sees a scale below 2^-95 and none beyond 2^32, P is multiplied
+                        // by 2^64 more, and the values are widened times 2^-64.  What sees a NaN value is NaN, whatever its P
                         uint32_t again = scs;
                         asm volatile("" : "+v"(again));  // else the word read above is kept
-                        const uint32_t x = value_scales(again);
-                        const bool huge = __any((x & x << 1 & x << 2 & x << 3 & FIRST) != 0);
+                        const uint32_t x = mine_there && t + lane < most ? value_scales(again) : 0x7f7f7f7fu;  // of what a row sees
                         const bool tiny = __any((~(x | x << 1 | x << 2) & FIRST) != 0) && !__any((x & (x << 1 | x << 2) & FIRST) != 0);
-                        const int shift = huge ? -8 : tiny ? 64 : 0;
-                        const float up = __uint_as_float((uint32_t)(127 - shift) << 23);
-                        auto scale_of = [&](uint32_t word, int i) __attribute__((always_inline)) {
-                            return __int_as_float(max(__float_as_int(paged_scale(word, i)) + shift * (1 << 23), 0));
+                        const float up = tiny ? 0x1p-64f : 1.f;
+                        const uint32_t shift = tiny ? 64u << 23 : 0;
+                        auto scaled = [&](float prob, uint32_t word, int i) __attribute__((always_inline)) {
+                            const float y = mul_zero(prob, __uint_as_float(__float_as_uint(paged_scale(word, i)) + shift));
+                            return fminf(y, TERMS == 1 ? 0x1.fep127f : 0x1.fffffep127f);
                         };
-                        if (huge) {
+                        if (__any((x & x << 1 & x << 2 & x << 3 & FIRST) != 0)) {  // 240 and up
 #pragma unroll
                             for (int blk = 0; blk < SPK; ++blk) {
-                                const uint64_t nan = __ballot((x >> (8 * blk) & 255u) == 255u && mine_there);  // key t + lane
+                                const uint64_t nan = __ballot((x >> (8 * blk) & 255u) == 255u);  // key t + lane
                                 if (nan == 0) continue;
 #pragma unroll
                                 for (int nt = 0; nt < N; ++nt) {
@@ -521,11 +521,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few4_kernel(PagedArgs a)
                                 u32x4_t pf[N][TERMS];
 #pragma unroll
                                 for (int j = 0; j < 8; j += 2) {
-                                    const float s0 = SPK == 4 ? scale_of(vs[j], blk) : scale_of(vs[j / 2], blk);
-                                    const float s1 = SPK == 4 ? scale_of(vs[j + 1], blk) : scale_of(vs[j / 2], 2 + blk);
 #pragma unroll
                                     for (int nt = 0; nt < N; ++nt) {
-                                        const float x0 = mul_zero(p[nt][8 * h + j], s0), x1 = mul_zero(p[nt][8 * h + j + 1], s1);
+                                        const float x0 = scaled(p[nt][8 * h + j], SPK == 4 ? vs[j] : vs[j / 2], blk);
+                                        const float x1 = scaled(p[nt][8 * h + j + 1], SPK == 4 ? vs[j + 1] : vs[j / 2], SPK == 4 ? blk : 2 + blk);
                                         if constexpr (TERMS == 1) pf[nt][0][j >> 1] = pack_bf16x2(x0, x1);
                                         else {
                                             uint32_t y[3];

@@ -145,3 +145,43 @@ def test_values_near_the_ends_of_the_range(dtype, n, D, page, size):
     c.set("v", *quantise4(v))
     out, lse = c.attn()
     compare(dtype, out, lse, c.reference(), f"{dtype} {size}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 6, 40])
+@pytest.mark.parametrize("D,page", [(128, 32), (64, 64), (64, 16)])
+@pytest.mark.parametrize("size", [-110, -90, 0, 100])
+def test_hidden_codes_and_scales_of_every_size_do_not_matter(dtype, n, D, page, size):
+    """Free pages and rows behind a sequence's end hold any codes under any scales, or zeros: the same bits."""
+    got = []
+    for junk in (False, True):
+        c = Paged4([n, n], [700, 333], 8, 2, D, page, dtype, seed=38, junk=True)
+        dead = {x: c.scales[x] == 255 for x in "kv"}  # as junk has them
+        v = np.random.default_rng(9).standard_normal(c.vals["v"].shape) * 2.0 ** size
+        c.set("v", *quantise4(v))
+        rng = np.random.default_rng(10)
+        for x in "kv":
+            d = np.repeat(dead[x], 16, -1)
+            c.scales[x][dead[x]] = rng.choice([0, 1, 20, 127, 180, 245, 250, 254, 255], dead[x].sum()) if junk else 127
+            c.raw[x][d] = rng.integers(0, 256, d.sum()) if junk else 0
+        got.append(c.attn())
+    assert torch.isfinite(got[0][0].float()).all() and got[0][0].any()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 6, 40])
+@pytest.mark.parametrize("D,page", [(128, 32), (64, 64)])
+def test_small_values_beside_zeros_under_large_scales(dtype, n, D, page):
+    """Values of 2^-100 in all blocks of 32 but the second, zeros under scales of 2^118 to 2^127 there: every element to
+    its own precision."""
+    c = Paged4([n, n], [700, 333], 8, 2, D, page, dtype, seed=39)
+    v = np.random.default_rng(11).standard_normal(c.vals["v"].shape) * 2.0 ** -100
+    v[..., 32:64] = 0
+    code, byte = quantise4(v)
+    byte[..., 1] = np.random.default_rng(12).integers(245, 255, byte[..., 1].shape)
+    c.set("v", code, byte)
+    out, lse = c.attn()
+    assert not out[..., 32:64].any()
+    compare(dtype, out, lse, c.reference(), dtype)
