@@ -730,8 +730,10 @@ size_t pdec_table_workspace_size(const pdec_table_dims* dims);
  * Positions and slots behind the last token are left as they were.  All arrays are
  * int32 in device memory but slots; workspace: >= pdec_table_workspace_size(dims)
  * bytes, device, 16-byte aligned, contents ignored.  A page must be in the free list
- * and the tables once at most; pages outside [0, num_pages) count as lacking
- * afterwards.  Asynchronous on `stream`.  Returns a pdec_status.
+ * and the tables once at most, but for pages that several sequences read and none
+ * writes (a prefix of whole pages that they share): those stand in all their rows.
+ * Pages outside [0, num_pages) count as lacking afterwards.  Asynchronous on
+ * `stream`.  Returns a pdec_status.
  */
 int pdec_paged_reserve(const pdec_table_dims* dims, const int32_t* new_tokens, const int32_t* seq_lens,
                        int32_t* block_table, const int32_t* free_pages, const int32_t* free_in, int32_t* free_out,
@@ -745,8 +747,11 @@ int pdec_paged_reserve(const pdec_table_dims* dims, const int32_t* new_tokens, c
  * accepted length, one with a sliding window its last keys.  The entries become -1, the
  * pages go to the end of the free list in the opposite order of the reservation (from
  * the last sequence's last entry), so that a reservation of the same keys takes them
- * again.  Arrays as above (free_pages is written).  Asynchronous on `stream`.
- * Returns a pdec_status.
+ * again.  Users of a page are not counted: sequences that share a prefix's pages keep
+ * at least the prefix (keep_from 0, keep_len its length), also those that have ended,
+ * until the last one that has them gives them back with its own; the others' rows
+ * are then overwritten by the caller.  Arrays as above (free_pages is written).
+ * Asynchronous on `stream`.  Returns a pdec_status.
  */
 int pdec_paged_release(const pdec_table_dims* dims, const int32_t* keep_from, const int32_t* keep_len,
                        int32_t* block_table, int32_t* free_pages, const int32_t* free_in, int32_t* free_out,
@@ -764,8 +769,10 @@ int pdec_paged_release(const pdec_table_dims* dims, const int32_t* keep_from, co
  *                       is divided by factor, the first pair's stays;
  *   PDEC_ROPE_BY_PARTS  u_i f_i + (1 - u_i) f_i / factor, u_i = (turns_i - slow_turns) /
  *                       (fast_turns - slow_turns) within [0, 1], turns_i = original_len
- *                       f_i / 2 pi the pair's turns over the trained length;
+ *                       f_i / 2 pi the pair's turns over the trained length (weights made
+ *                       with a ramp over the pair's number i instead take a table);
  *   PDEC_ROPE_TABLE     freqs[i], from device memory.
+ * A token has one position, by which all its pairs turn.
  * Angles are formed in double.  float32 rows turn in double and are rounded once,
  * bfloat16 rows in float32.
  */

@@ -55,9 +55,10 @@ template <> struct RopeReal<float> { typedef double type; };
 // Stores to global memory, where the compiler can not tell by itself that it is.
 typedef __attribute__((address_space(1))) u32x4_t rope_global_t;
 __device__ inline void rope_store(void* p, u32x4_t x) { *(rope_global_t*)(uintptr_t)p = x; }
-// Past the caches' working set.  The append's rows (queries among them) of 8192 tokens of 36
-// heads of 128 (151 MB) took 38 us kept in the caches and take 28, of 16384 68 and 63; up to
-// 4096 the two are alike, alone and with a reader of the queries behind.  (Rows turned alone keep
+// Past the caches' working set.  The append's rows (queries among them) of 4096 tokens of 36
+// heads of 128 (75 MB) took 19.7 us kept in the caches and take 16.3, of 8192 39 and 35, of 16384
+// 68 and 63; with a reader of the queries behind 29.7 and 29.2, 55.5 and 54.7, 109 and 105; up to
+// 2048 the two are alike.  (Rows turned alone keep
 // the caches, as who reads them next gains more: float32 gradients, 262 MB, past them and not: 52
 // and 56 us into memory of their own, 52 and 48 into that of the call before, of which some is
 // still cached, 99 and 87 with a reader of the turned queries behind; 131 MB 25 and 31, 25 and 26,

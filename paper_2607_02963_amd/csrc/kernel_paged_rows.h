@@ -21,7 +21,8 @@
 //
 // 4-bit pages (paged_e2m1.h): the same, with half the bytes and, a word being eight
 // elements of one scale, one 16-byte store for four widening instructions: 2048 tokens
-// over 32768 keys of 28 heads of 128 over 4 take 890 us, 1045 TFLOP/s.
+// over 32768 keys of 28 heads of 128 over 4 take 885 to 930 us by the card, 1000 to 1055
+// TFLOP/s.
 //
 // Units that all rows of a wave see whole take that pipelined loop.  Units
 // with hidden keys (the chunk's own tokens, the sequence's end, absent pages)

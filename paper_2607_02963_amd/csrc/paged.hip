@@ -177,7 +177,8 @@ int plan_attn(const pdec_paged_dims* d, AttnPlan& p)
         if (!f32 && !four && (d->cache_dtype == PDEC_DTYPE_E4M3 || d->head_dim == 64) && a.H_kv % 2 == 0) p.few.heads = 2;
         // a start's price, in positions; over 4-bit pages, whose units are the shortest, it was swept.  Units of
         // one tile (4, 8, 16, 24, 32): 32 tokens over 1200 to 16384 keys, heads of 128, 44.2, 42.7, 40.5, 41.1,
-        // 41.3 us.  Items of more rows, whose units are 3 positions and up (paged_price; 36, 48, 72, 96): 2 to 9
+        // 41.3 us; heads of 64 (8, 16, 24, 32, 48): 20 tokens over 1000 to 8000 keys 23.7, 22.0, 21.7, 22.4, 23.8, 40
+        // over 2000 to 30000 79, 77, 76, 76, 75.6, and of five batches more all within 3% of their best at 24.  Items of more rows, whose units are 3 positions and up (paged_price; 36, 48, 72, 96): 2 to 9
         // drafted tokens of 13 sequences, heads of 64, -, 25.9, 24.7, 25.7, 1 to 4 of 32 sequences, heads of 128,
         // 47.7, 47.1, 45.9, - (units alike, at the best price: 25.5, 49.1)
         const bool weighed = four && p.few.rows > 16;
