@@ -26,8 +26,8 @@
 // of their 24 bits each: exact, and 4-bit keys and values are exact in bfloat16, so that
 // three products are the float32 product, at the rate of the bfloat16 ones (a third of
 // 1200 TFLOP/s against 154 on the float32 matrix product): 512 tokens over 4000 keys,
-// 28 heads of 128, took 389 us on the float32 product and take 134; 32 single tokens over
-// 3000 keys 51 and 28.
+// 28 heads of 128, took 389 us on the float32 product and take 124; 32 tokens of one sequence
+// over 3000 keys 51 and 19.5, one of each of 32 sequences 27.3 (53 MB).
 //
 // What bounds it: the bytes and the parts' starts and ends.  One token of each of 32
 // sequences of 1200 to 16384 keys, 28 heads of 128 over 4 (153.5 MB): 40 us as a call;
@@ -40,8 +40,8 @@
 // Up to three tiles of 16 rows at D = 128, four at D = 64 (one and two in float32): one more
 // and the state leaves the registers.  So many are worked on one (D = 128) or two (D = 64)
 // after the other, keys and values widened anew, with the queries in LDS: 5 tokens of 32
-// sequences, 35 rows of 128, 70.5 us (all tiles at once, spilling, 133; the kernel for many
-// rows 109), 13 of 20 sequences, 52 rows of 64, 47 (60; 66).  With four tiles at D = 128, 64
+// sequences, 35 rows of 128, 72 us (all tiles at once, spilling, 133; the kernel for many
+// rows 109), 13 of 20 sequences, 52 rows of 64, 48 (60; 66).  With four tiles at D = 128, 64
 // rows of 16 sequences took 32.6 us, of the kernel for many rows 26.6.  bfloat16 batches of
 // more rows take that, float32 ones more items of these.
 #pragma once

@@ -16,7 +16,7 @@
 // What bounds it: the chain of memory round trips: lengths, entries, the sums, the free
 // list, the entries again.  32 sequences a token each: 5.8 us on the device, 7.6 as a call.
 // 1500 sequences of up to 511 new tokens and 9000 keys (300000 tokens served), reserved and released:
-// 27.2 us for the two calls; the kernels 3.3 and 14.5, 3.2 and 7.9, of which positions and
+// 27.5 us for the two calls; the kernels 3.3 and 14.9, 3.3 and 7.9, of which positions and
 // slots are 3.7.
 #pragma once
 

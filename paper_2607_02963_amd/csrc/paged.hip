@@ -194,10 +194,11 @@ size_t workspace_of(const AttnPlan& p) { return std::max<size_t>(align256(p.few_
 // Tokens from which a wave of the append takes four: 16384 tokens of 4 heads of 128 took
 // 15.3 us by one and take 12.0; up to 4096 both take the call's own 8.9.
 constexpr int kAppendMany = 2048;
-// Dense bytes from which the rows of a 4-bit cache, four times its own bytes, pass the caches by.  Rows of
-// 4 heads of 128 by themselves, kept and past them: 20000 (41 MB) 10.6 and 10.0 us, 30000 14.2 and 13.4, 60000
-// 28.8 and 24.5 (30700 with 7600 appended before 25.5 and 21.4); with readers of both tensors behind: 16000 21
-// and 23, 20000 26.2 and 27.8, 30000 37.5 and 37.9, 60000 70.4 and 67.8; up to 12000 alike.
+// Dense bytes from which the rows of a 4-bit cache, four times its own bytes, pass the caches by.  They
+// are read back to be read: with readers of both tensors behind, in a graph, kept and past the caches: 1000
+// rows of 4 heads of 128 (2 MB) 7.8 and 8.0 us, 5000 to 12000 alike, 16000 (33 MB) 21.0 and 22.7, 24000 (49 MB)
+// 28.9 and 31.3, 30000 37.5 and 37.6, 60000 70.3 and 67.6.  By themselves 5000 5.1 and 4.3, 16000 8.9 and 7.6,
+// 30000 14.3 and 13.5, 60000 28.9 and 24.6 (30700 with 7600 appended before 25.5 and 21.4).
 constexpr int64_t kReadOnce = 48 << 20;
 constexpr int kReadRows = 4;  // rows per wave of the read-back (32768 rows: 24.2 us, by 8 26.8, by 16 25.7)
 
